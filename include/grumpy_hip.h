@@ -31,6 +31,8 @@
  *   - Supported element types: f32 and i32 for computation; i64 only as the
  *     result of an i32 sum (NumPy's default on Linux).  Mixed i32/f32
  *     arithmetic would promote to f64 in NumPy and is refused
+ *     (GR_ERR_DTYPE).  bf16 leaves and views of them are operands and results of
+ *     the calls of grumpy_hip_attention.h; every other call refuses them
  *     (GR_ERR_DTYPE).
  */
 #ifndef GRUMPY_HIP_H
@@ -61,7 +63,7 @@ typedef enum {
   GR_ERR_NODEVICE = 11    /* context was created without a device */
 } gr_status;
 
-typedef enum { GR_F32 = 0, GR_I32 = 1, GR_I64 = 2 } gr_dtype;
+typedef enum { GR_F32 = 0, GR_I32 = 1, GR_I64 = 2, GR_BF16 = 3 } gr_dtype;
 
 typedef enum {
   /* unary (Section 1 / Section 2: pointwise NumPy operations) */

@@ -11,22 +11,43 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgrumpy_hip.so")
-SOURCES = ["recorder.cpp", "plan.cpp", "codegen.cpp", "runtime.cpp", "interp.cpp", "plancache.cpp", "stream_kernels.hip", "interp_kernel.hip", "static_scratch.hip"]
+SOURCES = ["recorder.cpp", "plan.cpp", "codegen.cpp", "runtime.cpp", "interp.cpp", "plancache.cpp", "stream_kernels.hip", "interp_kernel.hip", "static_scratch.hip",
+           "attention.cpp", "attention_parts.hip", "rotary.hip", "attention_forward_bf16.hip", "attention_forward_f32.hip", "attention_grad_q_bf16.hip", "attention_grad_q_f32.hip",
+           "attention_grad_kv_bf16.hip", "attention_grad_kv_f32.hip"]
+
+
+def compile_parallel(cmd, lib, link):
+    """Compiles SOURCES with `cmd`, one compiler process per file, in parallel, and links them to `lib`; returns what the compiler said."""
+    import concurrent.futures
+    import tempfile
+    with tempfile.TemporaryDirectory(prefix="grumpy_build_") as tmp:
+        def run(args, what):
+            r = subprocess.run(args, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            # hipcc's host pass warns that it does not know the packed-fp32 feature: harmless, filtered
+            out = "\n".join(l for l in r.stdout.splitlines() if "is not a recognized feature for this target" not in l)
+            if r.returncode != 0:
+                raise RuntimeError(f"hipcc failed on {what}:\n" + out)
+            return out
+
+        def compile_one(src):
+            obj = os.path.join(tmp, src + ".o")
+            return obj, run(cmd + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj], src)
+        with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            # (the longest first)
+            done = dict(zip(SOURCES[::-1], pool.map(compile_one, SOURCES[::-1])))
+        said = [done[s][1] for s in SOURCES]
+        said.append(run(cmd + link + ["-shared", "-o", lib] + [done[s][0] for s in SOURCES] + ["-lhiprtc"], os.path.basename(lib)))
+    return "\n".join(t for t in said if t.strip())
 
 
 def build(verbose: bool = False, pack: bool = True) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, "--offload-arch=gfx950", "-O2", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
+    cmd = [hipcc, "--offload-arch=gfx950", "-O2", "-std=c++17", "-fPIC", "-ffp-contract=off",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
-           "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES] + ["-lhiprtc"]
+           "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]
     if verbose:
         print(" ".join(cmd))
-    # hipcc's host pass warns that it does not know the packed-fp32 feature: harmless, filtered
-    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in r.stdout.splitlines() if "is not a recognized feature for this target" not in l)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+    out = compile_parallel(cmd, LIB, [])
     if verbose and out.strip():
         print(out)
     build_fastbind(verbose)
@@ -56,27 +77,13 @@ def build_sanitized(verbose: bool = False) -> str:
     drive the host logic through a device-less context in dry-run mode (tests/test_sanitized_host.py): a process
     that loads it sets GRUMPY_HIP_LIB to the path returned and preloads sanitizer_runtime().  One compiler process
     per source file, in parallel."""
-    import concurrent.futures
-    import tempfile
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     common = [hipcc, "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-fPIC", "-ffp-contract=off",
               "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option",
               "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined"]
-    with tempfile.TemporaryDirectory(prefix="grumpy_san_") as tmp:
-        def compile_one(src):
-            obj = os.path.join(tmp, src + ".o")
-            r = subprocess.run(common + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-            if r.returncode != 0:
-                raise RuntimeError(f"hipcc failed on {src}:\n" + r.stdout)
-            return obj
-        with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
-            objs = list(pool.map(compile_one, SOURCES))
-        cmd = common + ["-shared", "-shared-libsan", "-o", SAN_LIB] + objs + ["-lhiprtc"]
-        if verbose:
-            print(" ".join(cmd))
-        r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-        if r.returncode != 0:
-            raise RuntimeError("linking the sanitized library failed:\n" + r.stdout)
+    out = compile_parallel(common, SAN_LIB, ["-shared-libsan"])
+    if verbose and out.strip():
+        print(out)
     return SAN_LIB
 
 

@@ -1,0 +1,429 @@
+// The gradient of attention.  With p = exp(score - lse), t the tanh of a capped score and delta = sum over d of dout * out:
+//   dv = p^T dout,   dp = dout v^T,   ds = p (dp - delta) (1 - t^2) scale,   dq = ds k,   dk = ds^T q.
+// p is formed again from q, k and lse.  Two kernels, so that every sum stays in registers of one workgroup and its order is fixed
+// (no atomic additions, the same bits from call to call):
+//   gr_attention_grad_q   walks the keys for 128 rows of queries, as the forward kernel does;
+//   gr_attention_grad_kv  walks the queries of all heads that share a head of k and v for a block of keys.
+// Probabilities are carried 2^32 times as large (LIFT, taken out of the sums in the end), so that those below float32's normal numbers
+// still count in the gradients of keys that every query all but ignores; there is room for it above.
+// They form q k^T and dout v^T twice, 7 products of the size of q k^T where a single kernel would have 5 and an addition to dq in memory
+// per tile.
+#pragma once
+
+#include "attention_kernels.h"
+
+namespace gr {
+namespace attn {
+
+template <class T, int DP>
+struct ShapeQ {
+  static constexpr int THREADS = 256, KEYS = tile_rows(sizeof(T), DP), ROWS = 128, TILE = KEYS * Tile<T, DP>::ROW;
+  static constexpr int LDS = 4 * TILE + 256;
+  static constexpr int REGS = DP / 16 * 4 * (int)sizeof(T) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
+  static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+};
+
+template <class T, int DP, int MODE>
+__global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_grad_q_kernel(const Args a) {
+  typedef ShapeQ<T, DP> S;
+  typedef Tile<T, DP> L;
+  typedef typename Frag<T>::type F;
+  extern __shared__ char smem_[];
+  GR_LDS char* const smem = (GR_LDS char*)smem_;
+  GR_LDS int* const shared = (GR_LDS int*)(smem + 4 * S::TILE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
+  const Place place = place_of(blockIdx.x, a.B * a.HK, a.blocks);
+  if (place.block >= a.blocks) return;
+  const int rb = a.blocks - 1 - place.block;
+  const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
+  const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + wave * 32;
+  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int row = wrow0 + col;
+  const bool valid = row < R;
+  const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
+  const int see = valid ? keys_seen(a, i, len, pre) : 0;
+  const int i_last = (row0 + S::ROWS <= R ? row0 + S::ROWS - 1 : R - 1) / a.G;
+  const int end = keys_seen(a, i_last, len, pre);
+  const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
+  const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
+  int doc = -1, w_lo = 0x7fffffff, w_hi = -1, w_all = 0x7fffffff, lo = 0, up = 0;
+  if (a.kdoc) {
+    if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
+    w_lo = doc >= 0 ? doc : 0x7fffffff; w_hi = doc; w_all = valid ? doc : 0x7fffffff;
+    for (int m = 16; m; m >>= 1) {
+      w_lo = min(w_lo, __shfl_xor(w_lo, m)); w_hi = max(w_hi, __shfl_xor(w_hi, m)); w_all = min(w_all, __shfl_xor(w_all, m));
+    }
+    w_lo = __builtin_amdgcn_readfirstlane(w_lo); w_hi = __builtin_amdgcn_readfirstlane(w_hi); w_all = __builtin_amdgcn_readfirstlane(w_all);
+    if (lane == 0) { shared[2 * wave] = w_lo; shared[2 * wave + 1] = w_hi; }
+    __syncthreads();
+    lo = 0x7fffffff; up = -1;
+    for (int w = 0; w < 4; ++w) { lo = min(lo, shared[2 * w]); up = max(up, shared[2 * w + 1]); }
+    lo = __builtin_amdgcn_readfirstlane(lo); up = __builtin_amdgcn_readfirstlane(up);
+  }
+  const int pieces = (a.M + 31) / 32;
+  const int* const ranges = a.kdoc ? a.kranges + (int64_t)b * pieces * 2 : nullptr;
+  Finder<S::KEYS / 32> find{ranges, pieces, lo, up};
+
+  F qf[L::STEPS], df[L::STEPS];
+  {
+    const T* q = at<T>(a.q, b, i, h);
+    const T* d = at<T>(a.dout, b, i, h);
+#pragma unroll
+    for (int s = 0; s < L::STEPS; ++s) { qf[s] = L::fetch(q, s, hi, a.D, valid, a.q.aligned); df[s] = L::fetch(d, s, hi, a.D, valid, a.dout.aligned); }
+  }
+  const int64_t stat = ((int64_t)b * a.H + h) * a.N + i;
+  // a row that sees nothing has lse = -inf: its probabilities are 2^-inf
+  const float lse_ = valid ? a.lse[stat] : -INF, less = lse_ == -INF ? INF : lse_ * LOG2E - LIFT, delta = valid ? a.delta[stat] : 0.0f;
+  // (an lse of 2^20 and more is rounded by as much as an exponent counts: no probability passes 1 for that)
+  const bool huge = __any(less != INF && __builtin_fabsf(less) > 1048576.0f);
+  const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
+  const float pos = MODE & MODE_BIAS ? (float)(a.position + i) : 0.0f;
+
+  f32x16 o[L::BLOCKS];
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d) o[d] = (f32x16)0.0f;
+
+  const int tiles = (end + S::KEYS - 1) / S::KEYS;
+  const T* const kbase = at<T>(a.k, b, 0, hk);
+  const T* const vbase = at<T>(a.v, b, 0, hk);
+  auto load = [&](int t, int stage) {
+    const int64_t k0 = (int64_t)t * S::KEYS;
+    const int rows = min(S::KEYS, len - (int)k0);
+    L::template load<S::KEYS, 256>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, tid, a.k.direct);
+    L::template load<S::KEYS, 256>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, tid, a.v.direct);
+  };
+  int t = find.next(0, tiles, lane), stage = 0;
+  if (t < tiles) load(t, 0);
+  while (t < tiles) {
+    const int after = find.next(t + 1, tiles, lane);
+    arrive();
+    if (after < tiles) load(after, stage ^ 1);
+    const GR_LDS char* const kt = smem + 2 * stage * S::TILE;
+    const GR_LDS char* const vt = kt + S::TILE;
+#pragma unroll 1
+    for (int kb = 0; kb < S::KEYS / 32; ++kb) {
+      const int key0 = t * S::KEYS + kb * 32;
+      if (key0 >= w_last) break;
+      bool whole = key0 + 32 <= w_first;
+      if (ranges) whole = whole && ranges[2 * (key0 / 32)] == w_hi && ranges[2 * (key0 / 32) + 1] == w_hi && w_all == w_hi;
+      f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
+#pragma unroll
+      for (int st = 0; st < L::STEPS; ++st) {
+        s = mma(L::row(kt, kb * 32 + col, st, hi), qf[st], s);
+        dp = mma(L::row(vt, kb * 32 + col, st, hi), df[st], dp);
+      }
+      finished(s, dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = key0 + (r & 3) + 8 * (r >> 2) + 4 * hi;
+        float y = s[r], bend = 1.0f;
+        if constexpr (MODE & MODE_CAP) { y = capped<T, MODE>(y, a.cin); bend = __builtin_fmaf(-y, y, 1.0f); }
+        if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf(pos - (float)key), -less));
+        else y = __builtin_fmaf(y, a.c, -less);
+        s[r] = y;
+        dp[r] -= delta;
+        if constexpr (MODE & MODE_CAP) dp[r] *= bend;
+      }
+      if (huge) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_fminf(s[r], LIFT);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]) * dp[r];
+      if (!whole) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = key0 + (r & 3) + 8 * (r >> 2) + 4 * hi;
+          bool seen = key < see;
+          if (a.kdoc && seen) seen = doc >= 0 && a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn] == doc;
+          s[r] = seen ? s[r] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        F f;
+        operand(s, st, f);
+#pragma unroll
+        for (int d = 0; d < L::BLOCKS; ++d) o[d] = mma(L::column(kt, kb * 32 + st * 16, d, lane), f, o[d]);
+      }
+    }
+    t = after;
+    stage ^= 1;
+  }
+  finished(o);
+  if (!valid) return;
+  T* const dq = at<T>(a.dq, b, i, h);
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const float by = a.scale * UNLIFT, x[4] = {o[d][r] * by, o[d][r + 1] * by, o[d][r + 2] * by, o[d][r + 3] * by};
+      store4(dq, d * 32 + 2 * r + 4 * hi, a.D, x, a.dq.aligned);
+    }
+}
+
+// Which of dk and dv a launch forms: both, or, where the operands and sums of both do not fit a lane's registers, one each.
+enum { BOTH = 0, ONLY_V = 1, ONLY_K = 2 };
+
+template <class T, int DP, int WHICH>
+struct ShapeKV {
+  static constexpr int ROWS = tile_rows(sizeof(T), DP), KEYS = 128, TILE = ROWS * Tile<T, DP>::ROW;   // rows: of a tile of queries
+  static constexpr int STATS = 4 * ROWS + 4;                 // four numbers per row, and whether any lse is huge
+  static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
+  static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
+  static constexpr int PER_CU = REGS <= 240 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+};
+
+template <class T, int DP, int MODE, int WHICH>
+__global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_attention_grad_kv_kernel(const Args a) {
+  typedef ShapeKV<T, DP, WHICH> S;
+  typedef Tile<T, DP> L;
+  typedef typename Frag<T>::type F;
+  constexpr bool WANT_K = WHICH != ONLY_V, WANT_V = WHICH != ONLY_K;
+  extern __shared__ char smem_[];
+  GR_LDS char* const smem = (GR_LDS char*)smem_;
+  GR_LDS float* const stats = (GR_LDS float*)(smem + 4 * S::TILE);   // [stage][less, delta, keys seen, document][row]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
+  const int pairs = a.B * a.HK;
+  const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
+  if (place.block >= a.blocks * a.splits) return;
+  const int split = place.block % a.splits, kblock = place.block / a.splits;   // the first keys are seen by the most queries
+  const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
+  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int block0 = kblock * S::KEYS, key0 = block0 + wave * 32, key = key0 + col;
+  const bool valid = key < len;
+
+  int doc = -1, lo = 0, up = 0, w_doc = -1;
+  bool w_one = false;
+  const int kpieces = (a.M + 31) / 32, qpieces = (a.N + 31) / 32;
+  if (a.kdoc) {
+    if (valid) doc = a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn];
+    lo = 0x7fffffff; up = -1;
+    const int* kr = a.kranges + (int64_t)b * kpieces * 2;
+    for (int e = block0 / 32; e < block0 / 32 + 4 && e < kpieces; ++e) {
+      // (numbers below zero belong to no document; a piece of nothing else has no largest)
+      const int l = kr[2 * e] < 0 ? 0 : kr[2 * e], u = kr[2 * e + 1];
+      if (u >= 0) { lo = min(lo, l); up = max(up, u); }
+      if (e == key0 / 32) { w_one = kr[2 * e] == u && u >= 0; w_doc = u; }
+    }
+  }
+  const int* const ranges = a.kdoc ? a.qranges + (int64_t)b * qpieces * 2 : nullptr;
+
+  F kf[L::STEPS], vf[WANT_K ? L::STEPS : 1];
+  {
+    const T* k = at<T>(a.k, b, valid ? key : 0, hk);
+    const T* v = at<T>(a.v, b, valid ? key : 0, hk);
+#pragma unroll
+    for (int s = 0; s < L::STEPS; ++s) {
+      kf[s] = L::fetch(k, s, hi, a.D, valid, a.k.aligned);
+      if constexpr (WANT_K) vf[s] = L::fetch(v, s, hi, a.D, valid, a.v.aligned);
+    }
+  }
+  f32x16 ok[WANT_K ? L::BLOCKS : 1], ov[WANT_V ? L::BLOCKS : 1];
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d) {
+    if constexpr (WANT_K) ok[d] = (f32x16)0.0f;
+    if constexpr (WANT_V) ov[d] = (f32x16)0.0f;
+  }
+
+  // The queries that see a key of the block: all from the first one that does, since what a query sees grows with its place.
+  int first = 0;
+  if (block0 >= len) first = a.N;
+  else if (a.causal && block0 >= pre) {
+    const int64_t f = (int64_t)block0 - a.position;
+    first = f < 0 ? 0 : f < a.N ? (int)f : a.N;
+  }
+  const int t0 = first / S::ROWS, tiles = (a.N + S::ROWS - 1) / S::ROWS, span = first < a.N ? tiles - t0 : 0;
+  // units: tiles of the first head, of the second, ..; a split takes a run of them
+  const int64_t units = (int64_t)span * a.G;
+  const int u0 = (int)(units * split / a.splits), u1 = (int)(units * (split + 1) / a.splits);
+
+  Finder<S::ROWS / 32> find{ranges, qpieces, lo, up};
+  // the unit at or after u that has something to do
+  auto next = [&](int u) {
+    while (u < u1) {
+      const int g = u / span, t = t0 + (u - g * span), n = find.next(t, tiles, lane);
+      if (n < tiles) return min(u + (n - t), u1);
+      u = (g + 1) * span;
+      find.base = -1;
+    }
+    return u1;
+  };
+  float r_less = 0.0f, r_delta = 0.0f;
+  int r_see = 0, r_doc = -1;
+  auto load = [&](int u, int stage) {
+    const int g = u / span, t = t0 + (u - g * span), h = hk * a.G + g;
+    const int64_t i0 = (int64_t)t * S::ROWS;
+    const int rows = min(S::ROWS, a.N - (int)i0);
+    L::template load<S::ROWS, 256>(smem + 2 * stage * S::TILE, at<T>(a.q, b, i0, h), a.q.sn, rows, a.D, tid, a.q.direct);
+    L::template load<S::ROWS, 256>(smem + (2 * stage + 1) * S::TILE, at<T>(a.dout, b, i0, h), a.dout.sn, rows, a.D, tid, a.dout.direct);
+    if (tid < S::ROWS) {
+      const bool in = tid < rows;
+      const int i = (int)i0 + (in ? tid : 0);
+      const int64_t stat = ((int64_t)b * a.H + h) * a.N + i;
+      const float e = in ? a.lse[stat] : -INF;
+      r_less = e == -INF ? INF : e * LOG2E - LIFT;
+      r_delta = in ? a.delta[stat] : 0.0f;
+      r_see = in ? keys_seen(a, i, len, pre) : 0;
+      r_doc = in && a.kdoc ? a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn] : -1;
+    }
+  };
+  auto settle = [&](int stage) {
+    if (tid < S::ROWS) {
+      GR_LDS float* const to = stats + stage * S::STATS;
+      to[tid] = r_less;
+      to[S::ROWS + tid] = r_delta;
+      ((GR_LDS int*)to)[2 * S::ROWS + tid] = r_see;
+      ((GR_LDS int*)to)[3 * S::ROWS + tid] = r_doc;
+      // (an lse of 2^20 and more is rounded by as much as an exponent counts: no probability passes 1 for that)
+      const bool huge = __any(r_less != INF && __builtin_fabsf(r_less) > 1048576.0f);
+      if (tid == 0) ((GR_LDS int*)to)[4 * S::ROWS] = huge;
+    }
+  };
+  int u = next(u0), stage = 0;
+  if (u < u1) { load(u, 0); settle(0); }
+  while (u < u1) {
+    const int after = next(u + 1);
+    arrive();
+    if (after < u1) load(after, stage ^ 1);
+    const int g = u / span, t = t0 + (u - g * span), h = hk * a.G + g;
+    const GR_LDS char* const qt = smem + 2 * stage * S::TILE;
+    const GR_LDS char* const dt = qt + S::TILE;
+    const GR_LDS float* const st = stats + stage * S::STATS;
+    const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
+    const bool huge = __builtin_amdgcn_readfirstlane(((const GR_LDS int*)st)[4 * S::ROWS]) != 0;
+#pragma unroll 1
+    for (int rb = 0; rb < S::ROWS / 32; ++rb) {
+      const int i0 = t * S::ROWS + rb * 32;
+      if (i0 >= a.N) break;
+      const int see_last = keys_seen(a, min(i0 + 31, a.N - 1), len, pre);
+      if (see_last <= key0) continue;
+      // (rows behind the last query need no mask: their lse is none)
+      bool whole = keys_seen(a, i0, len, pre) >= key0 + 32;
+      if (ranges) whole = whole && w_one && ranges[2 * (i0 / 32)] == w_doc && ranges[2 * (i0 / 32) + 1] == w_doc;
+      f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
+#pragma unroll
+      for (int x = 0; x < L::STEPS; ++x) {
+        s = mma(L::row(qt, rb * 32 + col, x, hi), kf[x], s);
+        if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + col, x, hi), vf[x], dp);
+      }
+      if constexpr (WANT_K) finished(s, dp);
+      else finished(s);
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int rr = rb * 32 + 8 * r4 + 4 * hi;
+        const f32x4 less = *(const GR_LDS f32x4*)(st + rr), delta = *(const GR_LDS f32x4*)(st + S::ROWS + rr);
+        const i32x4 see = whole ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rr), docs = whole ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 3 * S::ROWS + rr);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * r4 + e;
+          float y = s[r], bend = 1.0f;
+          if constexpr (MODE & MODE_CAP) { y = capped<T, MODE>(y, a.cin); bend = __builtin_fmaf(-y, y, 1.0f); }
+          float x;
+          if constexpr (MODE & MODE_BIAS) x = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf((float)(a.position + t * S::ROWS + rr + e) - (float)key), -less[e]));
+          else x = __builtin_fmaf(y, a.c, -less[e]);
+          float p = exp2_(huge ? __builtin_fminf(x, LIFT) : x);
+          if (!whole) {
+            bool seen = key < see[e];
+            if (a.kdoc) seen = seen && doc >= 0 && docs[e] == doc;
+            p = seen ? p : 0.0f;
+          }
+          s[r] = p;
+          if constexpr (WANT_K) {
+            float d = p * (dp[r] - delta[e]);
+            if constexpr (MODE & MODE_CAP) d *= bend;
+            if (!whole) d = p == 0.0f ? 0.0f : d;    // (masked, or too small to count)
+            dp[r] = d;
+          }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        F f;
+        if constexpr (WANT_V) {
+          operand(s, x, f);
+#pragma unroll
+          for (int d = 0; d < L::BLOCKS; ++d) ov[d] = mma(L::column(dt, rb * 32 + x * 16, d, lane), f, ov[d]);
+        }
+        if constexpr (WANT_K) {
+          operand(dp, x, f);
+#pragma unroll
+          for (int d = 0; d < L::BLOCKS; ++d) ok[d] = mma(L::column(qt, rb * 32 + x * 16, d, lane), f, ok[d]);
+        }
+      }
+    }
+    if (after < u1) settle(stage ^ 1);
+    u = after;
+    stage ^= 1;
+  }
+  if constexpr (WANT_K) finished(ok);
+  if constexpr (WANT_V) finished(ov);
+  if (key >= a.M) return;
+  if (a.splits > 1) {
+    // (splits, 2, B * HK, M, DP)
+    const int64_t plane = (int64_t)pairs * a.M * DP, to = ((int64_t)place.pair * a.M + key) * DP + 2 * split * plane;
+#pragma unroll
+    for (int d = 0; d < L::BLOCKS; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int n = d * 32 + 2 * r + 4 * hi;
+        if constexpr (WANT_K) { const f32x4 x = {ok[d][r], ok[d][r + 1], ok[d][r + 2], ok[d][r + 3]}; *(f32x4*)(a.part_o + to + n) = x; }
+        if constexpr (WANT_V) { const f32x4 x = {ov[d][r], ov[d][r + 1], ov[d][r + 2], ov[d][r + 3]}; *(f32x4*)(a.part_o + plane + to + n) = x; }
+      }
+    return;
+  }
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int n = d * 32 + 2 * r + 4 * hi;
+      if constexpr (WANT_K) {
+        const float by = a.scale * UNLIFT, x[4] = {ok[d][r] * by, ok[d][r + 1] * by, ok[d][r + 2] * by, ok[d][r + 3] * by};
+        store4(at<T>(a.dk, b, key, hk), n, a.D, x, a.dk.aligned);
+      }
+      if constexpr (WANT_V) {
+        const float x[4] = {ov[d][r] * UNLIFT, ov[d][r + 1] * UNLIFT, ov[d][r + 2] * UNLIFT, ov[d][r + 3] * UNLIFT};
+        store4(at<T>(a.dv, b, key, hk), n, a.D, x, a.dv.aligned);
+      }
+    }
+}
+
+template <class T, int DP, int MODE>
+static hipError_t grad_q_one(const Args& a, unsigned grid, hipStream_t stream) {
+  gr_attention_grad_q_kernel<T, DP, MODE><<<dim3(grid), dim3(256), ShapeQ<T, DP>::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <class T, int DP, int MODE, int WHICH>
+static hipError_t grad_kv_part(const Args& a, unsigned grid, hipStream_t stream) {
+  gr_attention_grad_kv_kernel<T, DP, MODE, WHICH><<<dim3(grid), dim3(256), ShapeKV<T, DP, WHICH>::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <class T, int DP, int MODE>
+static hipError_t grad_kv_one(const Args& a, unsigned grid, hipStream_t stream) {
+  if constexpr (sizeof(T) * DP >= 1024) {
+    const hipError_t e = grad_kv_part<T, DP, MODE, ONLY_V>(a, grid, stream);
+    return e != hipSuccess ? e : grad_kv_part<T, DP, MODE, ONLY_K>(a, grid, stream);
+  } else {
+    return grad_kv_part<T, DP, MODE, BOTH>(a, grid, stream);
+  }
+}
+
+#define GR_BY_SHAPE(F)                                                                                            \
+  switch (dp * 4 + mode) {                                                                                        \
+    case 256: return F<T, 64, 0>(a, grid, stream); case 257: return F<T, 64, 1>(a, grid, stream);                 \
+    case 258: return F<T, 64, 2>(a, grid, stream); case 259: return F<T, 64, 3>(a, grid, stream);                 \
+    case 384: return F<T, 96, 0>(a, grid, stream); case 385: return F<T, 96, 1>(a, grid, stream);                 \
+    case 386: return F<T, 96, 2>(a, grid, stream); case 387: return F<T, 96, 3>(a, grid, stream);                 \
+    case 512: return F<T, 128, 0>(a, grid, stream); case 513: return F<T, 128, 1>(a, grid, stream);               \
+    case 514: return F<T, 128, 2>(a, grid, stream); case 515: return F<T, 128, 3>(a, grid, stream);               \
+    case 1024: return F<T, 256, 0>(a, grid, stream); case 1025: return F<T, 256, 1>(a, grid, stream);             \
+    case 1026: return F<T, 256, 2>(a, grid, stream); default: return F<T, 256, 3>(a, grid, stream);               \
+  }
+template <class T>
+static hipError_t grad_q_all(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream) { GR_BY_SHAPE(grad_q_one) }
+template <class T>
+static hipError_t grad_kv_all(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream) { GR_BY_SHAPE(grad_kv_one) }
+#undef GR_BY_SHAPE
+
+}  // namespace attn
+}  // namespace gr

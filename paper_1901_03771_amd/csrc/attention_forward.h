@@ -1,0 +1,304 @@
+// The output of attention: out = sum over the keys a query sees of exp(score - lse) v, lse = log(sum of exp(score)).
+//
+// One pass over the keys with a running maximum m and sum l per query (a lane's column, see attention_kernels.h):
+// scores^T = K Q^T, p = 2^(score - m), out^T += V^T p.  m only moves when a score exceeds it by 2^8 or more: any m serves, since it
+// cancels, and p <= 2^8 is far from overflow, so the products so far are rescaled a few times per row and not per tile.
+//
+// The rows of one head of k and v are the queries of all its G heads, query by query: k and v are read once for all of them, and a
+// causal block of 128 rows spans 128 / G positions.  Two forms:
+//   own rows  (DIVIDED = false): each of four waves has 32 rows, all waves walk the same tiles of keys;
+//   own keys  (DIVIDED = true):  up to 32 rows, each wave takes 32 keys of every tile, and the waves' sums are joined at the end:
+//              single tokens and other calls of at most 32 rows per head, whose time is that of reading k and v.
+// Either may split the keys over workgroups as well (a.splits), which leaves (m, l, sums) for combine().
+#pragma once
+
+#include "attention_kernels.h"
+
+namespace gr {
+namespace attn {
+
+template <class T, int DP, bool DIVIDED>
+struct Shape {
+  static constexpr int WAVES = DIVIDED ? shared_waves(sizeof(T), DP) : 4;
+  static constexpr int THREADS = 64 * WAVES;
+  static constexpr int KEYS = DIVIDED ? 32 * WAVES : tile_rows(sizeof(T), DP);   // of a tile
+  static constexpr int KB = DIVIDED ? 1 : KEYS / 32;                              // blocks of 32 keys a wave multiplies
+  static constexpr int ROWS = DIVIDED ? 32 : 32 * WAVES;
+  static constexpr int TILE = KEYS * Tile<T, DP>::ROW;
+  // two stages of a tile of k and one of v; the joining waves' sums lie over them
+  static constexpr int LDS = 4 * TILE + 256;
+  static_assert(!DIVIDED || WAVES * 32 * (DP + 4) * 4 <= 4 * TILE, "the waves' sums fit the stages");
+  // registers: operands of q, sums, scores.  Two workgroups per compute unit where they fit 256.
+  static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) + DP / 2 + 16 * KB;
+  static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+};
+
+template <class T, int DP, int MODE, bool DIVIDED>
+__global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIVIDED>::PER_CU)) void gr_attention_kernel(const Args a) {
+  typedef Shape<T, DP, DIVIDED> S;
+  typedef Tile<T, DP> L;
+  typedef typename Frag<T>::type F;
+  extern __shared__ char smem_[];
+  GR_LDS char* const smem = (GR_LDS char*)smem_;
+  GR_LDS int* const shared = (GR_LDS int*)(smem + 4 * S::TILE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
+  const int pairs = a.B * a.HK;
+  const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
+  if (place.block >= a.blocks * a.splits) return;
+  // the last blocks of rows see the most keys: they start first
+  const int split = place.block % a.splits, rb = a.blocks - 1 - place.block / a.splits;
+  const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
+  const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + (DIVIDED ? 0 : wave * 32);
+  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int row = wrow0 + col;
+  const bool valid = row < R;
+  const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
+  const int see = valid ? keys_seen(a, i, len, pre) : 0;
+  // of the workgroup's rows, and of this wave's: how many keys the last one sees, the first one
+  const int i_last = (row0 + S::ROWS <= R ? row0 + S::ROWS - 1 : R - 1) / a.G;
+  const int end = keys_seen(a, i_last, len, pre);
+  const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
+  const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
+
+  // documents: this lane's, the wave's and the workgroup's smallest and largest
+  int doc = -1, w_lo = 0x7fffffff, w_hi = -1, w_all = 0x7fffffff, lo = 0, up = 0;
+  if (a.kdoc) {
+    if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
+    w_lo = doc >= 0 ? doc : 0x7fffffff; w_hi = doc; w_all = valid ? doc : 0x7fffffff;
+    for (int m = 16; m; m >>= 1) {
+      w_lo = min(w_lo, __shfl_xor(w_lo, m)); w_hi = max(w_hi, __shfl_xor(w_hi, m)); w_all = min(w_all, __shfl_xor(w_all, m));
+    }
+    w_lo = __builtin_amdgcn_readfirstlane(w_lo); w_hi = __builtin_amdgcn_readfirstlane(w_hi); w_all = __builtin_amdgcn_readfirstlane(w_all);
+    if (lane == 0) { shared[2 * wave] = w_lo; shared[2 * wave + 1] = w_hi; }
+    __syncthreads();
+    lo = 0x7fffffff; up = -1;
+    for (int w = 0; w < S::WAVES; ++w) { lo = min(lo, shared[2 * w]); up = max(up, shared[2 * w + 1]); }
+    lo = __builtin_amdgcn_readfirstlane(lo); up = __builtin_amdgcn_readfirstlane(up);
+  }
+  const int pieces = (a.M + 31) / 32;
+  const int* const ranges = a.kdoc ? a.kranges + (int64_t)b * pieces * 2 : nullptr;
+  Finder<S::KEYS / 32> find{ranges, pieces, lo, up};
+
+  // the rows' operands
+  F qf[L::STEPS];
+  {
+    const T* q = at<T>(a.q, b, i, h);
+#pragma unroll
+    for (int s = 0; s < L::STEPS; ++s) qf[s] = L::fetch(q, s, hi, a.D, valid, a.q.aligned);
+  }
+  const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
+  const float pos = MODE & MODE_BIAS ? (float)(a.step ? (int64_t)len - 1 : a.position + i) : 0.0f;
+  const float c = MODE & MODE_BIAS ? 1.0f : a.c;
+
+  f32x16 o[L::BLOCKS];
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d) o[d] = (f32x16)0.0f;
+  float my = -INF, m = -INF, l = 0.0f;   // the running maximum, as y and in binary logarithms
+
+  const int tiles = (end + S::KEYS - 1) / S::KEYS, per = (tiles + a.splits - 1) / a.splits;
+  const int t1 = min(tiles, (split + 1) * per);
+  const T* const kbase = at<T>(a.k, b, 0, hk);
+  const T* const vbase = at<T>(a.v, b, 0, hk);
+  // (rows from the length on are never read: what a cache holds there has no say, not even infinities times zero)
+  auto load = [&](int t, int stage) {
+    const int64_t k0 = (int64_t)t * S::KEYS;
+    const int rows = min(S::KEYS, len - (int)k0);
+    L::template load<S::KEYS, S::THREADS>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, tid, a.k.direct);
+    L::template load<S::KEYS, S::THREADS>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, tid, a.v.direct);
+  };
+  int t = find.next(split * per, t1, lane), stage = 0;
+  if (t < t1) load(t, 0);
+  while (t < t1) {
+    const int after = find.next(t + 1, t1, lane);
+    arrive();
+    if (after < t1) load(after, stage ^ 1);
+    const GR_LDS char* const kt = smem + 2 * stage * S::TILE + (DIVIDED ? wave * 32 * L::ROW : 0);
+    const GR_LDS char* const vt = kt + S::TILE;
+    const int key0 = t * S::KEYS + (DIVIDED ? wave * 32 : 0);
+    if (key0 < w_last) {
+      bool whole = key0 + 32 * S::KB <= w_first;
+      if (ranges) {
+#pragma unroll
+        for (int kb = 0; kb < S::KB; ++kb) {
+          const int e = key0 / 32 + kb;
+          whole = whole && ranges[2 * e] == w_hi && ranges[2 * e + 1] == w_hi && w_all == w_hi;
+        }
+      }
+      f32x16 s[S::KB];
+#pragma unroll
+      for (int kb = 0; kb < S::KB; ++kb) {
+        s[kb] = (f32x16)0.0f;
+#pragma unroll
+        for (int st = 0; st < L::STEPS; ++st) s[kb] = mma(L::row(kt, kb * 32 + col, st, hi), qf[st], s[kb]);
+      }
+      if constexpr (S::KB == 2) finished(s[0], s[1]);
+      else finished(s[0]);
+      if constexpr (MODE != 0) {
+#pragma unroll
+        for (int kb = 0; kb < S::KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float y = s[kb][r];
+            if constexpr (MODE & MODE_CAP) y = capped<T, MODE>(y, a.cin);
+            if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, -slope * __builtin_fabsf(pos - (float)(key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi)));
+            s[kb][r] = y;
+          }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int kb = 0; kb < S::KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi;
+            bool seen = key < see;
+            if (a.kdoc && seen) seen = doc >= 0 && a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn] == doc;
+            s[kb][r] = seen ? s[kb][r] : -INF;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < S::KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kb][r]);
+      top = max_halves(top);
+      if (__any(top * c > m + 8.0f)) {
+        const float to = __builtin_fmaxf(my, top), by = to == -INF ? 1.0f : exp2_((my - to) * c);
+        my = to;
+        m = to * c;
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < L::BLOCKS; ++d) o[d] *= by;
+      }
+      const float less = m == -INF ? 0.0f : m;
+      // (scores of 2^20 and more: m is rounded by as much as an exponent counts, so the difference is taken before the product)
+      const bool huge = __any(__builtin_fabsf(less) > 1048576.0f);
+#pragma unroll
+      for (int kb = 0; kb < S::KB; ++kb) {
+        if (huge) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = exp2_((s[kb][r] - (my == -INF ? 0.0f : my)) * c);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = exp2_(__builtin_fmaf(s[kb][r], c, -less));
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) l += s[kb][r];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          F p;
+          operand(s[kb], st, p);
+#pragma unroll
+          for (int d = 0; d < L::BLOCKS; ++d) o[d] = mma(L::column(vt, kb * 32 + st * 16, d, lane), p, o[d]);
+        }
+      }
+    }
+    t = after;
+    stage ^= 1;
+  }
+  finished(o);
+  l = sum_halves(l);
+
+  if constexpr (DIVIDED) {
+    // the waves' sums: each scaled to the largest maximum, added in the order of the waves
+    GR_LDS float* const sums = (GR_LDS float*)smem;          // [wave][row][DP + 4]
+    constexpr int PITCH = DP + 4;
+    __syncthreads();
+    if (hi == 0) { sums[(wave * 32 + col) * PITCH + DP] = m; sums[(wave * 32 + col) * PITCH + DP + 1] = l; }
+    __syncthreads();
+    float top = -INF, total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < S::WAVES; ++w) top = __builtin_fmaxf(top, sums[(w * 32 + col) * PITCH + DP]);
+#pragma unroll
+    for (int w = 0; w < S::WAVES; ++w) {
+      const float mw = sums[(w * 32 + col) * PITCH + DP];
+      total += sums[(w * 32 + col) * PITCH + DP + 1] * (mw == -INF ? 0.0f : exp2_(mw - top));
+    }
+    const float by = m == -INF ? 0.0f : exp2_(m - top);
+#pragma unroll
+    for (int d = 0; d < L::BLOCKS; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 x = {o[d][r] * by, o[d][r + 1] * by, o[d][r + 2] * by, o[d][r + 3] * by};
+        *(GR_LDS f32x4*)(sums + (wave * 32 + col) * PITCH + d * 32 + 2 * r + 4 * hi) = x;
+      }
+    __syncthreads();
+    // wave w finishes the blocks d = w, w + WAVES, ..: its lanes keep the rows they had
+#pragma unroll
+    for (int d = 0; d < L::BLOCKS; ++d) {
+      if (d % S::WAVES != wave) continue;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        f32x4 x = (f32x4)0.0f;
+#pragma unroll
+        for (int w = 0; w < S::WAVES; ++w) x += *(const GR_LDS f32x4*)(sums + (w * 32 + col) * PITCH + d * 32 + 2 * r + 4 * hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][r + e] = x[e];
+      }
+    }
+    m = top;
+    l = total;
+  }
+
+  if (!valid) return;
+  const bool mine = !DIVIDED || wave == 0;
+  if (a.splits > 1) {
+    const int64_t at_row = ((int64_t)split * pairs + place.pair) * R + row;
+    float* const po = a.part_o + at_row * DP;
+#pragma unroll
+    for (int d = 0; d < L::BLOCKS; ++d) {
+      if (DIVIDED && d % S::WAVES != wave) continue;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 x = {o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+        *(f32x4*)(po + d * 32 + 2 * r + 4 * hi) = x;
+      }
+    }
+    if (mine && hi == 0) { a.part_ml[2 * at_row] = m; a.part_ml[2 * at_row + 1] = l; }
+    return;
+  }
+  // a row that sees nothing: out = 0, lse = -inf
+  const float inv = m == -INF ? 0.0f : 1.0f / l;
+  T* const out = at<T>(a.out, b, i, h);
+  T* const rest = a.rest.p ? at<T>(a.rest, b, i, h) : nullptr;
+#pragma unroll
+  for (int d = 0; d < L::BLOCKS; ++d) {
+    if (DIVIDED && d % S::WAVES != wave) continue;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      float x[4], y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { x[e] = o[d][r + e] * inv; y[e] = x[e] - (float)(T)x[e]; }
+      store4(out, d * 32 + 2 * r + 4 * hi, a.D, x, a.out.aligned);
+      if (rest) store4(rest, d * 32 + 2 * r + 4 * hi, a.D, y, a.rest.aligned);
+    }
+  }
+  if (a.lse && mine && hi == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
+}
+
+template <class T, int DP, int MODE, bool DIVIDED>
+static hipError_t forward_one(const Args& a, unsigned grid, hipStream_t stream) {
+  typedef Shape<T, DP, DIVIDED> S;
+  gr_attention_kernel<T, DP, MODE, DIVIDED><<<dim3(grid), dim3(S::THREADS), S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <class T, int DP, bool DIVIDED>
+static hipError_t forward_mode(const Args& a, int mode, unsigned grid, hipStream_t stream) {
+  switch (mode) {
+    case 0: return forward_one<T, DP, 0, DIVIDED>(a, grid, stream);
+    case 1: return forward_one<T, DP, 1, DIVIDED>(a, grid, stream);
+    case 2: return forward_one<T, DP, 2, DIVIDED>(a, grid, stream);
+    default: return forward_one<T, DP, 3, DIVIDED>(a, grid, stream);
+  }
+}
+template <class T>
+static hipError_t forward_all(const Args& a, int dp, int mode, bool divided, unsigned grid, hipStream_t stream) {
+  switch (dp) {
+    case 64: return divided ? forward_mode<T, 64, true>(a, mode, grid, stream) : forward_mode<T, 64, false>(a, mode, grid, stream);
+    case 96: return divided ? forward_mode<T, 96, true>(a, mode, grid, stream) : forward_mode<T, 96, false>(a, mode, grid, stream);
+    case 128: return divided ? forward_mode<T, 128, true>(a, mode, grid, stream) : forward_mode<T, 128, false>(a, mode, grid, stream);
+    default: return divided ? forward_mode<T, 256, true>(a, mode, grid, stream) : forward_mode<T, 256, false>(a, mode, grid, stream);
+  }
+}
+
+}  // namespace attn
+}  // namespace gr

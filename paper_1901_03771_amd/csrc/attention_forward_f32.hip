@@ -1,0 +1,2 @@
+#include "attention_forward.h"
+hipError_t gr::attn::forward_f32(const Args& a, int dp, int mode, bool divided, unsigned grid, hipStream_t stream) { return forward_all<float>(a, dp, mode, divided, grid, stream); }

@@ -1,0 +1,2 @@
+#include "attention_backward.h"
+hipError_t gr::attn::grad_kv_bf16(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream) { return grad_kv_all<__bf16>(a, dp, mode, grid, stream); }

@@ -148,6 +148,12 @@ struct gr_ctx {
   size_t scan_cells_bytes = 0;
   uint32_t scan_epoch = 0;
 
+  // temporary memory of the attention calls, and blocks that a captured call has used and that were outgrown since
+  void* attention_space = nullptr;
+  size_t attention_space_bytes = 0;
+  bool attention_captured = false;
+  std::vector<std::pair<void*, size_t>> attention_kept;
+
   // gr_materialize_into_static: this device's copy of the library's static device array, and the
   // part of it the running request has taken (static_mode is set for the duration of such a call)
   unsigned char* static_base = nullptr;
@@ -201,6 +207,15 @@ gr_status collect_all_jobs(gr_ctx* c, bool load);
 gr_status compile_group(gr_ctx* c, GroupPlan& g, gr_ctx::Kernel** out);
 gr_status launch_group(gr_ctx* c, const GroupPlan& g, gr_ctx::Kernel* k, void* out_ptr, void* pair_out_ptr);
 gr_status execute_plan(gr_ctx* c, Plan* plan, Node* root, void* user_out, bool check_alias);
+
+// Where the elements of (a view of) a materialised array lie: its element (0,..,0), strides, extent.
+struct StoredView {
+  char* data = nullptr;
+  int64_t strides[MAXD] = {0};
+  uintptr_t lo = 0, hi = 0;
+};
+bool stored_view(const Node* n, StoredView* v);
+gr_status prepare_write(gr_ctx* c, gr_array a);  // (a view of) a materialised array is about to be written by a kernel of its own
 
 // static_scratch.hip
 gr_status static_scratch_attach(gr_ctx* c);

@@ -12,6 +12,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "../../include/grumpy_hip_attention.h"
 #include "../../include/grumpy_hip_tuning.h"
 
 namespace gr {
@@ -166,7 +167,7 @@ struct NodeIdLess {
 };
 using NodeSet = std::set<const Node*, NodeIdLess>;
 
-inline size_t itemsize(gr_dtype dt) { return dt == GR_I64 ? 8 : 4; }
+inline size_t itemsize(gr_dtype dt) { return dt == GR_I64 ? 8 : dt == GR_BF16 ? 2 : 4; }
 
 // ---- plan --------------------------------------------------------------------
 

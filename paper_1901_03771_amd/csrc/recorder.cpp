@@ -200,6 +200,11 @@ static gr_array finish(gr_ctx* c, Node* n) {
   return n->id;
 }
 
+// bf16 arrays only go through the calls of attention.cpp.
+static gr_status refuse_bf16(gr_ctx* ctx, const char* call) {
+  return fail(ctx, GR_ERR_DTYPE, std::string(call) + ": bf16 arrays are operands of the attention and rotary calls only");
+}
+
 static bool is_unary(int op) { return op >= GR_NEG && op <= GR_ERF; }
 static bool is_binary(int op) { return op >= GR_ADD && op <= GR_MINIMUM; }
 static bool is_reduce(int op) { return op >= GR_SUM && op <= GR_MIN; }
@@ -280,7 +285,7 @@ gr_status gr_array_from_device(gr_ctx* ctx, void* dptr, gr_dtype dtype, int ndim
                                const int64_t* strides_elems, gr_array* out) {
   if (!ctx || !out) return GR_ERR_ARG;
   if (ndim < 0 || ndim > MAXD || (ndim > 0 && !shape)) return fail(ctx, GR_ERR_ARG, "from_device: bad rank or NULL shape");
-  { const int dt = enum_arg(dtype); if (dt != GR_F32 && dt != GR_I32 && dt != GR_I64) return fail(ctx, GR_ERR_ARG, "from_device: bad dtype"); }
+  { const int dt = enum_arg(dtype); if (dt != GR_F32 && dt != GR_I32 && dt != GR_I64 && dt != GR_BF16) return fail(ctx, GR_ERR_ARG, "from_device: bad dtype"); }
   int64_t n = 1;
   for (int d = 0; d < ndim; ++d)
     if (shape[d] < 0) return fail(ctx, GR_ERR_ARG, "from_device: negative extent");
@@ -332,6 +337,7 @@ gr_status gr_unary(gr_ctx* ctx, gr_op op, gr_array a, gr_array* out) {
   Node* x = lookup(ctx, a);
   if (!x) return fail(ctx, GR_ERR_HANDLE, "unary: bad handle");
   if (x->kind == Kind::SCALAR) return fail(ctx, GR_ERR_UNSUPPORTED, "unary: operand is a bare scalar");
+  if (x->dtype == GR_BF16) return refuse_bf16(ctx, "unary");
   if (x->dtype == GR_I64) return fail(ctx, GR_ERR_UNSUPPORTED, "unary: i64 arithmetic is not supported");
   if (x->dtype == GR_I32 && !(op == GR_NEG || op == GR_ABS || op == GR_SQUARE))
     return fail(ctx, GR_ERR_DTYPE, "unary: float function of an i32 array would promote to f64");
@@ -359,6 +365,7 @@ static gr_status binary(gr_ctx* ctx, gr_op op, Node* x, Node* y, gr_array* out) 
   if (wx && wy) return fail(ctx, GR_ERR_UNSUPPORTED, "binary: two bare scalars");
   gr_dtype dt = wx ? y->dtype : x->dtype;
   if (!wx && !wy && x->dtype != y->dtype) return fail(ctx, GR_ERR_DTYPE, "binary: mixed element types would promote to f64");
+  if (dt == GR_BF16) return refuse_bf16(ctx, "binary");
   if (dt == GR_I64) return fail(ctx, GR_ERR_UNSUPPORTED, "binary: i64 arithmetic is not supported");
   if (dt == GR_I32 && op == GR_DIV) return fail(ctx, GR_ERR_UNSUPPORTED, "binary: integer division is not supported");
   const Node* w = wx ? x : (wy ? y : nullptr);
@@ -494,6 +501,7 @@ gr_status gr_reshape(gr_ctx* ctx, gr_array a, int ndim, const int64_t* shape, gr
   Node* x = lookup(ctx, a);
   if (!x) return fail(ctx, GR_ERR_HANDLE, "reshape: bad handle");
   if (x->kind == Kind::SCALAR) return fail(ctx, GR_ERR_UNSUPPORTED, "reshape: operand is a bare scalar");
+  if (x->dtype == GR_BF16) return refuse_bf16(ctx, "reshape");
   if (ndim < 0 || ndim > MAXD || (ndim > 0 && !shape)) return fail(ctx, GR_ERR_ARG, "reshape: bad rank or NULL shape");
   if (!count_fits(shape, ndim)) return fail(ctx, GR_ERR_SHAPE, "reshape: element counts differ");
   int64_t want[MAXD], known = 1;
@@ -526,6 +534,7 @@ gr_status gr_reduce(gr_ctx* ctx, gr_op op, gr_array a, const int* axes, int naxe
   Node* x = lookup(ctx, a);
   if (!x) return fail(ctx, GR_ERR_HANDLE, "reduce: bad handle");
   if (x->kind == Kind::SCALAR) return fail(ctx, GR_ERR_UNSUPPORTED, "reduce: operand is a bare scalar");
+  if (x->dtype == GR_BF16) return refuse_bf16(ctx, "reduce");
   if (x->dtype == GR_I64) return fail(ctx, GR_ERR_UNSUPPORTED, "reduce: i64 operands are not supported");
   if (naxes < 0 || naxes > x->ndim || (naxes > 0 && !axes)) return fail(ctx, GR_ERR_AXIS, "reduce: bad axis list");
   bool red[MAXD];
@@ -561,6 +570,7 @@ gr_status gr_scan(gr_ctx* ctx, gr_op op, gr_array a, int axis, gr_array* out) {
   Node* x = lookup(ctx, a);
   if (!x) return fail(ctx, GR_ERR_HANDLE, "scan: bad handle");
   if (x->kind == Kind::SCALAR) return fail(ctx, GR_ERR_UNSUPPORTED, "scan: operand is a bare scalar");
+  if (x->dtype == GR_BF16) return refuse_bf16(ctx, "scan");
   if (x->dtype == GR_I64) return fail(ctx, GR_ERR_UNSUPPORTED, "scan: i64 operands are not supported");
   if (x->ndim < 1) return fail(ctx, GR_ERR_AXIS, "scan: rank-0 operand has no axis");
   int ax = axis < 0 ? axis + x->ndim : axis;

@@ -1,0 +1,123 @@
+// Rotary positions: pair i of a head at position p turns by the angle p f_i,
+//   lo' = factor (lo cos - hi sin),  hi' = factor (hi cos + lo sin);
+// the gradient is the same turn backwards.  A read and a write of the tensor bound it.
+//
+// A workgroup takes a few tokens and a run of heads.  It forms their sines and cosines once, in LDS, for all its heads, then moves whole
+// 16-byte vectors.  The angle is formed in turns, in 64 bits, and its whole turns are taken off there: at position 10^6 an angle
+// held in 32 bits is off by 0.06.  What is left, an eighth of a turn at most around a quarter, is small enough for Taylor's
+// polynomials in 32 bits (sine to x^9: 2e-9 off at pi / 4; cosine to x^10: 1e-10).
+#include "attention_kernels.h"
+
+namespace gr {
+namespace attn {
+
+static __device__ __forceinline__ void turn(double turns, float& c, float& s) {
+  const double r = turns - __builtin_rint(turns);           // [-1/2, 1/2]
+  const double q = __builtin_rint(4.0 * r);
+  const float x = (float)((r - 0.25 * q) * 6.283185307179586);
+  const float z = x * x;
+  float u = 1.0f / 362880.0f;
+  u = __builtin_fmaf(u, z, -1.0f / 5040.0f);
+  u = __builtin_fmaf(u, z, 1.0f / 120.0f);
+  u = __builtin_fmaf(u, z, -1.0f / 6.0f);
+  const float sn = __builtin_fmaf(x * z, u, x);
+  float w = -1.0f / 3628800.0f;
+  w = __builtin_fmaf(w, z, 1.0f / 40320.0f);
+  w = __builtin_fmaf(w, z, -1.0f / 720.0f);
+  w = __builtin_fmaf(w, z, 1.0f / 24.0f);
+  w = __builtin_fmaf(w, z, -0.5f);
+  const float cs = __builtin_fmaf(z, w, 1.0f);
+  const int k = (int)q & 3;
+  c = k & 1 ? sn : cs;
+  s = k & 1 ? cs : sn;
+  if (k == 1 || k == 2) c = -c;
+  if (k >= 2) s = -s;
+}
+
+// VECTORS: rows of whole aligned vectors, halves (or neighbouring pairs) and the part behind them of whole vectors too
+template <class T, bool VECTORS>
+__global__ __launch_bounds__(256) void gr_rotary_kernel(const Rotary r) {
+  extern __shared__ float table[];   // [token][cos of the pairs, sin of the pairs]
+  const int tid = threadIdx.x;
+  const int64_t token0 = (int64_t)blockIdx.x * r.tokens, all = (int64_t)r.B * r.N;
+  const int tokens = (int)(all - token0 < r.tokens ? all - token0 : r.tokens);
+  const int head0 = blockIdx.y * r.heads, heads = r.H - head0 < r.heads ? r.H - head0 : r.heads;
+  const int P = r.pairs;
+  for (int k = tid; k < tokens * P; k += 256) {
+    const int n = k / P, i = k - n * P;
+    const int64_t t = token0 + n, b = t / r.N, at_n = t - b * r.N;
+    const int64_t pos = r.positions ? (int64_t)r.positions[b * r.positions_sb + at_n * r.positions_sn] : r.position + at_n;
+    float c, s;
+    turn((double)pos * r.turns[i], c, s);
+    table[2 * n * P + i] = c * r.factor;
+    table[2 * n * P + P + i] = r.inverse ? -s * r.factor : s * r.factor;
+  }
+  __syncthreads();
+  constexpr int V = VECTORS ? 16 / (int)sizeof(T) : 1;
+  typedef T vec __attribute__((ext_vector_type(VECTORS ? 16 / (int)sizeof(T) : 2)));
+  // units of a head: pairs (V at a time, V / 2 where pairs are neighbours), then what is not turned
+  const int turned = r.interleaved ? (VECTORS ? 2 * P / V : P) : P / V, units = turned + (r.D - 2 * P) / V;
+  const bool in_place = r.x.p == r.y.p;
+  for (int k = tid; k < tokens * heads * units; k += 256) {
+    const int u = k % units, nh = k / units, n = nh / heads, h = head0 + nh - n * heads;
+    const int64_t t = token0 + n, b = t / r.N, at_n = t - b * r.N;
+    const T* x = at<T>(r.x, b, at_n, h);
+    T* y = at<T>(r.y, b, at_n, h);
+    const float* cs = table + 2 * n * P;
+    const float* sn = cs + P;
+    if constexpr (VECTORS) {
+      if (u >= turned) {
+        const int d = 2 * P + (u - turned) * V;
+        if (!in_place) *(vec*)(y + d) = *(const vec*)(x + d);
+      } else if (r.interleaved) {
+        const vec v = *(const vec*)(x + u * V);
+        vec w;
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float c = cs[u * (V / 2) + e / 2], s = sn[u * (V / 2) + e / 2], lo = (float)v[e], hi = (float)v[e + 1];
+          w[e] = (T)__builtin_fmaf(lo, c, -hi * s);
+          w[e + 1] = (T)__builtin_fmaf(hi, c, lo * s);
+        }
+        *(vec*)(y + u * V) = w;
+      } else {
+        const vec v = *(const vec*)(x + u * V), w = *(const vec*)(x + P + u * V);
+        vec p, q;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float c = cs[u * V + e], s = sn[u * V + e], lo = (float)v[e], hi = (float)w[e];
+          p[e] = (T)__builtin_fmaf(lo, c, -hi * s);
+          q[e] = (T)__builtin_fmaf(hi, c, lo * s);
+        }
+        *(vec*)(y + u * V) = p;
+        *(vec*)(y + P + u * V) = q;
+      }
+    } else {
+      if (u >= turned) {
+        const int d = 2 * P + u - turned;
+        if (!in_place) y[d] = x[d];
+      } else {
+        const int a = r.interleaved ? 2 * u : u, c = r.interleaved ? 2 * u + 1 : P + u;
+        const float lo = (float)x[a], hi = (float)x[c];
+        y[a] = (T)__builtin_fmaf(lo, cs[u], -hi * sn[u]);
+        y[c] = (T)__builtin_fmaf(hi, cs[u], lo * sn[u]);
+      }
+    }
+  }
+}
+
+template <class T>
+static hipError_t rotary_of(Rotary r, hipStream_t stream) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool vectors = r.x.aligned && r.y.aligned && (r.interleaved ? 2 * r.pairs % V == 0 : r.pairs % V == 0);
+  const int64_t tokens = (int64_t)r.B * r.N;
+  const dim3 grid((unsigned)((tokens + r.tokens - 1) / r.tokens), (unsigned)((r.H + r.heads - 1) / r.heads));
+  const size_t lds = (size_t)r.tokens * r.pairs * 8;
+  if (vectors) gr_rotary_kernel<T, true><<<grid, dim3(256), lds, stream>>>(r);
+  else gr_rotary_kernel<T, false><<<grid, dim3(256), lds, stream>>>(r);
+  return hipGetLastError();
+}
+
+hipError_t rotary(const Rotary& r, int type, hipStream_t stream) { return type == TYPE_BF16 ? rotary_of<__bf16>(r, stream) : rotary_of<float>(r, stream); }
+
+}  // namespace attn
+}  // namespace gr

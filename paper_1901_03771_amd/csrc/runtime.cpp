@@ -1197,6 +1197,8 @@ gr_status gr_ctx_destroy(gr_ctx* ctx) {
   while (!ctx->programs.empty()) program_free(ctx, ctx->programs.back());
   if (ctx->workspace) ctx_free(ctx, ctx->workspace, ctx->workspace_bytes);
   if (ctx->scan_cells) ctx_free(ctx, ctx->scan_cells, ctx->scan_cells_bytes);
+  if (ctx->attention_space) ctx_free(ctx, ctx->attention_space, ctx->attention_space_bytes);
+  for (auto& k : ctx->attention_kept) ctx_free(ctx, k.first, k.second);
   for (auto& kv : ctx->cache) if (kv.second.module) (void)hipModuleUnload(kv.second.module);
   for (auto& p : ctx->prof) { (void)hipEventDestroy(p.e0); (void)hipEventDestroy(p.e1); }
   for (hipEvent_t e : ctx->event_pool) (void)hipEventDestroy(e);
@@ -1406,6 +1408,59 @@ static gr_status assign_in_place(gr_ctx* ctx, Node* v, const Node* base, const O
   return st;
 }
 
+// The storage [lo, hi) is about to be written: arrays recorded earlier that read it are evaluated now, so that they keep the
+// values they had when recorded, and results of earlier direct assignments that still live inside it get their own
+// copy.  `except`: the value that is to be written.
+static gr_status settle_readers(gr_ctx* ctx, uintptr_t lo, uintptr_t hi, const Node* except) {
+  std::vector<gr_array> pending, aliases;
+  ctx->nodes.each([&](Node* n) {
+    if (n == except || n->kind == Kind::SCALAR) return;
+    if (n->materialized) {
+      // (also one that only views refer to: the destination itself may be a view of it)
+      if (n->cow_alias) { uintptr_t a, b; extent_of(n, &a, &b); if (a < hi && lo < b) aliases.push_back(n->id); }
+      return;
+    }
+    if (n->handle_refs <= 0) return;
+    if (n->is_view()) { const Node* vb; int64_t o, st[MAXD]; if (resolve_view_rt(n, &vb, &o, st)) return; }  // aliases see the new contents
+    std::set<const Node*> seen;
+    if (reads_range(n, lo, hi, &seen)) pending.push_back(n->id);
+  });
+  for (gr_array id : pending) {
+    gr_status st = gr_materialize(ctx, id);
+    if (st != GR_OK) return st;
+  }
+  for (gr_array id : aliases) {
+    gr_status st = unshare(ctx, id);
+    if (st != GR_OK) return st;
+  }
+  return GR_OK;
+}
+
+bool stored_view(const Node* n, StoredView* v) {
+  const Node* base = nullptr;
+  int64_t offset;
+  if (!resolve_view_rt(n, &base, &offset, v->strides)) return false;
+  v->data = (char*)base->data + offset * (int64_t)itemsize(n->dtype);
+  view_extent(base, n->ndim, n->shape, offset, v->strides, &v->lo, &v->hi);
+  return true;
+}
+
+gr_status prepare_write(gr_ctx* ctx, gr_array a) {
+  StoredView v;
+  Node* n = lookup(ctx, a);
+  if (!n || !stored_view(n, &v)) return fail(ctx, GR_ERR_UNSUPPORTED, "a result is not (a view of) a materialised array");
+  if (v.lo == v.hi) return GR_OK;
+  gr_status st = settle_readers(ctx, v.lo, v.hi, nullptr);
+  if (st != GR_OK) return st;
+  // (the array may just have moved to a buffer of its own)
+  const Node* base = nullptr;
+  int64_t offset, strides[MAXD];
+  n = lookup(ctx, a);
+  if (!n || !resolve_view_rt(n, &base, &offset, strides)) return fail(ctx, GR_ERR_HANDLE, "a result's handle vanished");
+  drop_shadow(ctx, const_cast<Node*>(base));
+  return GR_OK;
+}
+
 }  // namespace gr
 
 extern "C" gr_status gr_array_lend_buffer(gr_ctx* ctx, gr_array a, void* dptr2, size_t bytes) {
@@ -1435,6 +1490,7 @@ extern "C" gr_status gr_assign(gr_ctx* ctx, gr_array dst, gr_array value) {
   OutSpec spec;
   if (!resolve_view_rt(d, &base, &spec.base, spec.strides)) return fail(ctx, GR_ERR_UNSUPPORTED, "assign: destination is not (a view of) a materialised array");
   if (v->dtype != d->dtype) return fail(ctx, GR_ERR_DTYPE, "assign: element types differ");
+  if (d->dtype == GR_BF16) return fail(ctx, GR_ERR_DTYPE, "assign: bf16 arrays are operands of the attention and rotary calls only");
   if (v->ndim != d->ndim) return fail(ctx, GR_ERR_SHAPE, "assign: shapes differ");
   for (int k = 0; k < d->ndim; ++k) {
     if (v->shape[k] != d->shape[k]) return fail(ctx, GR_ERR_SHAPE, "assign: shapes differ");
@@ -1445,28 +1501,9 @@ extern "C" gr_status gr_assign(gr_ctx* ctx, gr_array dst, gr_array value) {
   uintptr_t lo, hi;
   view_extent(base, d->ndim, d->shape, spec.base, spec.strides, &lo, &hi);
 
-  // 1. Arrays recorded earlier that read this storage keep the values they had when recorded:
-  //    evaluate them now.  Results of earlier direct assignments that still live inside this
-  //    storage get their own copy.
-  std::vector<gr_array> pending, aliases;
-  ctx->nodes.each([&](Node* n) {
-    if (n == v || n->kind == Kind::SCALAR) return;
-    if (n->materialized) {
-      // (also one that only views refer to: the destination itself may be a view of it)
-      if (n->cow_alias) { uintptr_t a, b; extent_of(n, &a, &b); if (a < hi && lo < b) aliases.push_back(n->id); }
-      return;
-    }
-    if (n->handle_refs <= 0) return;
-    if (n->is_view()) { const Node* vb; int64_t o, st[MAXD]; if (resolve_view_rt(n, &vb, &o, st)) return; }  // aliases see the new contents
-    std::set<const Node*> seen;
-    if (reads_range(n, lo, hi, &seen)) pending.push_back(n->id);
-  });
-  for (gr_array id : pending) {
-    gr_status st = gr_materialize(ctx, id);
-    if (st != GR_OK) return st;
-  }
-  for (gr_array id : aliases) {
-    gr_status st = unshare(ctx, id);
+  // 1. Arrays recorded earlier that read this storage keep the values they had when recorded.
+  {
+    gr_status st = settle_readers(ctx, lo, hi, v);
     if (st != GR_OK) return st;
   }
   v = lookup(ctx, value);

@@ -22,7 +22,7 @@ from typing import Optional, Sequence
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("GRUMPY_HIP_LIB", os.path.join(_HERE, "libgrumpy_hip.so"))
 
-GR_F32, GR_I32, GR_I64 = 0, 1, 2
+GR_F32, GR_I32, GR_I64, GR_BF16 = 0, 1, 2, 3
 GR_NEG, GR_ABS, GR_EXP, GR_LOG, GR_SQRT, GR_SQUARE, GR_TANH, GR_ERF = range(8)
 GR_ADD, GR_SUB, GR_MUL, GR_DIV, GR_MAXIMUM, GR_MINIMUM, GR_POW_INT = range(16, 23)
 _UNARY = {"neg": 0, "abs": 1, "exp": 2, "log": 3, "sqrt": 4, "square": 5, "tanh": 6, "erf": 7}
@@ -32,13 +32,14 @@ STATUS = {0: "GR_OK", 1: "GR_ERR_HANDLE", 2: "GR_ERR_SHAPE", 3: "GR_ERR_DTYPE", 
           5: "GR_ERR_UNSUPPORTED", 6: "GR_ERR_ARG", 7: "GR_ERR_COMPILE", 8: "GR_ERR_HIP", 9: "GR_ERR_OOM",
           10: "GR_ERR_ALIAS", 11: "GR_ERR_NODEVICE"}
 
-# every symbol include/grumpy_hip.h declares
+# every symbol that the headers under include/ declare
 SYMBOLS = [
     "gr_ctx_create", "gr_ctx_destroy", "gr_ctx_set_stream", "gr_ctx_set_allocator", "gr_ctx_set_option", "gr_sync",
     "gr_last_error", "gr_array_from_device", "gr_array_lend_buffer", "gr_scalar", "gr_unary", "gr_binary", "gr_binary_scalar", "gr_slice", "gr_transpose", "gr_reshape",
     "gr_reduce", "gr_scan", "gr_dot", "gr_materialize", "gr_materialize_into", "gr_materialize_into_static", "gr_static_scratch_bytes", "gr_program_create", "gr_program_run", "gr_program_destroy", "gr_assign", "gr_ndim", "gr_shape", "gr_dtype_of",
     "gr_is_materialized", "gr_data_ptr", "gr_retain", "gr_release", "gr_plan_describe", "gr_plan_source",
     "gr_plan_compile", "gr_compile_wait", "gr_stats", "gr_profile_reset", "gr_profile_read", "gr_stream_copy", "gr_stream_read",
+    "gr_attention", "gr_attention_grad", "gr_attention_step", "gr_rotary",
 ]
 
 
@@ -57,6 +58,12 @@ class Stats(ctypes.Structure):
                 ("bytes_allocated", ctypes.c_uint64), ("disk_hits", ctypes.c_uint64),
                 ("nodes_merged", ctypes.c_uint64), ("interp_launches", ctypes.c_uint64),
                 ("assign_swaps", ctypes.c_uint64), ("plan_hits", ctypes.c_uint64), ("pool_bytes", ctypes.c_uint64)]
+
+
+class _Scores(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_double), ("cap", ctypes.c_double), ("slopes", ctypes.c_uint64), ("causal", ctypes.c_int),
+                ("position", ctypes.c_int64), ("prefix", ctypes.c_uint64), ("q_documents", ctypes.c_uint64),
+                ("k_documents", ctypes.c_uint64), ("lengths", ctypes.c_uint64)]
 
 
 _lib = None
@@ -100,6 +107,9 @@ def lib():
         "gr_stats": [P, PP(Stats)], "gr_profile_reset": [P],
         "gr_profile_read": [P, ctypes.c_char_p, PP(U64), PP(ctypes.c_double)],
         "gr_stream_copy": [P, P, P, SZ], "gr_stream_read": [P, P, SZ, P],
+        "gr_attention": [P, PP(_Scores)] + [U64] * 6, "gr_attention_grad": [P, PP(_Scores)] + [U64] * 10,
+        "gr_attention_step": [P, PP(_Scores)] + [U64] * 4,
+        "gr_rotary": [P, U64, U64, I64, PP(ctypes.c_double), I, I, I, ctypes.c_double, U64],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -279,7 +289,7 @@ class Context:
             torch = _torch()
             if not isinstance(t, torch.Tensor):
                 raise TypeError("expected a torch.Tensor on the GPU")
-            _TORCH_DTYPES.update({torch.float32: GR_F32, torch.int32: GR_I32, torch.int64: GR_I64})
+            _TORCH_DTYPES.update({torch.float32: GR_F32, torch.int32: GR_I32, torch.int64: GR_I64, torch.bfloat16: GR_BF16})
             if t.dtype not in _TORCH_DTYPES:
                 raise GrError(3, f"unsupported dtype {t.dtype}")
             dt = _TORCH_DTYPES[t.dtype]
@@ -298,6 +308,13 @@ class Context:
         is_int = isinstance(v, int) or type(v).__name__.startswith(("int", "uint"))
         self.check(lib().gr_scalar(self._p, float(v), int(is_int), ctypes.byref(h)))
         return Array(self, h.value)
+
+    def scores(self, scale: Optional[float] = None, cap: float = 0.0, slopes=None, causal: bool = False, position: int = 0,
+               prefix=None, documents=None, lengths=None) -> "Scores":
+        """How attention forms its scores and what a query sees (gr_scores), for ``attention``, ``attention_grad`` and
+        ``attention_step``.  scale: None = 1 / sqrt(D).  documents: the i32 array (B, N) of both sides, or a pair of
+        arrays, of the queries (B, N) and of the keys (B, M)."""
+        return Scores(self, scale, cap, slopes, causal, position, prefix, documents, lengths)
 
     # -- streaming ceiling kernels ----------------------------------------------
     def stream_copy(self, dst, src):
@@ -473,7 +490,9 @@ class _ArrayMethods:
         Section 2) and returns its value as a torch tensor on the context's device: a copy by default,
         with copy=False a tensor that shares the node's storage (and keeps this handle alive)."""
         torch = _torch()
-        dt = {GR_F32: (torch.float32, "<f4", 4), GR_I32: (torch.int32, "<i4", 4), GR_I64: (torch.int64, "<i8", 8)}[self.dtype_code]
+        # (the array interface has no bfloat16: those are handed over as 16-bit integers and seen as what they are)
+        dt = {GR_F32: (torch.float32, "<f4", 4), GR_I32: (torch.int32, "<i4", 4), GR_I64: (torch.int64, "<i8", 8),
+              GR_BF16: (torch.bfloat16, "<i2", 2)}[self.dtype_code]
         shape = self.shape
         if 0 in shape:
             return torch.empty(shape, dtype=dt[0], device=f"cuda:{self.ctx.device}")
@@ -481,6 +500,8 @@ class _ArrayMethods:
         ptr, strides = self.data_ptr()
         view = torch.as_tensor(_DeviceExport(self, ptr, shape, tuple(s * dt[2] for s in strides), dt[1]),
                                device=f"cuda:{self.ctx.device}")
+        if view.dtype != dt[0]:
+            view = view.view(dt[0])
         return view.clone() if copy else view
 
     def numpy(self):
@@ -774,3 +795,125 @@ def clip(a, lo, hi):
     """NumPy's clip with two bounds."""
     return minimum(maximum(a, lo), hi)
 def min(a, axis=None, keepdims=False): return _reduce(34, a, axis, keepdims)  # noqa: A001
+
+
+# ---- attention and rotary positions (include/grumpy_hip_attention.h) ----------------------------------------------------
+
+class Scores:
+    """gr_scores: the description that the calls below take.  Keeps the arrays it names."""
+
+    __slots__ = ("ctx", "_c", "_scale", "_keep")
+
+    def __init__(self, ctx: Context, scale, cap, slopes, causal, position, prefix, documents, lengths):
+        qd, kd = documents if isinstance(documents, (tuple, list)) else (documents, documents)
+        self.ctx = ctx
+        self._keep = (slopes, prefix, qd, kd, lengths)
+        h = [0 if a is None else _operand(ctx, a).h for a in self._keep]
+        self._scale = scale
+        self._c = _Scores(0.0 if scale is None else scale, cap, h[0], builtins.bool(causal), position, h[1], h[2], h[3], h[4])
+
+    def _for(self, d: int):
+        if self._scale is None:
+            self._c.scale = builtins.max(d, 1) ** -0.5
+        return ctypes.byref(self._c)
+
+
+def _tensor(ctx: Context, a: "Array") -> int:
+    if not isinstance(a, Array):
+        raise TypeError("expected an Array of the context")
+    return _operand(ctx, a).h
+
+
+def _result_array(ctx: Context, given, shape, dtype: int) -> "Array":
+    """The array that a call writes: the caller's, or a new one over memory from torch."""
+    if given is not None:
+        return given
+    torch = _torch()
+    return ctx.array(torch.empty(shape, device=f"cuda:{ctx.device}",
+                                 dtype={GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]))
+
+
+def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=None, rest=None):
+    """softmax(scores) v (gr_attention) of q (B, N, H, D), k and v (B, M, HK, D), f32 or bf16; returns (out, lse).  out and
+    lse are new arrays where none are given; lse=False: not wanted, returned as None.  rest (bf16, optional): gets what out lost in
+    rounding, for attention_grad."""
+    ctx = q.ctx
+    hq, hk, hv = _tensor(ctx, q), _tensor(ctx, k), _tensor(ctx, v)
+    shape = q.shape if out is None or lse is None else None
+    d = q.shape[-1] if scores._scale is None else 0
+    out = _result_array(ctx, out, shape, q.dtype_code if out is None else 0)
+    if lse is None:
+        if len(shape) != 4:
+            raise GrError(2, "attention: q is (B, N, H, D)")
+        lse = _result_array(ctx, None, (shape[0], shape[2], shape[1]), GR_F32)
+    elif lse is False:
+        lse = None
+    st = lib().gr_attention(ctx._p, scores._for(d), hq, hk, hv, _tensor(ctx, out), 0 if lse is None else _tensor(ctx, lse),
+                            0 if rest is None else _tensor(ctx, rest))
+    if st:
+        ctx.check(st)
+    return out, lse
+
+
+def attention_grad(dout: "Array", q: "Array", k: "Array", v: "Array", scores: Scores, out: "Array", lse: "Array", rest=None,
+                   dq=None, dk=None, dv=None):
+    """The gradients of q, k and v (gr_attention_grad) for the gradient of out; returns (dq, dk, dv)."""
+    ctx = q.ctx
+    h = [_tensor(ctx, a) for a in (q, k, v, out)]
+    h.append(0 if rest is None else _tensor(ctx, rest))
+    h += [_tensor(ctx, lse), _tensor(ctx, dout)]
+    dq = _result_array(ctx, dq, q.shape if dq is None else None, q.dtype_code if dq is None else 0)
+    dk = _result_array(ctx, dk, k.shape if dk is None else None, k.dtype_code if dk is None else 0)
+    dv = _result_array(ctx, dv, v.shape if dv is None else None, v.dtype_code if dv is None else 0)
+    st = lib().gr_attention_grad(ctx._p, scores._for(q.shape[-1] if scores._scale is None else 0), *h,
+                                 _tensor(ctx, dq), _tensor(ctx, dk), _tensor(ctx, dv))
+    if st:
+        ctx.check(st)
+    return dq, dk, dv
+
+
+def attention_step(q: "Array", k: "Array", v: "Array", scores: Scores, out=None):
+    """One new token per sequence (gr_attention_step): q (B, H, D) against the first lengths[b] rows of k and v (B, M, HK, D)."""
+    ctx = q.ctx
+    h = [_tensor(ctx, a) for a in (q, k, v)]
+    out = _result_array(ctx, out, q.shape if out is None else None, q.dtype_code if out is None else 0)
+    st = lib().gr_attention_step(ctx._p, scores._for(q.shape[-1] if scores._scale is None else 0), *h, _tensor(ctx, out))
+    if st:
+        ctx.check(st)
+    return out
+
+
+def rotary_frequencies(values: int, base: float = 10000.0, stretch: float = 1.0, context: int = 0, slow: float = 1.0,
+                       fast: float = 32.0):
+    """Radians per position of the pairs of `values` values of a head: base ** (-2 i / values), a ctypes array of doubles as
+    ``rotary`` takes it.  stretch > 1 makes positions fit a context so many times longer: every pair slower by it
+    (context = 0), or by wavelength: pairs that turn ``fast`` times or more within ``context`` positions keep their pace,
+    those that turn ``slow`` times or less go slower by the whole of it, in between a linear blend."""
+    if values < 0 or values % 2:
+        raise ValueError("an even number of values")
+    got = (ctypes.c_double * (values // 2))()
+    for i in range(values // 2):
+        f = base ** (-2.0 * i / values)
+        keep = 0.0
+        if context:
+            turns = context * f / 6.283185307179586
+            keep = builtins.min(1.0, builtins.max(0.0, (turns - slow) / (fast - slow)))
+        got[i] = f * keep + f / stretch * (1.0 - keep)
+    return got
+
+
+def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inverse: bool = False, factor: float = 1.0, out=None):
+    """x (B, N, H, D) with the pairs of every head turned by position * frequencies (gr_rotary).  positions: an i32 array (B, N), or
+    the position of the first token.  out: where to (x itself for in place); a new array if none is given."""
+    ctx = x.ctx
+    hx = _tensor(ctx, x)
+    n = len(frequencies)
+    if not isinstance(frequencies, ctypes.Array):
+        frequencies = (ctypes.c_double * builtins.max(n, 1))(*frequencies)
+    out = _result_array(ctx, out, x.shape if out is None else None, x.dtype_code if out is None else 0)
+    arr = isinstance(positions, Array)
+    st = lib().gr_rotary(ctx._p, hx, _tensor(ctx, positions) if arr else 0, 0 if arr else int(positions), frequencies, n,
+                         builtins.bool(interleaved), builtins.bool(inverse), factor, _tensor(ctx, out))
+    if st:
+        ctx.check(st)
+    return out

@@ -1,0 +1,556 @@
+"""Attention, its gradient, single-token steps and rotary positions (include/grumpy_hip_attention.h) against plain binary64 forms
+(attention_reference.py), and what the calls refuse."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import attention_reference as plain
+from paper_1901_03771_amd import lazy as gr
+
+F32, BF16 = torch.float32, torch.bfloat16
+NAMES = {F32: "f32", BF16: "bf16"}
+
+
+# ---------------------------------------------------------------- without a GPU --
+@pytest.fixture()
+def dry():
+    c = gr.Context(device=-1)
+    c.set_option("dry_run", 2)
+    yield c
+    c.close()
+
+
+def refused(code, call, /, *a, **kw):
+    with pytest.raises(gr.GrError) as e:
+        call(*a, **kw)
+    assert e.value.code == code, e.value
+
+
+class Specs:
+    """Leaves at addresses of their own that are never read."""
+
+    def __init__(self, ctx):
+        self.ctx, self.at = ctx, 1 << 20
+
+    def __call__(self, shape, dtype=gr.GR_F32, strides=None, off=0):
+        n = 1
+        for s in shape:
+            n *= max(s, 1)
+        a = self.ctx.from_device(self.at + off, dtype, tuple(shape), strides)
+        self.at += (64 * n + 8191) // 4096 * 4096
+        return a
+
+
+@pytest.mark.parametrize("dtype", [gr.GR_F32, gr.GR_BF16])
+def test_calls_run_dry_and_count_their_launches(dry, dtype):
+    s = Specs(dry)
+    q, k, v, o, do, dq = (s((2, 40, 6, 64), dtype) for _ in range(6))
+    k2, v2, dk, dv = (s((2, 50, 2, 64), dtype) for _ in range(4))
+    lse = s((2, 6, 40))
+    sc = dry.scores(cap=30.0, slopes=s((6,)), causal=True, position=10, prefix=s((2,), gr.GR_I32), lengths=s((2,), gr.GR_I32),
+                    documents=(s((2, 40), gr.GR_I32), s((2, 50), gr.GR_I32)))
+    before = dry.stats()["kernel_launches"]
+    gr.attention(q, k2, v2, sc, out=o, lse=lse)
+    gr.attention_grad(do, q, k2, v2, sc, o, lse, dq=dq, dk=dk, dv=dv)
+    assert dry.stats()["kernel_launches"] >= before + 5
+    gr.attention_step(s((2, 6, 64), dtype), k2, v2, dry.scores(lengths=s((2,), gr.GR_I32)), out=s((2, 6, 64), dtype))
+    gr.rotary(q, gr.rotary_frequencies(64), 5, out=q)
+    gr.rotary(q, gr.rotary_frequencies(32), s((2, 40), gr.GR_I32), interleaved=True, inverse=True, out=o)
+
+
+def test_refusals(dry):
+    s = Specs(dry)
+    q, k, v, o = s((2, 8, 4, 64)), s((2, 9, 2, 64)), s((2, 9, 2, 64)), s((2, 8, 4, 64))
+    lse, i2 = s((2, 4, 8)), s((2,), gr.GR_I32)
+    ok = dry.scores()
+    call = lambda sc=ok, q=q, k=k, v=v, o=o, lse=lse, rest=None: gr.attention(q, k, v, sc, out=o, lse=lse, rest=rest)  # noqa: E731
+    call()
+    refused("GR_ERR_SHAPE", call, q=s((2, 8, 3, 64)))                       # 3 heads on 2
+    refused("GR_ERR_SHAPE", call, q=s((8, 4, 64)))
+    refused("GR_ERR_SHAPE", call, v=s((2, 10, 2, 64)))
+    refused("GR_ERR_SHAPE", call, k=s((2, 9, 2, 32)))
+    refused("GR_ERR_SHAPE", call, o=s((2, 8, 4, 32)))
+    refused("GR_ERR_SHAPE", call, lse=s((2, 8, 4)))
+    refused("GR_ERR_UNSUPPORTED", call, q=s((2, 8, 4, 257)), k=s((2, 9, 2, 257)), v=s((2, 9, 2, 257)), o=s((2, 8, 4, 257)))
+    refused("GR_ERR_UNSUPPORTED", call, q=s((2, 8, 4, 0)), k=s((2, 9, 2, 0)), v=s((2, 9, 2, 0)), o=s((2, 8, 4, 0)))
+    refused("GR_ERR_DTYPE", call, q=s((2, 8, 4, 64), gr.GR_I32))
+    refused("GR_ERR_DTYPE", call, k=s((2, 9, 2, 64), gr.GR_BF16))
+    refused("GR_ERR_DTYPE", call, rest=s((2, 8, 4, 64)))                    # f32 results are not rounded further
+    refused("GR_ERR_UNSUPPORTED", call, q=s((2, 8, 4, 64), strides=(4096, 256, 64, 2)))
+    refused("GR_ERR_UNSUPPORTED", call, o=s((2, 8, 4, 64), strides=(4096, 0, 64, 1)))
+    refused("GR_ERR_UNSUPPORTED", call, o=s((2, 8, 4, 64), strides=(4096, 32, 64, 1)))
+    refused("GR_ERR_UNSUPPORTED", call, lse=s((2, 4, 8), strides=(64, 8, 1)))
+    refused("GR_ERR_UNSUPPORTED", call, o=s((2, 8, 4, 64)) + 1.0)           # nothing to write to
+    refused("GR_ERR_ALIAS", call, o=q)
+    refused("GR_ERR_ARG", call, dry.scores(scale=0.0))
+    refused("GR_ERR_ARG", call, dry.scores(scale=math.nan))
+    refused("GR_ERR_ARG", call, dry.scores(scale=-1.0))
+    refused("GR_ERR_ARG", call, dry.scores(cap=-1.0))
+    refused("GR_ERR_ARG", call, dry.scores(cap=math.inf))
+    refused("GR_ERR_ARG", call, dry.scores(prefix=i2))
+    refused("GR_ERR_ARG", call, dry.scores(position=1 << 40))
+    refused("GR_ERR_SHAPE", call, dry.scores(slopes=s((2,))))
+    refused("GR_ERR_DTYPE", call, dry.scores(slopes=s((4,), gr.GR_I32)))
+    refused("GR_ERR_DTYPE", call, dry.scores(lengths=s((2,))))
+    refused("GR_ERR_SHAPE", call, dry.scores(lengths=s((3,), gr.GR_I32)))
+    refused("GR_ERR_ARG", call, dry.scores(documents=(s((2, 8), gr.GR_I32), None)))
+    refused("GR_ERR_SHAPE", call, dry.scores(documents=s((2, 8), gr.GR_I32)))
+    d = [s((2, 8, 4, 64)), s((2, 9, 2, 64)), s((2, 9, 2, 64))]
+    grad = lambda **kw: gr.attention_grad(s((2, 8, 4, 64)), q, k, v, ok, o, lse, **{**dict(dq=d[0], dk=d[1], dv=d[2]), **kw})  # noqa: E731
+    grad()
+    refused("GR_ERR_ALIAS", grad, dv=d[1])
+    refused("GR_ERR_ALIAS", grad, dk=k)
+    refused("GR_ERR_SHAPE", grad, dq=d[1])
+    st = lambda sc, q=s((2, 4, 64)), o=s((2, 4, 64)): gr.attention_step(q, k, v, sc, out=o)  # noqa: E731
+    st(dry.scores(lengths=i2))
+    refused("GR_ERR_ARG", st, ok)                                           # no lengths
+    refused("GR_ERR_ARG", st, dry.scores(lengths=i2, causal=True))
+    refused("GR_ERR_SHAPE", st, dry.scores(lengths=i2), q=q)
+    rot = lambda x=q, f=gr.rotary_frequencies(64), p=0, o=o, **kw: gr.rotary(x, f, p, out=o, **kw)  # noqa: E731
+    rot()
+    refused("GR_ERR_SHAPE", rot, f=gr.rotary_frequencies(66))
+    refused("GR_ERR_ARG", rot, f=[math.inf])
+    refused("GR_ERR_ARG", rot, f=gr.rotary_frequencies(514))
+    refused("GR_ERR_ARG", rot, factor=math.nan)
+    refused("GR_ERR_SHAPE", rot, p=s((2, 9), gr.GR_I32))
+    refused("GR_ERR_DTYPE", rot, p=s((2, 8)))
+    refused("GR_ERR_DTYPE", rot, x=s((2, 8, 4, 64), gr.GR_I32))
+    # NULL scores, dead handles
+    L, u = gr.lib(), ctypes.c_uint64
+    assert L.gr_attention(dry._p, None, q.h, k.h, v.h, o.h, 0, 0) == 6
+    assert L.gr_attention_step(dry._p, None, 1 << 40, k.h, v.h, o.h) == 1
+    assert L.gr_attention(None, None, u(1), u(1), u(1), u(1), u(0), u(0)) == 6
+
+
+def test_without_a_device_arguments_are_checked_first():
+    c = gr.Context(device=-1)
+    s = Specs(c)
+    q, k = s((1, 8, 4, 64)), s((1, 8, 4, 64))
+    refused("GR_ERR_NODEVICE", gr.attention, q, k, s((1, 8, 4, 64)), c.scores(), out=s((1, 8, 4, 64)), lse=False)
+    refused("GR_ERR_SHAPE", gr.attention, q, k, s((1, 9, 4, 64)), c.scores(), out=s((1, 8, 4, 64)), lse=False)
+    refused("GR_ERR_NODEVICE", gr.rotary, q, gr.rotary_frequencies(64), 0, out=k)
+    c.close()
+
+
+def test_bf16_arrays_go_nowhere_else(dry):
+    s = Specs(dry)
+    a, b = s((4, 8), gr.GR_BF16), s((4, 8))
+    for f in (lambda: a + 1.0, lambda: a + a, lambda: a + b, lambda: -a, lambda: gr.exp(a), lambda: a.sum(), lambda: a.cumsum(0), lambda: a.reshape(32),
+              lambda: gr.dot(a, a), lambda: a[1:] * 2.0):
+        refused("GR_ERR_DTYPE", f)
+
+    def assign():
+        a[1:] = s((3, 8), gr.GR_BF16)
+    refused("GR_ERR_DTYPE", assign)
+    refused("GR_ERR_DTYPE", lambda: a[1:].plan())
+    assert a[1:, 2:].shape == (3, 6) and a.T.shape == (8, 4) and a[1:].dtype_code == gr.GR_BF16
+    assert a[1:, 2:].data_ptr()[0] == a.data_ptr()[0] + 2 * (8 + 2)
+
+
+def test_packed_results_are_told_from_overlapping_ones(dry):
+    s = Specs(dry)
+    q, k, v, o, do, lse = s((2, 8, 4, 64)), s((2, 8, 4, 64)), s((2, 8, 4, 64)), s((2, 8, 4, 64)), s((2, 8, 4, 64)), s((2, 4, 8))
+    base, row = s.at, 3 * 4 * 64
+    s.at += 1 << 20
+    part = lambda off, heads=4: dry.from_device(base + 4 * off, gr.GR_F32, (2, 8, heads, 64), (8 * row, row, 64, 1))  # noqa: E731
+    gr.attention_grad(do, q, k, v, dry.scores(), o, lse, dq=part(0), dk=part(256), dv=part(512))
+    refused("GR_ERR_ALIAS", gr.attention_grad, do, q, k, v, dry.scores(), o, lse, dq=part(0), dk=part(255), dv=part(512))
+    refused("GR_ERR_ALIAS", gr.attention_grad, do, q, k, v, dry.scores(), o, lse, dq=part(0), dk=part(256), dv=part(768))   # the next row
+    refused("GR_ERR_ALIAS", gr.attention_grad, do, part(0), k, v, dry.scores(), o, lse, dq=part(0), dk=part(256), dv=part(512))
+
+
+def test_frequencies():
+    f = gr.rotary_frequencies(8, base=100.0)
+    assert [round(x, 12) for x in f] == [round(100.0 ** (-i / 4), 12) for i in range(4)]
+    assert all(a == b / 4 for a, b in zip(gr.rotary_frequencies(8, 100.0, stretch=4.0), f))
+    g = gr.rotary_frequencies(64, stretch=8.0, context=4096)
+    plain_f = gr.rotary_frequencies(64)
+    assert g[0] == plain_f[0] and g[31] == plain_f[31] / 8 and all(a <= b <= 8 * a * (1 + 1e-12) for a, b in zip(g, plain_f))
+    with pytest.raises(ValueError):
+        gr.rotary_frequencies(7)
+
+
+def test_reference_gradient_against_differences():
+    """The formulas that the kernels are compared with, against central differences of the plain output."""
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(1, 5, h, 6, generator=g, dtype=torch.float64) for h in (4, 2, 2))
+    w = torch.randn(1, 5, 4, 6, generator=g, dtype=torch.float64)
+    kw = dict(cap=2.0, slopes=[0.5, 0.25, 0.1, 0.0], causal=True, prefix=torch.tensor([2]), documents=torch.tensor([[0, 0, 0, 1, 1]]))
+    ref = plain.attention(q, k, v, w, **kw)
+    for name, t in (("dq", q), ("dk", k), ("dv", v)):
+        for at in [(0, 0, 0, 0), (0, 3, 1, 5), (0, 4, 1, 2), (0, 1, 0, 3)]:
+            e = torch.zeros_like(t)
+            e[at] = 1e-5
+            i = ("dq", "dk", "dv").index(name)
+            up = [x + e if n == i else x for n, x in enumerate((q, k, v))]
+            dn = [x - e if n == i else x for n, x in enumerate((q, k, v))]
+            slope = ((plain.attention(*up, **kw)["out"] - plain.attention(*dn, **kw)["out"]) * w).sum() / 2e-5
+            assert abs(float(slope - ref[name][at])) < 1e-7, (name, at)
+
+
+# ------------------------------------------------------------------- on the GPU --
+@pytest.fixture(scope="module")
+def ctx():
+    c = gr.Context()
+    yield c
+    c.close()
+
+
+def normal(seed, *shape, dtype=F32, by=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * by).to(dtype).cuda()
+
+
+def case(B, N, M, H, HK, D, dtype, grad=True, **kw):
+    name = "-".join(str(x) for x in (B, N, M, H, HK, D)) + "-" + NAMES[dtype] + "".join(f"-{k}{'' if v is True else v}" for k, v in kw.items())
+    return pytest.param(dict(B=B, N=N, M=M, H=H, HK=HK, D=D, dtype=dtype, grad=grad, **kw), id=name)
+
+
+def options(c, seed=0):
+    """The tensors that a case's options name."""
+    g = torch.Generator().manual_seed(1000 + seed)
+    B, N, M = c["B"], c["N"], c["M"]
+    kw = dict(cap=c.get("cap", 0.0), causal=c.get("causal", False), position=c.get("position", 0))
+    if "scale" in c:
+        kw["scale"] = c["scale"]
+    if c.get("slopes"):
+        kw["slopes"] = torch.tensor([2.0 ** -(1 + i % 7) for i in range(c["H"])])
+    if c.get("prefix"):
+        kw["prefix"] = torch.randint(0, M + 2, (B,), generator=g, dtype=torch.int32)
+    if c.get("lengths"):
+        kw["lengths"] = torch.randint(-1, M + 3, (B,), generator=g, dtype=torch.int32)
+    if c.get("documents"):
+        ids = torch.sort(torch.randint(-1, c["documents"], (B, M), generator=g, dtype=torch.int32), 1)[0]
+        if c.get("shuffled"):
+            ids = ids[:, torch.randperm(M, generator=g)]
+        kw["documents"] = (ids[:, M - N:].contiguous() if N <= M else torch.randint(-1, c["documents"], (B, N), generator=g, dtype=torch.int32), ids)
+    return kw
+
+
+def on_gpu(ctx, kw):
+    got = {}
+    for w, t in kw.items():
+        if w == "documents":
+            t = tuple(ctx.array(x.cuda()) for x in t)
+        elif isinstance(t, torch.Tensor):
+            t = ctx.array(t.cuda())
+        got[w] = t
+    return ctx.scores(**got)
+
+
+def run_case(ctx, c, q, k, v, dout, kw, results=None):
+    """Through the entry points; returns torch tensors."""
+    sc = on_gpu(ctx, kw)
+    A = ctx.array
+    out = torch.empty_like(q) if results is None else results["out"]
+    out.fill_(7.0)
+    lse = torch.full((c["B"], c["H"], c["N"]), 7.0, device="cuda")
+    rest = A(torch.empty_like(q)) if c["dtype"] == BF16 and c["grad"] else None
+    gr.attention(A(q), A(k), A(v), sc, out=A(out), lse=A(lse), rest=rest)
+    got = dict(out=out, lse=lse)
+    if c["grad"]:
+        for w, t in (("dq", q), ("dk", k), ("dv", v)):
+            got[w] = torch.empty_like(t) if results is None else results[w]
+            got[w].fill_(7.0)
+        gr.attention_grad(A(dout), A(q), A(k), A(v), sc, A(out), A(lse), rest=rest, dq=A(got["dq"]), dk=A(got["dk"]), dv=A(got["dv"]))
+    torch.cuda.synchronize()
+    return got
+
+
+def tensors(c, seed=0):
+    by = 3.0 if c.get("cap") else 1.0
+    q, k, v, d = (normal(seed + i, c["B"], n, h, c["D"], dtype=c["dtype"], by=f)
+                  for i, (n, h, f) in enumerate(((c["N"], c["H"], by), (c["M"], c["HK"], 1.0), (c["M"], c["HK"], 1.0), (c["N"], c["H"], 1.0))))
+    return q, k, v, d
+
+
+CASES = [
+    case(1, 1, 1, 1, 1, 64, F32), case(1, 1, 1, 1, 1, 64, BF16),
+    case(2, 5, 7, 2, 1, 8, F32), case(2, 5, 7, 2, 1, 8, BF16),
+    case(1, 32, 32, 1, 1, 32, BF16, causal=True), case(1, 33, 31, 3, 1, 64, F32),
+    case(2, 64, 64, 4, 2, 64, F32, causal=True), case(2, 64, 64, 4, 2, 64, BF16, causal=True),
+    case(1, 129, 129, 2, 2, 128, BF16, causal=True), case(1, 129, 129, 2, 2, 128, F32, causal=True),
+    case(2, 65, 200, 8, 2, 96, BF16, causal=True, position=135), case(2, 65, 200, 8, 2, 96, F32, causal=True, position=135),
+    case(1, 70, 70, 2, 1, 80, F32, causal=True, slopes=True), case(1, 70, 70, 2, 1, 80, BF16, causal=True, slopes=True),
+    case(1, 100, 130, 6, 3, 256, BF16, cap=5.0), case(1, 100, 130, 6, 3, 256, F32, cap=5.0),
+    case(2, 77, 77, 4, 4, 100, BF16, cap=20.0, causal=True, prefix=True), case(2, 77, 77, 4, 4, 100, F32, cap=20.0, causal=True, prefix=True),
+    case(2, 150, 150, 4, 1, 64, BF16, causal=True, documents=4), case(2, 150, 150, 4, 1, 64, F32, documents=3),
+    case(1, 90, 260, 2, 1, 128, BF16, documents=5, shuffled=True, causal=True, position=100), case(1, 90, 260, 2, 1, 128, F32, documents=2, shuffled=True),
+    case(3, 40, 300, 4, 2, 64, BF16, lengths=True), case(3, 40, 300, 4, 2, 64, F32, lengths=True, cap=10.0, slopes=True, causal=True, position=200),
+    case(2, 200, 60, 2, 2, 64, BF16, causal=True, position=-100), case(2, 50, 60, 2, 2, 72, F32, causal=True, position=-30, prefix=True),
+    case(1, 3, 1000, 8, 1, 128, BF16, causal=True, position=990, grad=False), case(2, 2, 700, 4, 4, 256, F32, grad=False),
+    case(1, 4, 5, 32, 1, 160, BF16, cap=3.0, slopes=True), case(1, 3, 40, 16, 1, 192, F32, cap=3.0, slopes=True, causal=True, position=37),
+    case(1, 300, 300, 1, 1, 1, F32), case(1, 50, 50, 2, 1, 3, BF16, causal=True),
+    case(1, 600, 600, 16, 2, 64, BF16, causal=True), case(1, 16, 2100, 2, 1, 64, F32, causal=True, position=2084),
+    case(1, 64, 64, 2, 2, 64, F32, scale=40.0), case(1, 64, 64, 2, 2, 64, BF16, scale=1e-4),
+    case(2, 0, 5, 2, 1, 64, F32), case(2, 5, 0, 2, 1, 64, BF16), case(0, 5, 5, 2, 1, 64, F32),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("c", CASES)
+def test_against_plain(ctx, c):
+    q, k, v, d = tensors(c)
+    kw = options(c)
+    got = run_case(ctx, c, q, k, v, d, kw)
+    ref = plain.attention(q, k, v, d if c["grad"] else None, **kw)
+    plain.check(got, ref, c["dtype"], c["D"], c["M"], c["N"], c["H"] // c["HK"], "plain", cap=c.get("cap", 0.0))
+
+
+LAYOUTS = ["heads_first", "packed", "odd_address", "odd_rows", "backwards", "broadcast"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_strides(ctx, layout, dtype):
+    c = dict(B=2, N=75, M=75, H=4, HK=4, D=64, dtype=dtype, grad=True, causal=True)
+    shape = (2, 75, 4, 64)
+
+    def lay(seed, part):
+        t = normal(seed, *shape, dtype=dtype)
+        if layout == "heads_first":
+            r = torch.empty(2, 4, 75, 64, dtype=dtype, device="cuda").transpose(1, 2)
+        elif layout == "packed":
+            r = packs[part // 3][:, :, part % 3]
+        elif layout == "odd_address":
+            r = torch.empty(2 * 75 * 256 + 1, dtype=dtype, device="cuda")[1:].view(shape)
+        elif layout == "odd_rows":
+            r = torch.empty(2, 75, 4, 65, dtype=dtype, device="cuda")[..., :64]
+        elif layout == "backwards":
+            n = 2 * 75 * 256
+            r = None
+            base = torch.empty(n, dtype=dtype, device="cuda")
+            a = ctx.from_device(base.data_ptr() + base.element_size() * (n - 256), {F32: gr.GR_F32, BF16: gr.GR_BF16}[dtype], shape, (-256, -512, 64, 1), owner=base)
+            back = base.view(75, 2, 4, 64).flip(0, 1).transpose(0, 1)   # (a copy: what the view shows)
+            return a, back, base
+        else:
+            r = torch.empty(2, 75, 1, 64, dtype=dtype, device="cuda").expand(shape) if part in (1, 2) else torch.empty(shape, dtype=dtype, device="cuda")
+            if part in (1, 2):
+                r[:, :, :1].copy_(t[:, :, :1])
+                return r
+        r.copy_(t)
+        return r
+
+    packs = [torch.zeros(2, 75, 3, 4, 64, dtype=dtype, device="cuda") for _ in range(3)]
+    kw = options(c)
+    if layout == "backwards":
+        arrays, shown, bases = [], [], []
+        for i in range(8):
+            a, _, base = lay(i, i)
+            base.copy_(normal(i, base.numel(), dtype=dtype))
+            arrays.append(a)
+            bases.append(base)
+        show = lambda b: b.view(75, 2, 4, 64).flip(0, 1).transpose(0, 1)  # noqa: E731
+        q, k, v, d = (show(b).clone() for b in bases[:4])
+        sc = on_gpu(ctx, kw)
+        lse = ctx.array(torch.empty(2, 4, 75, device="cuda"))
+        gr.attention(*arrays[:3], sc, out=arrays[4], lse=lse)
+        gr.attention_grad(arrays[3], *arrays[:3], sc, arrays[4], lse, dq=arrays[5], dk=arrays[6], dv=arrays[7])
+        torch.cuda.synchronize()
+        got = dict(zip(("out", "dq", "dk", "dv"), (show(b) for b in bases[4:])))
+    else:
+        q, k, v, d = (lay(i, i) for i in range(4))
+        res = dict(zip(("out", "dq", "dk", "dv"), (torch.empty_like(d) if layout == "broadcast" else lay(9 + i, (3, 6, 7, 8)[i]) for i in range(4))))
+        if layout == "packed":
+            res["out"] = torch.empty_like(d)
+        got = run_case(ctx, c, q, k, v, d, kw, results=res)
+    ref = plain.attention(q, k, v, d, **kw)
+    plain.check({w: t for w, t in got.items()}, ref, dtype, 64, 75, 75, 1, layout)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+def test_what_is_not_seen_has_no_say(ctx, dtype):
+    """Infinities and NaN behind the lengths, in keys that belong to no document, in masked scores."""
+    c = dict(B=2, N=40, M=200, H=4, HK=2, D=64, dtype=dtype, grad=True)
+    q, k, v, d = tensors(c)
+    lengths = torch.tensor([130, 0], dtype=torch.int32)
+    clean = run_case(ctx, c, q, k, v, d, dict(lengths=lengths))
+    for t, bad in ((k, math.nan), (v, math.inf)):
+        t[0, 130:] = bad
+        t[1] = bad
+    dirty = run_case(ctx, c, q, k, v, d, dict(lengths=lengths))
+    for w in clean:
+        assert torch.equal(clean[w], dirty[w]), w
+    assert (dirty["out"][1] == 0).all() and (dirty["lse"][1] == -math.inf).all() and (dirty["dk"][0, 130:] == 0).all() and (dirty["dq"][1] == 0).all()
+    # a query far to the left of everything: its scores are the type's lowest numbers, not masked ones
+    low = run_case(ctx, dict(c, grad=False), (q.float() * 0 + 1e15).to(dtype), (k.float() * 0 - 1e15).nan_to_num(-1e15).to(dtype), torch.ones_like(v), d, {})
+    assert torch.isfinite(low["out"]).all() and ((low["out"].float() - 1).abs() < 0.01).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("B,M,H,HK,D,kw", [
+    (1, 1, 1, 1, 64, {}), (3, 40, 4, 4, 64, {}), (2, 300, 8, 1, 128, dict(cap=10.0)), (4, 1000, 16, 2, 96, dict(slopes=True)),
+    (1, 5000, 32, 1, 64, dict(cap=30.0, slopes=True)), (2, 777, 40, 1, 80, {}), (2, 129, 6, 3, 256, dict(cap=5.0)), (1, 33, 2, 2, 5, {}), (2, 0, 2, 1, 64, {}),
+])
+def test_single_tokens(ctx, B, M, H, HK, D, kw, dtype):
+    q, k, v = normal(1, B, H, D, dtype=dtype, by=2.0), normal(2, B, M, HK, D, dtype=dtype), normal(3, B, M, HK, D, dtype=dtype)
+    g = torch.Generator().manual_seed(5)
+    kw = dict(kw, lengths=torch.randint(0, M + 1, (B,), generator=g, dtype=torch.int32))
+    kw["lengths"][0] = M
+    if kw.pop("slopes", None):
+        kw["slopes"] = torch.tensor([2.0 ** -(1 + i % 9) for i in range(H)])
+    for b in range(B):
+        k[b, int(kw["lengths"][b]):] = math.nan
+        v[b, int(kw["lengths"][b]):] = math.nan
+    out = torch.full_like(q, 7.0)
+    gr.attention_step(ctx.array(q), ctx.array(k), ctx.array(v), on_gpu(ctx, kw), out=ctx.array(out))
+    torch.cuda.synchronize()
+    ref = plain.attention(q[:, None], k.nan_to_num(0.0), v.nan_to_num(0.0), step=True, **kw)
+    plain.check(dict(out=out[:, None]), ref, dtype, D, M, 1, H // HK, "step", cap=kw.get("cap", 0.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("B,N,H,D,part", [(1, 1, 1, 64, 64), (2, 33, 3, 80, 32), (1, 7, 2, 5, 4), (3, 100, 32, 128, 128), (2, 9, 1, 256, 256), (1, 5, 4, 96, 90), (1, 3, 2, 8, 0)])
+def test_rotary(ctx, B, N, H, D, part, interleaved, dtype):
+    x = normal(1, B, N, H, D, dtype=dtype)
+    f = gr.rotary_frequencies(part)
+    g = torch.Generator().manual_seed(2)
+    pos = torch.randint(-5, 2_000_000_000, (B, N), generator=g, dtype=torch.int32)
+    for inverse, factor in ((False, 1.0), (True, 1.25)):
+        ref = plain.rotary(x, f, pos.numpy(), interleaved, inverse, factor)
+        # two products, each of a sine off by half a step and a few of the polynomial's roundings; angles: positions below 2^31 in 64 bits leave 2e-7 of a turn's last place
+        size = plain.rotary(x.abs(), [0.0] * (part // 2), pos.numpy())
+        bar = plain.HALF[dtype] * ref.abs() + (6 * 2.0 ** -24 + 1e-6) * factor * 2 * size.amax(-1, keepdim=True)
+        y = gr.rotary(ctx.array(x), f, ctx.array(pos.cuda()), interleaved, inverse, factor).torch().cpu().double()
+        assert ((y - ref).abs() <= bar).all(), float(((y - ref).abs() / bar).max())
+        z = x.clone()
+        gr.rotary(ctx.array(z), f, ctx.array(pos.cuda()), interleaved, inverse, factor, out=ctx.array(z))   # in place
+        assert torch.equal(z.cpu().double(), y)
+    # small positions: right to a few roundings
+    ref = plain.rotary(x, f, torch.arange(N).numpy()[None] + 3, interleaved)
+    y = gr.rotary(ctx.array(x), f, 3, interleaved).torch().cpu().double()
+    assert ((y - ref).abs() <= plain.HALF[dtype] * ref.abs() + 8 * 2.0 ** -24 * x.abs().amax().item()).all()
+    # strided, unaligned, into a strided place
+    wide = torch.empty(B, H, N, D + 3, dtype=dtype, device="cuda")
+    src, dst = wide[..., 1:D + 1].transpose(1, 2), torch.zeros(B, N, H, 2 * D + 1, dtype=dtype, device="cuda")
+    src.copy_(x)
+    gr.rotary(ctx.array(src), f, 3, interleaved, out=ctx.array(dst[..., D:2 * D]))
+    assert torch.equal(dst[..., D:2 * D].cpu().double(), y) and (dst[..., :D] == 0).all() and (dst[..., 2 * D:] == 0).all()
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences(ctx):
+    """dq, dk, dv of the kernels against differences of the kernels' own output: f32, one direction at a time."""
+    c = dict(B=1, N=40, M=40, H=4, HK=2, D=64, dtype=F32, grad=True, cap=4.0, causal=True, slopes=True)
+    q, k, v, d = tensors(c)
+    kw = options(c)
+    got = run_case(ctx, c, q, k, v, d, kw)
+    fwd = dict(c, grad=False)
+    for name, i in (("dq", 0), ("dk", 1), ("dv", 2)):
+        ts = [q, k, v]
+        e = normal(50 + i, *ts[i].shape)
+        h = 2.0 ** -6
+        up, dn = list(ts), list(ts)
+        up[i], dn[i] = ts[i] + h * e, ts[i] - h * e
+        slope = ((run_case(ctx, fwd, *up, d, kw)["out"].double() - run_case(ctx, fwd, *dn, d, kw)["out"].double()) * d.double()).sum() / (2 * h)
+        # the difference is off by h^2 / 6 of a third derivative and 2^-24 / h of the output's size
+        want = (got[name].double() * e.double()).sum()
+        size = (got[name].double().norm() * e.double().norm())
+        assert abs(float(slope - want)) <= 2e-3 * float(size) + 1e-2, (name, float(slope), float(want))
+
+
+@pytest.mark.gpu
+def test_same_bits_every_time(ctx):
+    c = dict(B=1, N=500, M=900, H=8, HK=1, D=64, dtype=BF16, grad=True, causal=True, position=400)
+    q, k, v, d = tensors(c)
+    first = run_case(ctx, c, q, k, v, d, options(c))
+    for _ in range(3):
+        again = run_case(ctx, c, q, k, v, d, options(c))
+        for w in first:
+            assert torch.equal(first[w], again[w]), w
+
+
+@pytest.mark.gpu
+def test_lazy_operands_and_pending_readers(ctx):
+    """Operands that are still expressions are evaluated; what was recorded over a result's storage keeps the old values."""
+    x = normal(1, 24, 32)
+    w = [normal(2 + i, 32, 64) for i in range(3)]
+    lx = ctx.array(x)
+    q, k, v = (gr.reshape(gr.dot(lx, ctx.array(t)) * 0.5, (1, 24, 4, 16)) for t in w)
+    out = torch.full((1, 24, 4, 16), 3.0, device="cuda")
+    lo = ctx.array(out)
+    pending = lo * 2.0
+    o, lse = gr.attention(q, k, v, ctx.scores(causal=True), out=lo)
+    after = lo + 1.0
+    ref = plain.attention(*((x @ t * 0.5).view(1, 24, 4, 16) for t in w), causal=True)
+    assert (pending.torch() == 6.0).all()
+    assert (after.torch().cpu().double() - 1.0 - ref["out"]).abs().max() < 1e-4
+    assert (lse.torch().cpu().double() - ref["lse"]).abs().max() < 1e-4
+    assert o is lo
+
+
+@pytest.mark.gpu
+def test_graph_replays(ctx):
+    """Forward, gradient and a step captured together and replayed on new data, with eager work in between."""
+    stream = torch.cuda.Stream()
+    c2 = gr.Context(stream=stream.cuda_stream)
+    c = dict(B=1, N=100, M=100, H=4, HK=1, D=64, dtype=BF16, grad=True, causal=True)
+    with torch.cuda.stream(stream):
+        q, k, v, d = tensors(c)
+        docs = torch.arange(100, device="cuda", dtype=torch.int32)[None] // 40
+        lens = torch.tensor([70], device="cuda", dtype=torch.int32)
+        res = dict(out=torch.empty_like(q), rest=torch.empty_like(q), lse=torch.empty(1, 4, 100, device="cuda"), dq=torch.empty_like(q), dk=torch.empty_like(k),
+                   dv=torch.empty_like(v), tok=torch.empty(1, 4, 64, dtype=BF16, device="cuda"))
+
+        def go(r):
+            A = c2.array
+            sc = c2.scores(causal=True, documents=A(docs))
+            gr.attention(A(q), A(k), A(v), sc, out=A(r["out"]), lse=A(r["lse"]), rest=A(r["rest"]))
+            gr.attention_grad(A(d), A(q), A(k), A(v), sc, A(r["out"]), A(r["lse"]), rest=A(r["rest"]), dq=A(r["dq"]), dk=A(r["dk"]), dv=A(r["dv"]))
+            gr.attention_step(A(q[:, 5]), A(k), A(v), c2.scores(lengths=A(lens)), out=A(r["tok"]))
+
+        go(res)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            go(res)
+        for rep in range(3):
+            for t, s in ((q, 1), (k, 2), (v, 3), (d, 4)):
+                t.copy_(normal(100 * rep + s, *t.shape, dtype=BF16))
+            eager = {w: torch.empty_like(t) for w, t in res.items()}
+            for t in res.values():
+                t.zero_()
+            graph.replay()
+            stream.synchronize()
+            go(eager)
+            stream.synchronize()
+            for w in res:
+                assert torch.equal(res[w], eager[w]), (rep, w)
+    # a call that would have to allocate during a capture says so
+    c3 = gr.Context(stream=stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        one = [normal(7, 1, 4, 1, 64, dtype=BF16), normal(8, 1, 6000, 1, 64, dtype=BF16), torch.empty(1, 4, 1, 64, dtype=BF16, device="cuda")]
+        graph2 = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph2, stream=stream):
+            refused("GR_ERR_OOM", gr.attention, c3.array(one[0]), c3.array(one[1]), c3.array(one[1]), c3.scores(), out=c3.array(one[2]), lse=False)
+            one[2].zero_()
+    c3.close()
+    del graph, graph2
+    c2.close()
+
+
+@pytest.mark.gpu
+def test_far_offsets(ctx):
+    """Rows behind 2^32 elements of a buffer, and rows whose steps are too long for the fast loads."""
+    step = (1 << 31) // 64 + 64            # elements between rows: 64 rows pass 2^31, 129 pass 2^32
+    k = torch.zeros(130 * step, dtype=BF16, device="cuda")
+    v = torch.zeros(130 * step, dtype=BF16, device="cuda")
+    kv = normal(1, 2, 130, 64, dtype=BF16)
+    for i, t in enumerate((k, v)):
+        t.as_strided((130, 64), (step, 1)).copy_(kv[i])
+    q = normal(2, 1, 4, 2, 64, dtype=BF16)
+    for shape, strides in (((1, 130, 1, 64), (0, step, 0, 1)), ((130, 1, 1, 64), (step, 0, 0, 1))):
+        B = shape[0]
+        lk, lv = (ctx.from_device(t.data_ptr(), gr.GR_BF16, shape, strides, owner=t) for t in (k, v))
+        qb = q.expand(B, 4, 2, 64).contiguous()
+        out = torch.empty_like(qb)
+        gr.attention(ctx.array(qb), lk, lv, ctx.scores(), out=ctx.array(out), lse=False)
+        ref = plain.attention(qb, kv[0].view(shape), kv[1].view(shape))
+        plain.check(dict(out=out), ref, BF16, 64, shape[1], 4, 2, "far")
