@@ -315,7 +315,7 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   const bool divided = rows <= 32;
   const int keys = keys_of(divided, size, dp);
   a.blocks = (int)((rows + (divided ? 31 : 127)) / (divided ? 32 : 128));
-  a.splits = splits_of(pairs * a.blocks, ((int64_t)a.M + keys - 1) / keys, 128);
+  a.splits = splits_of(pairs * a.blocks, ((int64_t)a.M + keys - 1) / keys, MAX_SPLITS);
   const int64_t blocks = (int64_t)a.blocks * a.splits;
   if (blocks * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
@@ -438,19 +438,21 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   const int qtile = tile_rows(size, dp);
   const int ksplits = splits_of(pairs * kblocks, (((int64_t)a.N + qtile - 1) / qtile) * a.G, 16);
   if (std::max(qblocks, kblocks * ksplits) * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
-  const size_t dl = rounded((size_t)a.B * a.H * a.N * 4);
+  const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0, qr = a.kdoc ? rounded((size_t)a.B * ((a.N + 31) / 32) * 8) : 0;
+  const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0;
   const size_t parts = ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0;
   char* ws;
-  TRY(c.space(dl + kr + qr + parts, &ws));
-  float* const d = (float*)ws;
-  a.delta = d;
-  a.kranges = (int*)(ws + dl);
-  a.qranges = (int*)(ws + dl + kr);
-  a.part_o = (float*)(ws + dl + kr + qr);
+  TRY(c.space(2 * st + kr + qr + qd + parts, &ws));
+  a.less = (float*)ws;
+  a.delta = (float*)(ws + st);
+  a.kranges = (int*)(ws + 2 * st);
+  a.qranges = (int*)(ws + 2 * st + kr);
+  a.qdocs = (int*)(ws + 2 * st + kr + qr);
+  a.part_o = (float*)(ws + 2 * st + kr + qr + qd);
   if (a.kdoc && a.M > 0 && a.N > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   if (a.N > 0) {
-    TRY(c.launch("gr_attention_delta", [&] { return delta(a, type, d, c.ctx->stream); }));
+    TRY(c.launch("gr_attention_statistics", [&] { return statistics(a, type, c.ctx->stream); }));
     a.splits = 1;
     a.blocks = (int)qblocks;
     const unsigned grid = grid_of((int)pairs, qblocks);

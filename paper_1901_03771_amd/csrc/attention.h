@@ -20,7 +20,9 @@ struct Tensor {
 struct Args {
   Tensor q, k, v, out, rest, dout, dq, dk, dv;
   float* lse = nullptr;          // (B, H, N)
-  const float* delta = nullptr;  // (B, H, N): sum over d of dout * out
+  // of the gradient, (B, H, NP) with NP = N rounded up to whole tiles: less = lse in binary logarithms - LIFT (rows that see nothing, and
+  // rows behind the last: +inf), delta = sum over d of dout * out
+  float *less = nullptr, *delta = nullptr;
   float* part_o = nullptr;       // (splits, B * HK, N * G, DP) unnormalised sums of a split's keys, or the parts of dk and dv
   float* part_ml = nullptr;      // (splits, B * HK, N * G, 2) maximum (binary logarithms) and sum
   const float* slopes = nullptr; // (H), stride slopes_s
@@ -34,6 +36,7 @@ struct Args {
   int64_t qdoc_sb = 0, qdoc_sn = 0, kdoc_sb = 0, kdoc_sn = 0;
   int* kranges = nullptr;        // (B, ceil(M / 32), 2): smallest and largest document number of 32 keys
   int* qranges = nullptr;        // (B, ceil(N / 32), 2), the same of 32 queries
+  int* qdocs = nullptr;          // (B, NP), the documents of the queries side by side, -1 behind the last
   int64_t position = 0;          // of query 0
   int B = 0, N = 0, M = 0, H = 0, HK = 0, G = 0, D = 0;
   int causal = 0, step = 0;      // step: a query stands at its sequence's last key
@@ -46,9 +49,12 @@ struct Args {
 enum { MODE_CAP = 1, MODE_BIAS = 2 };
 enum { TYPE_F32 = 0, TYPE_BF16 = 1 };
 
+constexpr int64_t padded_rows(int64_t n) { return (n + 63) / 64 * 64; }
+
 // Sizes that host and kernels share, for an element of `size` bytes and heads padded to `dp` values.
 constexpr int row_values(int dp) { return dp <= 64 ? 64 : dp <= 128 ? 128 : 256; }                 // of a row in LDS
 constexpr int tile_rows(int size, int dp) { return size * row_values(dp) <= 256 ? 64 : 32; }       // of a tile that waves share
+constexpr int MAX_SPLITS = 128;
 constexpr int shared_waves(int size, int dp) { return size * row_values(dp) <= 256 ? 4 : size * row_values(dp) <= 512 ? 2 : 1; }  // that divide a tile's keys
 
 // Workgroups that place_of (attention_kernels.h) deals `blocks` of each of `pairs` heads to.
@@ -61,7 +67,7 @@ hipError_t forward_f32(const Args& a, int dp, int mode, bool divided, unsigned g
 hipError_t forward_bf16(const Args& a, int dp, int mode, bool divided, unsigned grid, hipStream_t stream);
 hipError_t combine(const Args& a, int type, int dp, hipStream_t stream);
 hipError_t ranges(const Args& a, hipStream_t stream);
-hipError_t delta(const Args& a, int type, float* to, hipStream_t stream);
+hipError_t statistics(const Args& a, int type, hipStream_t stream);
 hipError_t grad_q_f32(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);
 hipError_t grad_q_bf16(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);
 hipError_t grad_kv_f32(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);

@@ -71,11 +71,8 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
 #pragma unroll
     for (int s = 0; s < L::STEPS; ++s) { qf[s] = L::fetch(q, s, hi, a.D, valid, a.q.aligned); df[s] = L::fetch(d, s, hi, a.D, valid, a.dout.aligned); }
   }
-  const int64_t stat = ((int64_t)b * a.H + h) * a.N + i;
-  // a row that sees nothing has lse = -inf: its probabilities are 2^-inf
-  const float lse_ = valid ? a.lse[stat] : -INF, less = lse_ == -INF ? INF : lse_ * LOG2E - LIFT, delta = valid ? a.delta[stat] : 0.0f;
-  // (an lse of 2^20 and more is rounded by as much as an exponent counts: no probability passes 1 for that)
-  const bool huge = __any(less != INF && __builtin_fabsf(less) > 1048576.0f);
+  const int64_t stat = ((int64_t)b * a.H + h) * padded_rows(a.N) + i;
+  const float less = valid ? a.less[stat] : INF, delta = valid ? a.delta[stat] : 0.0f;
   const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
   const float pos = MODE & MODE_BIAS ? (float)(a.position + i) : 0.0f;
 
@@ -104,8 +101,11 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
     for (int kb = 0; kb < S::KEYS / 32; ++kb) {
       const int key0 = t * S::KEYS + kb * 32;
       if (key0 >= w_last) break;
-      bool whole = key0 + 32 <= w_first;
-      if (ranges) whole = whole && ranges[2 * (key0 / 32)] == w_hi && ranges[2 * (key0 / 32) + 1] == w_hi && w_all == w_hi;
+      bool whole = key0 + 32 <= w_first, one = true;
+      if (ranges) {
+        one = ranges[2 * (key0 / 32)] == w_hi && ranges[2 * (key0 / 32) + 1] == w_hi && w_all == w_hi && w_hi >= 0;
+        whole = whole && one;
+      }
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
@@ -124,19 +124,21 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
         dp[r] -= delta;
         if constexpr (MODE & MODE_CAP) dp[r] *= bend;
       }
-      if (huge) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_fminf(s[r], LIFT);
-      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]) * dp[r];
       if (!whole) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = key0 + (r & 3) + 8 * (r >> 2) + 4 * hi;
-          bool seen = key < see;
-          if (a.kdoc && seen) seen = doc >= 0 && a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn] == doc;
-          s[r] = seen ? s[r] : 0.0f;
+          s[r] = key < see ? s[r] : 0.0f;
+        }
+        if (!one) {
+          const int* const kd = a.kdoc + b * a.kdoc_sb;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = min(key0 + (r & 3) + 8 * (r >> 2) + 4 * hi, a.M - 1);
+            s[r] = kd[key * a.kdoc_sn] == doc && doc >= 0 ? s[r] : 0.0f;
+          }
         }
       }
 #pragma unroll
@@ -168,7 +170,7 @@ enum { BOTH = 0, ONLY_V = 1, ONLY_K = 2 };
 template <class T, int DP, int WHICH>
 struct ShapeKV {
   static constexpr int ROWS = tile_rows(sizeof(T), DP), KEYS = 128, TILE = ROWS * Tile<T, DP>::ROW;   // rows: of a tile of queries
-  static constexpr int STATS = 4 * ROWS + 4;                 // four numbers per row, and whether any lse is huge
+  static constexpr int STATS = 4 * ROWS;                     // less, delta and document of every row
   static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
   static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
   static constexpr int PER_CU = REGS <= 240 && 2 * LDS <= 160 * 1024 ? 2 : 1;
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   constexpr bool WANT_K = WHICH != ONLY_V, WANT_V = WHICH != ONLY_K;
   extern __shared__ char smem_[];
   GR_LDS char* const smem = (GR_LDS char*)smem_;
-  GR_LDS float* const stats = (GR_LDS float*)(smem + 4 * S::TILE);   // [stage][less, delta, keys seen, document][row]
+  GR_LDS float* const stats = (GR_LDS float*)(smem + 4 * S::TILE);   // [stage][less, delta, document][row]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
   const int pairs = a.B * a.HK;
   const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
@@ -249,39 +251,21 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     }
     return u1;
   };
-  float r_less = 0.0f, r_delta = 0.0f;
-  int r_see = 0, r_doc = -1;
   auto load = [&](int u, int stage) {
     const int g = u / span, t = t0 + (u - g * span), h = hk * a.G + g;
     const int64_t i0 = (int64_t)t * S::ROWS;
     const int rows = min(S::ROWS, a.N - (int)i0);
-    L::template load<S::ROWS, 256>(smem + 2 * stage * S::TILE, at<T>(a.q, b, i0, h), a.q.sn, rows, a.D, tid, a.q.direct);
-    L::template load<S::ROWS, 256>(smem + (2 * stage + 1) * S::TILE, at<T>(a.dout, b, i0, h), a.dout.sn, rows, a.D, tid, a.dout.direct);
-    if (tid < S::ROWS) {
-      const bool in = tid < rows;
-      const int i = (int)i0 + (in ? tid : 0);
-      const int64_t stat = ((int64_t)b * a.H + h) * a.N + i;
-      const float e = in ? a.lse[stat] : -INF;
-      r_less = e == -INF ? INF : e * LOG2E - LIFT;
-      r_delta = in ? a.delta[stat] : 0.0f;
-      r_see = in ? keys_seen(a, i, len, pre) : 0;
-      r_doc = in && a.kdoc ? a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn] : -1;
-    }
-  };
-  auto settle = [&](int stage) {
-    if (tid < S::ROWS) {
-      GR_LDS float* const to = stats + stage * S::STATS;
-      to[tid] = r_less;
-      to[S::ROWS + tid] = r_delta;
-      ((GR_LDS int*)to)[2 * S::ROWS + tid] = r_see;
-      ((GR_LDS int*)to)[3 * S::ROWS + tid] = r_doc;
-      // (an lse of 2^20 and more is rounded by as much as an exponent counts: no probability passes 1 for that)
-      const bool huge = __any(r_less != INF && __builtin_fabsf(r_less) > 1048576.0f);
-      if (tid == 0) ((GR_LDS int*)to)[4 * S::ROWS] = huge;
-    }
+    L::template load<S::ROWS, 256>(smem + 2 * stage * S::TILE, at<T>(a.q, b, i0, h), a.q.sn, rows, a.D, fresh(tid), a.q.direct);
+    L::template load<S::ROWS, 256>(smem + (2 * stage + 1) * S::TILE, at<T>(a.dout, b, i0, h), a.dout.sn, rows, a.D, fresh(tid), a.dout.direct);
+    // (a tile's rows behind the last are there: +inf, 0, -1)
+    const int64_t np = padded_rows(a.N), stat = ((int64_t)b * a.H + h) * np + i0;
+    GR_LDS float* const to = stats + stage * S::STATS;
+    if (wave == 0) load_words(to, a.less + stat, lane, S::ROWS);
+    else if (wave == 1) load_words(to + S::ROWS, a.delta + stat, lane, S::ROWS);
+    else if (wave == 2 && a.kdoc) load_words(to + 2 * S::ROWS, a.qdocs + b * np + i0, lane, S::ROWS);
   };
   int u = next(u0), stage = 0;
-  if (u < u1) { load(u, 0); settle(0); }
+  if (u < u1) load(u, 0);
   while (u < u1) {
     const int after = next(u + 1);
     arrive();
@@ -291,21 +275,24 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     const GR_LDS char* const dt = qt + S::TILE;
     const GR_LDS float* const st = stats + stage * S::STATS;
     const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
-    const bool huge = __builtin_amdgcn_readfirstlane(((const GR_LDS int*)st)[4 * S::ROWS]) != 0;
 #pragma unroll 1
     for (int rb = 0; rb < S::ROWS / 32; ++rb) {
       const int i0 = t * S::ROWS + rb * 32;
       if (i0 >= a.N) break;
       const int see_last = keys_seen(a, min(i0 + 31, a.N - 1), len, pre);
       if (see_last <= key0) continue;
+      const int fcol = fresh(col), flane = fresh(lane);
       // (rows behind the last query need no mask: their lse is none)
-      bool whole = keys_seen(a, i0, len, pre) >= key0 + 32;
-      if (ranges) whole = whole && w_one && ranges[2 * (i0 / 32)] == w_doc && ranges[2 * (i0 / 32) + 1] == w_doc;
+      bool whole = keys_seen(a, i0, len, pre) >= key0 + 32, one = true;
+      if (ranges) {
+        one = w_one && ranges[2 * (i0 / 32)] == w_doc && ranges[2 * (i0 / 32) + 1] == w_doc;
+        whole = whole && one;
+      }
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int x = 0; x < L::STEPS; ++x) {
-        s = mma(L::row(qt, rb * 32 + col, x, hi), kf[x], s);
-        if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + col, x, hi), vf[x], dp);
+        s = mma(L::row(qt, rb * 32 + fcol, x, hi), kf[x], s);
+        if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + fcol, x, hi), vf[x], dp);
       }
       if constexpr (WANT_K) finished(s, dp);
       else finished(s);
@@ -313,7 +300,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
       for (int r4 = 0; r4 < 4; ++r4) {
         const int rr = rb * 32 + 8 * r4 + 4 * hi;
         const f32x4 less = *(const GR_LDS f32x4*)(st + rr), delta = *(const GR_LDS f32x4*)(st + S::ROWS + rr);
-        const i32x4 see = whole ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rr), docs = whole ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 3 * S::ROWS + rr);
+        const i32x4 docs = one ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rr);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * r4 + e;
@@ -322,10 +309,10 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
           float x;
           if constexpr (MODE & MODE_BIAS) x = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf((float)(a.position + t * S::ROWS + rr + e) - (float)key), -less[e]));
           else x = __builtin_fmaf(y, a.c, -less[e]);
-          float p = exp2_(huge ? __builtin_fminf(x, LIFT) : x);
+          float p = exp2_(x);
           if (!whole) {
-            bool seen = key < see[e];
-            if (a.kdoc) seen = seen && doc >= 0 && docs[e] == doc;
+            bool seen = key < keys_seen(a, t * S::ROWS + rr + e, len, pre);
+            if (!one) seen = seen & (doc >= 0) & (docs[e] == doc);
             p = seen ? p : 0.0f;
           }
           s[r] = p;
@@ -343,16 +330,15 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
         if constexpr (WANT_V) {
           operand(s, x, f);
 #pragma unroll
-          for (int d = 0; d < L::BLOCKS; ++d) ov[d] = mma(L::column(dt, rb * 32 + x * 16, d, lane), f, ov[d]);
+          for (int d = 0; d < L::BLOCKS; ++d) ov[d] = mma(L::column(dt, rb * 32 + x * 16, d, flane), f, ov[d]);
         }
         if constexpr (WANT_K) {
           operand(dp, x, f);
 #pragma unroll
-          for (int d = 0; d < L::BLOCKS; ++d) ok[d] = mma(L::column(qt, rb * 32 + x * 16, d, lane), f, ok[d]);
+          for (int d = 0; d < L::BLOCKS; ++d) ok[d] = mma(L::column(qt, rb * 32 + x * 16, d, flane), f, ok[d]);
         }
       }
     }
-    if (after < u1) settle(stage ^ 1);
     u = after;
     stage ^= 1;
   }

@@ -33,7 +33,9 @@ struct Shape {
   static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
-template <class T, int DP, int MODE, bool DIVIDED>
+// PRECISE (bfloat16, where `rest` is wanted): a probability enters its product as the sum of two bfloat16 numbers, so that out + rest is the output to
+// 2^-16 and not only what 8 bits of every probability give: the gradient's dp - delta nearly cancels for queries that see few keys.
+template <class T, int DP, int MODE, bool DIVIDED, bool PRECISE>
 __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIVIDED>::PER_CU)) void gr_attention_kernel(const Args a) {
   typedef Shape<T, DP, DIVIDED> S;
   typedef Tile<T, DP> L;
@@ -116,13 +118,14 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
     const GR_LDS char* const vt = kt + S::TILE;
     const int key0 = t * S::KEYS + (DIVIDED ? wave * 32 : 0);
     if (key0 < w_last) {
-      bool whole = key0 + 32 * S::KB <= w_first;
+      bool whole = key0 + 32 * S::KB <= w_first, one = true;   // one: all keys and all of the wave's rows belong to one document
       if (ranges) {
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb) {
-          const int e = key0 / 32 + kb;
-          whole = whole && ranges[2 * e] == w_hi && ranges[2 * e + 1] == w_hi && w_all == w_hi;
+          const int e = min(key0 / 32 + kb, pieces - 1);
+          one &= ranges[2 * e] == w_hi && ranges[2 * e + 1] == w_hi && w_all == w_hi && w_hi >= 0;
         }
+        whole = whole && one;
       }
       f32x16 s[S::KB];
 #pragma unroll
@@ -150,10 +153,18 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi;
-            bool seen = key < see;
-            if (a.kdoc && seen) seen = doc >= 0 && a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn] == doc;
-            s[kb][r] = seen ? s[kb][r] : -INF;
+            s[kb][r] = key < see ? s[kb][r] : -INF;
           }
+        if (!one) {
+          const int* const kd = a.kdoc + b * a.kdoc_sb;
+#pragma unroll
+          for (int kb = 0; kb < S::KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int key = min(key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi, a.M - 1);
+              s[kb][r] = kd[key * a.kdoc_sn] == doc && doc >= 0 ? s[kb][r] : -INF;
+            }
+        }
       }
       float top = s[0][0];
 #pragma unroll
@@ -185,10 +196,19 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
         for (int r = 0; r < 16; ++r) l += s[kb][r];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          F p;
+          F p, low;
           operand(s[kb], st, p);
+          if constexpr (PRECISE) {
 #pragma unroll
-          for (int d = 0; d < L::BLOCKS; ++d) o[d] = mma(L::column(vt, kb * 32 + st * 16, d, lane), p, o[d]);
+            for (int j = 0; j < 8; ++j) s[kb][8 * st + j] -= (float)p[j];
+            operand(s[kb], st, low);
+          }
+#pragma unroll
+          for (int d = 0; d < L::BLOCKS; ++d) {
+            const F v = L::column(vt, kb * 32 + st * 16, d, lane);
+            o[d] = mma(v, p, o[d]);
+            if constexpr (PRECISE) o[d] = mma(v, low, o[d]);
+          }
         }
       }
     }
@@ -278,7 +298,13 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 template <class T, int DP, int MODE, bool DIVIDED>
 static hipError_t forward_one(const Args& a, unsigned grid, hipStream_t stream) {
   typedef Shape<T, DP, DIVIDED> S;
-  gr_attention_kernel<T, DP, MODE, DIVIDED><<<dim3(grid), dim3(S::THREADS), S::LDS, stream>>>(a);
+  if constexpr (sizeof(T) == 2) {
+    if (a.rest.p) {
+      gr_attention_kernel<T, DP, MODE, DIVIDED, true><<<dim3(grid), dim3(S::THREADS), S::LDS, stream>>>(a);
+      return hipGetLastError();
+    }
+  }
+  gr_attention_kernel<T, DP, MODE, DIVIDED, false><<<dim3(grid), dim3(S::THREADS), S::LDS, stream>>>(a);
   return hipGetLastError();
 }
 template <class T, int DP, bool DIVIDED>

@@ -63,6 +63,10 @@ static __device__ __forceinline__ void finished(f32x16 (&x)[N]) {
 
 static __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 static __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+// A value that the compiler takes to be new wherever this stands: what is computed from it is computed there, instead of once before the
+// loop at the price of registers that are full.
+static __device__ __forceinline__ int fresh(int x) { asm volatile("" : "+v"(x)); return x; }
+
 constexpr float INF = __builtin_inff();
 
 // The value of the lane's partner in the other half of the wave.
@@ -138,7 +142,7 @@ struct Tile {
       for (int n = 0; n < N; ++n) {
         const int i = n * THREADS + tid, r = i / CHUNKS, c = (i % CHUNKS) ^ twist(r);
         uint32_t off = (uint32_t)(r * sbytes + c * 16);
-        off = r < valid && c * EACH < D ? off : 0x80000000u;
+        off = (r < valid) & (c * EACH < D) ? off : 0x80000000u;
         // (the statement leaves the scalar condition code alone; wait states: M0, and a base that a vector instruction wrote)
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off), "s"(rsrc), "s"(lds0 + n * THREADS * 16) : "memory", "m0");
       }
@@ -176,6 +180,14 @@ struct Tile {
     return f;
   }
 };
+
+// One wave loads up to 64 neighbouring 4-byte values straight into LDS.
+static __device__ __forceinline__ void load_words(GR_LDS float* to, const void* from, int lane, int count) {
+  const uint64_t b = (uint64_t)from;
+  i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), 0x7fffffff, 0x00027000};
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)to);
+  if (lane < count) asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(lane * 4), "s"(rsrc), "s"(lds) : "memory", "m0");
+}
 
 // Waits for this wave's loads into LDS, then for everybody's.
 static __device__ __forceinline__ void arrive() {

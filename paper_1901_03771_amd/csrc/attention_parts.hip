@@ -1,27 +1,51 @@
-// The small kernels around attention: joining the splits of the keys, document ranges, delta, summing the parts of dk and dv.
+// The small kernels around attention: joining the splits of the keys, document ranges, the gradient's statistics of a row, summing the parts of dk and dv.
 #include "attention_kernels.h"
 
 namespace gr {
 namespace attn {
 
-// out and lse of a row from the splits' (m, l, sums): each scaled to the largest m, added in the order of the splits.  A thread has four
-// values of a row.
+// out and lse of a row from the splits' (m, l, sums): each scaled to the largest m, added in the order of the splits.  A workgroup has one
+// row: its threads read the splits' (m, l) once, a split each, then 256 / quads runs of splits are summed side by side for every four
+// values and joined in order.  (Threads that each walked all splits of four values took 68 us for 128 splits of 8 rows, a chain of 128 reads.)
 template <class T>
 __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a, int dp) {
-  const int quads = dp / 4, R = a.N * a.G, pairs = a.B * a.HK;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)pairs * R;
-  const int64_t row = id / quads;
-  const int d = (int)(id - row * quads) * 4;
-  if (row >= rows) return;
-  float m = -INF, l = 0.0f;
-  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.part_ml[2 * (s * rows + row)]);
+  __shared__ float by_[MAX_SPLITS];
+  __shared__ f32x4 sums[256];
+  __shared__ float tops[4], totals[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quads = dp / 4, R = a.N * a.G, pairs = a.B * a.HK;
+  const int64_t rows = (int64_t)pairs * R, row = blockIdx.x;
+  static_assert(MAX_SPLITS <= 256, "a split per thread");
+  const bool have = tid < a.splits;
+  const float ms = have ? a.part_ml[2 * (tid * rows + row)] : -INF, ls = have ? a.part_ml[2 * (tid * rows + row) + 1] : 0.0f;
+  float m = ms;
+  for (int x = 32; x; x >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x));
+  if (lane == 0) tops[wave] = m;
+  __syncthreads();
+  m = __builtin_fmaxf(__builtin_fmaxf(tops[0], tops[1]), __builtin_fmaxf(tops[2], tops[3]));
+  const float by = ms == -INF ? 0.0f : exp2_(ms - m);
+  if (have) by_[tid] = by;
+  float l = ms == -INF ? 0.0f : ls * by;
+  for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+  if (lane == 0) totals[wave] = l;
+  __syncthreads();
+  l = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+  const int runs = 256 / quads, run = tid / quads, d = (tid - run * quads) * 4;
   f32x4 x = (f32x4)0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = a.part_ml[2 * (s * rows + row)], by = ms == -INF ? 0.0f : exp2_(ms - m);
-    l = __builtin_fmaf(a.part_ml[2 * (s * rows + row) + 1], by, l);
-    const f32x4 p = *(const f32x4*)(a.part_o + (s * rows + row) * dp + d);
-    if (ms != -INF) for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(p[e], by, x[e]);
+  if (run < runs) {
+    const int per = (a.splits + runs - 1) / runs, s1 = min(a.splits, (run + 1) * per);
+    const float* p = a.part_o + row * dp + d;
+#pragma unroll 4
+    for (int s = run * per; s < s1; ++s) {
+      const float w = by_[s];
+      const f32x4 v = *(const f32x4*)(p + (int64_t)s * rows * dp);
+      // (a split that saw nothing: whatever its sums hold counts for nothing)
+      for (int e = 0; e < 4; ++e) x[e] = w == 0.0f ? x[e] : __builtin_fmaf(v[e], w, x[e]);
+    }
+    sums[tid] = x;
   }
+  __syncthreads();
+  if (run != 0) return;
+  for (int u = 1; u < runs; ++u) x += sums[u * quads + tid];
   const int pair = (int)(row / R), r = (int)(row - (int64_t)pair * R), i = r / a.G, g = r - i * a.G, b = pair / a.HK, h = (pair - b * a.HK) * a.G + g;
   const float inv = m == -INF ? 0.0f : 1.0f / l;
   float o[4], y[4];
@@ -31,27 +55,40 @@ __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a,
   if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
 }
 
-// Smallest and largest document number of 32 neighbours: half a wave each.
-__global__ __launch_bounds__(256) void gr_attention_ranges_kernel(const int* docs, int64_t sb, int64_t sn, int B, int N, int* to) {
+// Smallest and largest document number of 32 neighbours, half a wave each; `rows`, if given, gets the numbers themselves side by side, in
+// rows of a multiple of 64.
+__global__ __launch_bounds__(256) void gr_attention_ranges_kernel(const int* docs, int64_t sb, int64_t sn, int B, int N, int* to, int* rows) {
   const int pieces = (N + 31) / 32;
   const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
   if (id >= (int64_t)B * pieces) return;
   const int b = (int)(id / pieces), n = (int)(id - (int64_t)b * pieces) * 32 + (threadIdx.x & 31);
   int lo = n < N ? docs[b * sb + n * sn] : 0x7fffffff, hi = n < N ? lo : -1;
+  if (rows) {
+    const int64_t np = padded_rows(N);
+    rows[b * np + n] = hi;
+    if (n + 32 >= (int64_t)pieces * 32 && n + 32 < np) rows[b * np + n + 32] = -1;   // (an odd number of pieces)
+  }
   for (int m = 16; m; m >>= 1) { lo = min(lo, __shfl_xor(lo, m)); hi = max(hi, __shfl_xor(hi, m)); }
   if ((threadIdx.x & 31) == 0) { to[2 * id] = lo; to[2 * id + 1] = hi; }
 }
 
-// delta = sum over d of dout (out + rest), 16 lanes a row of (batch, query, head).  rest is what the rounding of out to 16 bits lost:
-// with it delta is that of the unrounded output, which matters for queries that see few keys, where dp - delta nearly cancels.
+// less and delta of the gradient, 16 lanes a row of (batch, query, head).  delta = sum over d of dout (out + rest); rest is what the rounding of
+// out to 16 bits lost: with it delta is that of the unrounded output, which matters for queries that see few keys, where dp - delta nearly
+// cancels.  An lse of 2^28 and more is rounded by more than 2^4: it is taken a little larger, so that no probability passes 1 by so much
+// that its lifted value could overflow.
 template <class T>
-__global__ __launch_bounds__(256) void gr_attention_delta_kernel(const Args a, float* to) {
-  const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4, rows = (int64_t)a.B * a.N * a.H;
+__global__ __launch_bounds__(256) void gr_attention_statistics_kernel(const Args a) {
+  const int64_t np = padded_rows(a.N), id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4, rows = a.B * np * a.H;
   if (id >= rows) return;   // (16 lanes leave together)
   const int part = threadIdx.x & 15;
   const int h = (int)(id % a.H);
   const int64_t bn = id / a.H;
-  const int i = (int)(bn % a.N), b = (int)(bn / a.N);
+  const int i = (int)(bn % np), b = (int)(bn / np);
+  const int64_t to = ((int64_t)b * a.H + h) * np + i;
+  if (i >= a.N) {
+    if (part == 0) { a.less[to] = INF; a.delta[to] = 0.0f; }
+    return;
+  }
   const T* o = at<T>(a.out, b, i, h);
   const T* r = a.rest.p ? at<T>(a.rest, b, i, h) : nullptr;
   const T* g = at<T>(a.dout, b, i, h);
@@ -67,7 +104,13 @@ __global__ __launch_bounds__(256) void gr_attention_delta_kernel(const Args a, f
     for (int d = part; d < a.D; d += 16) x = __builtin_fmaf((float)g[d], (float)o[d] + (r ? (float)r[d] : 0.0f), x);
   }
   for (int m = 8; m; m >>= 1) x += __shfl_xor(x, m);
-  if (part == 0) to[((int64_t)b * a.H + h) * a.N + i] = x;
+  if (part != 0) return;
+  const float e = a.lse[((int64_t)b * a.H + h) * a.N + i];
+  float less = e == -INF ? INF : e * LOG2E - LIFT;
+  const float size = __builtin_fabsf(less);
+  if (size >= 0x1p28f && size < INF) less += size * 0x1p-22f;
+  a.less[to] = less;
+  a.delta[to] = x;
 }
 
 // dk and dv from the parts of the splits of the queries, in the order of the splits.
@@ -93,24 +136,24 @@ __global__ __launch_bounds__(256) void gr_attention_sum_parts_kernel(const Args 
 static dim3 blocks_of(int64_t threads) { return dim3((unsigned)((threads + 255) / 256)); }
 
 hipError_t combine(const Args& a, int type, int dp, hipStream_t stream) {
-  const dim3 grid = blocks_of((int64_t)a.B * a.HK * a.N * a.G * (dp / 4));
+  const dim3 grid((unsigned)((int64_t)a.B * a.HK * a.N * a.G));
   if (type == TYPE_BF16) gr_attention_combine_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, dp);
   else gr_attention_combine_kernel<float><<<grid, dim3(256), 0, stream>>>(a, dp);
   return hipGetLastError();
 }
 
 hipError_t ranges(const Args& a, hipStream_t stream) {
-  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.M + 31) / 32) * 32), dim3(256), 0, stream>>>(a.kdoc, a.kdoc_sb, a.kdoc_sn, a.B, a.M, a.kranges);
+  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.M + 31) / 32) * 32), dim3(256), 0, stream>>>(a.kdoc, a.kdoc_sb, a.kdoc_sn, a.B, a.M, a.kranges, nullptr);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.qranges) return e;
-  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.N + 31) / 32) * 32), dim3(256), 0, stream>>>(a.qdoc, a.qdoc_sb, a.qdoc_sn, a.B, a.N, a.qranges);
+  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.N + 31) / 32) * 32), dim3(256), 0, stream>>>(a.qdoc, a.qdoc_sb, a.qdoc_sn, a.B, a.N, a.qranges, a.qdocs);
   return hipGetLastError();
 }
 
-hipError_t delta(const Args& a, int type, float* to, hipStream_t stream) {
-  const dim3 grid = blocks_of((int64_t)a.B * a.N * a.H * 16);
-  if (type == TYPE_BF16) gr_attention_delta_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, to);
-  else gr_attention_delta_kernel<float><<<grid, dim3(256), 0, stream>>>(a, to);
+hipError_t statistics(const Args& a, int type, hipStream_t stream) {
+  const dim3 grid = blocks_of(a.B * padded_rows(a.N) * a.H * 16);
+  if (type == TYPE_BF16) gr_attention_statistics_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a);
+  else gr_attention_statistics_kernel<float><<<grid, dim3(256), 0, stream>>>(a);
   return hipGetLastError();
 }
 
