@@ -320,11 +320,13 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   if (blocks * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0;
+  const size_t kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
   char* ws;
-  TRY(c.space(sums + ml + kr, &ws));
+  TRY(c.space(sums + ml + kr + kd, &ws));
   a.part_o = (float*)ws;
   a.part_ml = (float*)(ws + sums);
   a.kranges = (int*)(ws + sums + ml);
+  a.kdocs = (int*)(ws + sums + ml + kr);
   a.qranges = nullptr;
   if (a.kdoc && a.M > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   const unsigned grid = grid_of((int)pairs, blocks);
@@ -440,16 +442,17 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   if (std::max(qblocks, kblocks * ksplits) * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0, qr = a.kdoc ? rounded((size_t)a.B * ((a.N + 31) / 32) * 8) : 0;
-  const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0;
+  const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0, kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
   const size_t parts = ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0;
   char* ws;
-  TRY(c.space(2 * st + kr + qr + qd + parts, &ws));
+  TRY(c.space(2 * st + kr + qr + qd + kd + parts, &ws));
   a.less = (float*)ws;
   a.delta = (float*)(ws + st);
   a.kranges = (int*)(ws + 2 * st);
   a.qranges = (int*)(ws + 2 * st + kr);
   a.qdocs = (int*)(ws + 2 * st + kr + qr);
-  a.part_o = (float*)(ws + 2 * st + kr + qr + qd);
+  a.kdocs = (int*)(ws + 2 * st + kr + qr + qd);
+  a.part_o = (float*)(ws + 2 * st + kr + qr + qd + kd);
   if (a.kdoc && a.M > 0 && a.N > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   if (a.N > 0) {
     TRY(c.launch("gr_attention_statistics", [&] { return statistics(a, type, c.ctx->stream); }));

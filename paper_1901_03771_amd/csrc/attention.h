@@ -36,7 +36,7 @@ struct Args {
   int64_t qdoc_sb = 0, qdoc_sn = 0, kdoc_sb = 0, kdoc_sn = 0;
   int* kranges = nullptr;        // (B, ceil(M / 32), 2): smallest and largest document number of 32 keys
   int* qranges = nullptr;        // (B, ceil(N / 32), 2), the same of 32 queries
-  int* qdocs = nullptr;          // (B, NP), the documents of the queries side by side, -1 behind the last
+  int *qdocs = nullptr, *kdocs = nullptr;   // (B, NP) and (B, MP), the documents of queries and keys side by side, -1 behind the last
   int64_t position = 0;          // of query 0
   int B = 0, N = 0, M = 0, H = 0, HK = 0, G = 0, D = 0;
   int causal = 0, step = 0;      // step: a query stands at its sequence's last key
@@ -49,7 +49,7 @@ struct Args {
 enum { MODE_CAP = 1, MODE_BIAS = 2 };
 enum { TYPE_F32 = 0, TYPE_BF16 = 1 };
 
-constexpr int64_t padded_rows(int64_t n) { return (n + 63) / 64 * 64; }
+constexpr int64_t padded_rows(int64_t n) { return (n + 127) / 128 * 128; }   // no tile is taller
 
 // Sizes that host and kernels share, for an element of `size` bytes and heads padded to `dp` values.
 constexpr int row_values(int dp) { return dp <= 64 ? 64 : dp <= 128 ? 128 : 256; }                 // of a row in LDS

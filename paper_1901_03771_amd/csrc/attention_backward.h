@@ -18,9 +18,10 @@ namespace attn {
 template <class T, int DP>
 struct ShapeQ {
   static constexpr int THREADS = 256, KEYS = tile_rows(sizeof(T), DP), ROWS = 128, TILE = KEYS * Tile<T, DP>::ROW;
-  static constexpr int LDS = 4 * TILE + 256;
+  static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;   // two stages of k and v, 64 words to exchange, two stages of the keys' documents
   static constexpr int REGS = DP / 16 * 4 * (int)sizeof(T) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
-  static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr bool TIGHT = REGS > 128;   // of registers: addresses within tiles are formed anew for each tile
+  static constexpr int PER_CU = REGS <= 208 && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
 template <class T, int DP, int MODE>
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   const int rb = a.blocks - 1 - place.block;
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
   const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + wave * 32;
-  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
   const int row = wrow0 + col;
   const bool valid = row < R;
   const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
@@ -86,8 +87,9 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   auto load = [&](int t, int stage) {
     const int64_t k0 = (int64_t)t * S::KEYS;
     const int rows = min(S::KEYS, len - (int)k0);
-    L::template load<S::KEYS, 256>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, tid, a.k.direct);
-    L::template load<S::KEYS, 256>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, tid, a.v.direct);
+    L::template load<S::KEYS, 256>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.k.direct);
+    L::template load<S::KEYS, 256>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.v.direct);
+    if (a.kdoc && wave == 0) load_words((GR_LDS float*)(shared + 64 + stage * S::KEYS), a.kdocs + b * padded_rows(a.M) + k0, lane, S::KEYS);
   };
   int t = find.next(0, tiles, lane), stage = 0;
   if (t < tiles) load(t, 0);
@@ -103,14 +105,15 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
       if (key0 >= w_last) break;
       bool whole = key0 + 32 <= w_first, one = true;
       if (ranges) {
-        one = ranges[2 * (key0 / 32)] == w_hi && ranges[2 * (key0 / 32) + 1] == w_hi && w_all == w_hi && w_hi >= 0;
+        one = (scalar(ranges, 2 * (key0 / 32)) == w_hi) & (scalar(ranges, 2 * (key0 / 32) + 1) == w_hi) & (w_all == w_hi) & (w_hi >= 0);
         whole = whole && one;
       }
+      const int tcol = S::TIGHT ? fresh(col) : col, tlane = S::TIGHT ? fresh(lane) : lane;
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
-        s = mma(L::row(kt, kb * 32 + col, st, hi), qf[st], s);
-        dp = mma(L::row(vt, kb * 32 + col, st, hi), df[st], dp);
+        s = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s);
+        dp = mma(L::row(vt, kb * 32 + tcol, st, hi), df[st], dp);
       }
       finished(s, dp);
 #pragma unroll
@@ -133,11 +136,12 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
           s[r] = key < see ? s[r] : 0.0f;
         }
         if (!one) {
-          const int* const kd = a.kdoc + b * a.kdoc_sb;
+          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + kb * 32 + 4 * hi;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = min(key0 + (r & 3) + 8 * (r >> 2) + 4 * hi, a.M - 1);
-            s[r] = kd[key * a.kdoc_sn] == doc && doc >= 0 ? s[r] : 0.0f;
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const i32x4 n = *(const GR_LDS i32x4*)(kd + 8 * r4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[4 * r4 + e] = (n[e] == doc) & (doc >= 0) ? s[4 * r4 + e] : 0.0f;
           }
         }
       }
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
         F f;
         operand(s, st, f);
 #pragma unroll
-        for (int d = 0; d < L::BLOCKS; ++d) o[d] = mma(L::column(kt, kb * 32 + st * 16, d, lane), f, o[d]);
+        for (int d = 0; d < L::BLOCKS; ++d) o[d] = mma(L::column(kt, kb * 32 + st * 16, d, tlane), f, o[d]);
       }
     }
     t = after;
@@ -173,7 +177,7 @@ struct ShapeKV {
   static constexpr int STATS = 4 * ROWS;                     // less, delta and document of every row
   static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
   static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
-  static constexpr int PER_CU = REGS <= 240 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+    static constexpr int PER_CU = REGS <= 240 && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
 template <class T, int DP, int MODE, int WHICH>
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   if (place.block >= a.blocks * a.splits) return;
   const int split = place.block % a.splits, kblock = place.block / a.splits;   // the first keys are seen by the most queries
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
-  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
   const int block0 = kblock * S::KEYS, key0 = block0 + wave * 32, key = key0 + col;
   const bool valid = key < len;
 
@@ -204,9 +208,9 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     const int* kr = a.kranges + (int64_t)b * kpieces * 2;
     for (int e = block0 / 32; e < block0 / 32 + 4 && e < kpieces; ++e) {
       // (numbers below zero belong to no document; a piece of nothing else has no largest)
-      const int l = kr[2 * e] < 0 ? 0 : kr[2 * e], u = kr[2 * e + 1];
+      const int all = scalar(kr, 2 * e), l = all < 0 ? 0 : all, u = scalar(kr, 2 * e + 1);
       if (u >= 0) { lo = min(lo, l); up = max(up, u); }
-      if (e == key0 / 32) { w_one = kr[2 * e] == u && u >= 0; w_doc = u; }
+      if (e == key0 / 32) { w_one = all == u && u >= 0; w_doc = u; }
     }
   }
   const int* const ranges = a.kdoc ? a.qranges + (int64_t)b * qpieces * 2 : nullptr;
@@ -239,20 +243,31 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   // units: tiles of the first head, of the second, ..; a split takes a run of them
   const int64_t units = (int64_t)span * a.G;
   const int u0 = (int)(units * split / a.splits), u1 = (int)(units * (split + 1) / a.splits);
-
-  Finder<S::ROWS / 32> find{ranges, qpieces, lo, up};
-  // the unit at or after u that has something to do
-  auto next = [&](int u) {
-    while (u < u1) {
-      const int g = u / span, t = t0 + (u - g * span), n = find.next(t, tiles, lane);
-      if (n < tiles) return min(u + (n - t), u1);
-      u = (g + 1) * span;
-      find.base = -1;
+  // the first query that sees this lane's key
+  int from = 0x7fffffff;
+  if (valid) {
+    from = 0;
+    if (a.causal && key >= pre) {
+      const int64_t f = (int64_t)key - a.position;
+      from = f < 0 ? 0 : f < a.N ? (int)f : 0x7fffffff;
     }
-    return u1;
+  }
+
+  struct Unit { int u, g, t; };   // running number, head of the group, tile
+  Finder<S::ROWS / 32> find{ranges, qpieces, lo, up};
+  // the unit at or after x that has something to do
+  auto next = [&](Unit x) {
+    while (x.u < u1) {
+      if (x.t >= tiles) { x.t = t0; ++x.g; }
+      const int n = find.next(x.t, tiles, lane);
+      x.u += n - x.t;
+      x.t = n;
+      if (n < tiles) return x;
+    }
+    return x;
   };
-  auto load = [&](int u, int stage) {
-    const int g = u / span, t = t0 + (u - g * span), h = hk * a.G + g;
+  auto load = [&](const Unit& x, int stage) {
+    const int t = x.t, h = hk * a.G + x.g;
     const int64_t i0 = (int64_t)t * S::ROWS;
     const int rows = min(S::ROWS, a.N - (int)i0);
     L::template load<S::ROWS, 256>(smem + 2 * stage * S::TILE, at<T>(a.q, b, i0, h), a.q.sn, rows, a.D, fresh(tid), a.q.direct);
@@ -264,17 +279,21 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     else if (wave == 1) load_words(to + S::ROWS, a.delta + stat, lane, S::ROWS);
     else if (wave == 2 && a.kdoc) load_words(to + 2 * S::ROWS, a.qdocs + b * np + i0, lane, S::ROWS);
   };
-  int u = next(u0), stage = 0;
-  if (u < u1) load(u, 0);
-  while (u < u1) {
-    const int after = next(u + 1);
+  Unit now{u0, span > 0 ? u0 / span : 0, 0};
+  now.t = t0 + (u0 - now.g * span);
+  now = next(now);
+  int stage = 0;
+  if (now.u < u1) load(now, 0);
+  while (now.u < u1) {
+    const Unit after = next({now.u + 1, now.g, now.t + 1});
     arrive();
-    if (after < u1) load(after, stage ^ 1);
-    const int g = u / span, t = t0 + (u - g * span), h = hk * a.G + g;
+    if (after.u < u1) load(after, stage ^ 1);
+    const int t = now.t, h = hk * a.G + now.g;
     const GR_LDS char* const qt = smem + 2 * stage * S::TILE;
     const GR_LDS char* const dt = qt + S::TILE;
     const GR_LDS float* const st = stats + stage * S::STATS;
-    const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
+    const float slope = MODE & MODE_BIAS ? scalar_float(a.slopes, h * a.slopes_s) * LOG2E : 0.0f;
+    const float away = MODE & MODE_BIAS ? (float)(a.position + t * S::ROWS - key) : 0.0f;   // from this lane's key to the tile's first query
 #pragma unroll 1
     for (int rb = 0; rb < S::ROWS / 32; ++rb) {
       const int i0 = t * S::ROWS + rb * 32;
@@ -285,7 +304,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
       // (rows behind the last query need no mask: their lse is none)
       bool whole = keys_seen(a, i0, len, pre) >= key0 + 32, one = true;
       if (ranges) {
-        one = w_one && ranges[2 * (i0 / 32)] == w_doc && ranges[2 * (i0 / 32) + 1] == w_doc;
+        one = w_one & (scalar(ranges, 2 * (i0 / 32)) == w_doc) & (scalar(ranges, 2 * (i0 / 32) + 1) == w_doc);
         whole = whole && one;
       }
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
@@ -300,27 +319,38 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
       for (int r4 = 0; r4 < 4; ++r4) {
         const int rr = rb * 32 + 8 * r4 + 4 * hi;
         const f32x4 less = *(const GR_LDS f32x4*)(st + rr), delta = *(const GR_LDS f32x4*)(st + S::ROWS + rr);
-        const i32x4 docs = one ? (i32x4)0 : *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rr);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * r4 + e;
           float y = s[r], bend = 1.0f;
           if constexpr (MODE & MODE_CAP) { y = capped<T, MODE>(y, a.cin); bend = __builtin_fmaf(-y, y, 1.0f); }
-          float x;
-          if constexpr (MODE & MODE_BIAS) x = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf((float)(a.position + t * S::ROWS + rr + e) - (float)key), -less[e]));
-          else x = __builtin_fmaf(y, a.c, -less[e]);
-          float p = exp2_(x);
-          if (!whole) {
-            bool seen = key < keys_seen(a, t * S::ROWS + rr + e, len, pre);
-            if (!one) seen = seen & (doc >= 0) & (docs[e] == doc);
-            p = seen ? p : 0.0f;
-          }
-          s[r] = p;
+          if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf(away + (float)(rr + e)), -less[e]));
+          else y = __builtin_fmaf(y, a.c, -less[e]);
+          s[r] = exp2_(y);
           if constexpr (WANT_K) {
-            float d = p * (dp[r] - delta[e]);
-            if constexpr (MODE & MODE_CAP) d *= bend;
-            if (!whole) d = p == 0.0f ? 0.0f : d;    // (masked, or too small to count)
-            dp[r] = d;
+            dp[r] = s[r] * (dp[r] - delta[e]);
+            if constexpr (MODE & MODE_CAP) dp[r] *= bend;
+          }
+        }
+      }
+      if (!whole) {
+        const int i = i0 + 4 * hi;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool seen = i + (r & 3) + 8 * (r >> 2) >= from;
+          s[r] = seen ? s[r] : 0.0f;
+          if constexpr (WANT_K) dp[r] = seen ? dp[r] : 0.0f;
+        }
+        if (!one) {
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const i32x4 docs = *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rb * 32 + 8 * r4 + 4 * hi);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool seen = (docs[e] == doc) & (doc >= 0);
+              s[4 * r4 + e] = seen ? s[4 * r4 + e] : 0.0f;
+              if constexpr (WANT_K) dp[4 * r4 + e] = seen ? dp[4 * r4 + e] : 0.0f;
+            }
           }
         }
       }
@@ -339,7 +369,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
         }
       }
     }
-    u = after;
+    now = after;
     stage ^= 1;
   }
   if constexpr (WANT_K) finished(ok);
@@ -386,7 +416,7 @@ static hipError_t grad_kv_part(const Args& a, unsigned grid, hipStream_t stream)
 }
 template <class T, int DP, int MODE>
 static hipError_t grad_kv_one(const Args& a, unsigned grid, hipStream_t stream) {
-  if constexpr (sizeof(T) * DP >= 1024) {
+    if constexpr (sizeof(T) * DP >= 1024) {
     const hipError_t e = grad_kv_part<T, DP, MODE, ONLY_V>(a, grid, stream);
     return e != hipSuccess ? e : grad_kv_part<T, DP, MODE, ONLY_K>(a, grid, stream);
   } else {

@@ -25,11 +25,12 @@ struct Shape {
   static constexpr int KB = DIVIDED ? 1 : KEYS / 32;                              // blocks of 32 keys a wave multiplies
   static constexpr int ROWS = DIVIDED ? 32 : 32 * WAVES;
   static constexpr int TILE = KEYS * Tile<T, DP>::ROW;
-  // two stages of a tile of k and one of v; the joining waves' sums lie over them
-  static constexpr int LDS = 4 * TILE + 256;
+  // two stages of a tile of k and one of v (the joining waves' sums lie over them), 64 words to exchange, two stages of the keys' documents
+  static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;
   static_assert(!DIVIDED || WAVES * 32 * (DP + 4) * 4 <= 4 * TILE, "the waves' sums fit the stages");
   // registers: operands of q, sums, scores.  Two workgroups per compute unit where they fit 256.
   static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) + DP / 2 + 16 * KB;
+  static constexpr bool TIGHT = REGS > 128;   // of registers: addresses within tiles are formed anew for each tile
   static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
@@ -51,7 +52,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   const int split = place.block % a.splits, rb = a.blocks - 1 - place.block / a.splits;
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
   const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + (DIVIDED ? 0 : wave * 32);
-  const int len = length_of(a, b), pre = a.prefix ? a.prefix[b * a.prefix_s] : 0;
+  const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
   const int row = wrow0 + col;
   const bool valid = row < R;
   const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
@@ -105,8 +106,9 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   auto load = [&](int t, int stage) {
     const int64_t k0 = (int64_t)t * S::KEYS;
     const int rows = min(S::KEYS, len - (int)k0);
-    L::template load<S::KEYS, S::THREADS>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, tid, a.k.direct);
-    L::template load<S::KEYS, S::THREADS>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, tid, a.v.direct);
+    L::template load<S::KEYS, S::THREADS>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.k.direct);
+    L::template load<S::KEYS, S::THREADS>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.v.direct);
+    if (a.kdoc && wave * 64 < S::KEYS) load_words((GR_LDS float*)(shared + 64 + stage * S::KEYS + wave * 64), a.kdocs + b * padded_rows(a.M) + k0 + wave * 64, lane, S::KEYS - wave * 64);
   };
   int t = find.next(split * per, t1, lane), stage = 0;
   if (t < t1) load(t, 0);
@@ -123,16 +125,17 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb) {
           const int e = min(key0 / 32 + kb, pieces - 1);
-          one &= ranges[2 * e] == w_hi && ranges[2 * e + 1] == w_hi && w_all == w_hi && w_hi >= 0;
+          one &= (scalar(ranges, 2 * e) == w_hi) & (scalar(ranges, 2 * e + 1) == w_hi) & (w_all == w_hi) & (w_hi >= 0);
         }
         whole = whole && one;
       }
+      const int tcol = S::TIGHT ? fresh(col) : col, tlane = S::TIGHT ? fresh(lane) : lane;
       f32x16 s[S::KB];
 #pragma unroll
       for (int kb = 0; kb < S::KB; ++kb) {
         s[kb] = (f32x16)0.0f;
 #pragma unroll
-        for (int st = 0; st < L::STEPS; ++st) s[kb] = mma(L::row(kt, kb * 32 + col, st, hi), qf[st], s[kb]);
+        for (int st = 0; st < L::STEPS; ++st) s[kb] = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s[kb]);
       }
       if constexpr (S::KB == 2) finished(s[0], s[1]);
       else finished(s[0]);
@@ -156,13 +159,14 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
             s[kb][r] = key < see ? s[kb][r] : -INF;
           }
         if (!one) {
-          const int* const kd = a.kdoc + b * a.kdoc_sb;
+          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + (DIVIDED ? wave * 32 : 0) + 4 * hi;
 #pragma unroll
           for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int key = min(key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi, a.M - 1);
-              s[kb][r] = kd[key * a.kdoc_sn] == doc && doc >= 0 ? s[kb][r] : -INF;
+            for (int r4 = 0; r4 < 4; ++r4) {
+              const i32x4 n = *(const GR_LDS i32x4*)(kd + kb * 32 + 8 * r4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[kb][4 * r4 + e] = (n[e] == doc) & (doc >= 0) ? s[kb][4 * r4 + e] : -INF;
             }
         }
       }
@@ -205,7 +209,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
           }
 #pragma unroll
           for (int d = 0; d < L::BLOCKS; ++d) {
-            const F v = L::column(vt, kb * 32 + st * 16, d, lane);
+            const F v = L::column(vt, kb * 32 + st * 16, d, tlane);
             o[d] = mma(v, p, o[d]);
             if constexpr (PRECISE) o[d] = mma(v, low, o[d]);
           }

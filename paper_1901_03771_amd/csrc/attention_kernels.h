@@ -181,6 +181,12 @@ struct Tile {
   }
 };
 
+// A whole number at an address that is the same for the wave, written before this kernel began: a scalar load.  (A vector load would have to be
+// waited for behind all the tile's loads under way.)
+static __device__ __forceinline__ int scalar(const int* p, int64_t i) { return ((const __attribute__((address_space(4))) int*)p)[i]; }
+
+static __device__ __forceinline__ float scalar_float(const float* p, int64_t i) { return ((const __attribute__((address_space(4))) float*)p)[i]; }
+
 // One wave loads up to 64 neighbouring 4-byte values straight into LDS.
 static __device__ __forceinline__ void load_words(GR_LDS float* to, const void* from, int lane, int count) {
   const uint64_t b = (uint64_t)from;
@@ -231,7 +237,7 @@ static __device__ __forceinline__ int keys_seen(const Args& a, int i, int len, i
 }
 
 static __device__ __forceinline__ int length_of(const Args& a, int b) {
-  const int n = a.lengths ? a.lengths[b * a.lengths_s] : a.M;
+  const int n = a.lengths ? scalar(a.lengths, b * a.lengths_s) : a.M;
   return n < 0 ? 0 : n < a.M ? n : a.M;
 }
 

@@ -55,19 +55,17 @@ __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a,
   if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
 }
 
-// Smallest and largest document number of 32 neighbours, half a wave each; `rows`, if given, gets the numbers themselves side by side, in
-// rows of a multiple of 64.
+// Smallest and largest document number of 32 neighbours, half a wave each; `rows` gets the numbers themselves side by side, in rows of a
+// multiple of 128.
 __global__ __launch_bounds__(256) void gr_attention_ranges_kernel(const int* docs, int64_t sb, int64_t sn, int B, int N, int* to, int* rows) {
   const int pieces = (N + 31) / 32;
   const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
   if (id >= (int64_t)B * pieces) return;
   const int b = (int)(id / pieces), n = (int)(id - (int64_t)b * pieces) * 32 + (threadIdx.x & 31);
   int lo = n < N ? docs[b * sb + n * sn] : 0x7fffffff, hi = n < N ? lo : -1;
-  if (rows) {
-    const int64_t np = padded_rows(N);
-    rows[b * np + n] = hi;
-    if (n + 32 >= (int64_t)pieces * 32 && n + 32 < np) rows[b * np + n + 32] = -1;   // (an odd number of pieces)
-  }
+  const int64_t np = padded_rows(N);
+  rows[b * np + n] = hi;
+  for (int64_t r = n + 32; r >= (int64_t)pieces * 32 && r < np; r += 32) rows[b * np + r] = -1;
   for (int m = 16; m; m >>= 1) { lo = min(lo, __shfl_xor(lo, m)); hi = max(hi, __shfl_xor(hi, m)); }
   if ((threadIdx.x & 31) == 0) { to[2 * id] = lo; to[2 * id + 1] = hi; }
 }
@@ -143,7 +141,7 @@ hipError_t combine(const Args& a, int type, int dp, hipStream_t stream) {
 }
 
 hipError_t ranges(const Args& a, hipStream_t stream) {
-  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.M + 31) / 32) * 32), dim3(256), 0, stream>>>(a.kdoc, a.kdoc_sb, a.kdoc_sn, a.B, a.M, a.kranges, nullptr);
+  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.M + 31) / 32) * 32), dim3(256), 0, stream>>>(a.kdoc, a.kdoc_sb, a.kdoc_sn, a.B, a.M, a.kranges, a.kdocs);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.qranges) return e;
   gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.N + 31) / 32) * 32), dim3(256), 0, stream>>>(a.qdoc, a.qdoc_sb, a.qdoc_sn, a.B, a.N, a.qranges, a.qdocs);
