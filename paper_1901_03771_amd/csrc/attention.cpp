@@ -437,13 +437,18 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   const int64_t rows = (int64_t)a.N * a.G, pairs = (int64_t)a.B * a.HK;
   if (pairs == 0) return GR_OK;
   const int64_t qblocks = (rows + 127) / 128, kblocks = ((int64_t)a.M + 127) / 128;
-  const int qtile = tile_rows(size, dp);
-  const int ksplits = splits_of(pairs * kblocks, (((int64_t)a.N + qtile - 1) / qtile) * a.G, 16);
-  if (std::max(qblocks, kblocks * ksplits) * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
+  const int64_t tile = tile_rows(size, dp);
+  const int qsplits = splits_of(pairs * qblocks, ((int64_t)a.M + tile - 1) / tile, 16);
+  // For dk and dv, where a workgroup walks the queries of G heads, from every place on to the end: more and shorter walks even out what causal
+  // masks and documents leave of them.
+  const int64_t units = (((int64_t)a.N + tile - 1) / tile) * a.G;
+  int ksplits = splits_of(pairs * kblocks, units, 16);
+  if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));
+  if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0, qr = a.kdoc ? rounded((size_t)a.B * ((a.N + 31) / 32) * 8) : 0;
   const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0, kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
-  const size_t parts = ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0;
+  const size_t parts = std::max(ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0, qsplits > 1 ? rounded((size_t)qsplits * pairs * rows * dp * 4) : 0);
   char* ws;
   TRY(c.space(2 * st + kr + qr + qd + kd + parts, &ws));
   a.less = (float*)ws;
@@ -456,17 +461,18 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   if (a.kdoc && a.M > 0 && a.N > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   if (a.N > 0) {
     TRY(c.launch("gr_attention_statistics", [&] { return statistics(a, type, c.ctx->stream); }));
-    a.splits = 1;
+    a.splits = qsplits;
     a.blocks = (int)qblocks;
-    const unsigned grid = grid_of((int)pairs, qblocks);
+    const unsigned grid = grid_of((int)pairs, qblocks * qsplits);
     TRY(c.launch("gr_attention_grad_q", [&] { return type == TYPE_BF16 ? grad_q_bf16(a, dp, mode, grid, c.ctx->stream) : grad_q_f32(a, dp, mode, grid, c.ctx->stream); }));
+    if (qsplits > 1) TRY(c.launch("gr_attention_sum_parts", [&] { return sum_parts(a, type, dp, true, c.ctx->stream); }));
   }
   if (a.M > 0) {
     a.splits = ksplits;
     a.blocks = (int)kblocks;
     const unsigned grid = grid_of((int)pairs, kblocks * ksplits);
     TRY(c.launch("gr_attention_grad_kv", [&] { return type == TYPE_BF16 ? grad_kv_bf16(a, dp, mode, grid, c.ctx->stream) : grad_kv_f32(a, dp, mode, grid, c.ctx->stream); }));
-    if (ksplits > 1) TRY(c.launch("gr_attention_sum_parts", [&] { return sum_parts(a, type, dp, c.ctx->stream); }));
+    if (ksplits > 1) TRY(c.launch("gr_attention_sum_parts", [&] { return sum_parts(a, type, dp, false, c.ctx->stream); }));
   }
   return GR_OK;
 }

@@ -23,7 +23,7 @@ struct Args {
   // of the gradient, (B, H, NP) with NP = N rounded up to whole tiles: less = lse in binary logarithms - LIFT (rows that see nothing, and
   // rows behind the last: +inf), delta = sum over d of dout * out
   float *less = nullptr, *delta = nullptr;
-  float* part_o = nullptr;       // (splits, B * HK, N * G, DP) unnormalised sums of a split's keys, or the parts of dk and dv
+  float* part_o = nullptr;       // (splits, B * HK, N * G, DP) unnormalised sums of a split's keys; parts of dq, or of dk and dv, likewise
   float* part_ml = nullptr;      // (splits, B * HK, N * G, 2) maximum (binary logarithms) and sum
   const float* slopes = nullptr; // (H), stride slopes_s
   int64_t slopes_s = 0;
@@ -40,7 +40,7 @@ struct Args {
   int64_t position = 0;          // of query 0
   int B = 0, N = 0, M = 0, H = 0, HK = 0, G = 0, D = 0;
   int causal = 0, step = 0;      // step: a query stands at its sequence's last key
-  int splits = 1, blocks = 0;    // splits of the keys (of the queries, for dk and dv), blocks of rows (of keys) of a head
+  int splits = 1, blocks = 0;    // splits of the keys (for dk and dv: of the queries), blocks of rows (of keys) of a head
   float scale = 1.0f;
   float c = 0.0f;                // binary logarithm units: scale * log2(e), or cap * log2(e) where scores are capped
   float cin = 0.0f;              // argument of the tanh, in the unit that its form takes
@@ -72,7 +72,7 @@ hipError_t grad_q_f32(const Args& a, int dp, int mode, unsigned grid, hipStream_
 hipError_t grad_q_bf16(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);
 hipError_t grad_kv_f32(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);
 hipError_t grad_kv_bf16(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream);
-hipError_t sum_parts(const Args& a, int type, int dp, hipStream_t stream);
+hipError_t sum_parts(const Args& a, int type, int dp, bool queries, hipStream_t stream);
 
 constexpr int MAX_PAIRS = 256;
 struct Rotary {

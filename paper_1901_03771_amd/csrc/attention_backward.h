@@ -20,7 +20,7 @@ struct ShapeQ {
   static constexpr int THREADS = 256, KEYS = tile_rows(sizeof(T), DP), ROWS = 128, TILE = KEYS * Tile<T, DP>::ROW;
   static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;   // two stages of k and v, 64 words to exchange, two stages of the keys' documents
   static constexpr int REGS = DP / 16 * 4 * (int)sizeof(T) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
-  static constexpr bool TIGHT = REGS > 128;   // of registers: addresses within tiles are formed anew for each tile
+  static constexpr bool TIGHT = REGS > 160;   // of registers: addresses within tiles are formed anew for each tile
   static constexpr int PER_CU = REGS <= 208 && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
@@ -33,9 +33,10 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   GR_LDS char* const smem = (GR_LDS char*)smem_;
   GR_LDS int* const shared = (GR_LDS int*)(smem + 4 * S::TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
-  const Place place = place_of(blockIdx.x, a.B * a.HK, a.blocks);
-  if (place.block >= a.blocks) return;
-  const int rb = a.blocks - 1 - place.block;
+  const int pairs = a.B * a.HK;
+  const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
+  if (place.block >= a.blocks * a.splits) return;
+  const int split = place.block % a.splits, rb = a.blocks - 1 - place.block / a.splits;
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
   const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + wave * 32;
   const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
 #pragma unroll
   for (int d = 0; d < L::BLOCKS; ++d) o[d] = (f32x16)0.0f;
 
-  const int tiles = (end + S::KEYS - 1) / S::KEYS;
+  const int all = (end + S::KEYS - 1) / S::KEYS, per = (all + a.splits - 1) / a.splits, tiles = min(all, (split + 1) * per);
   const T* const kbase = at<T>(a.k, b, 0, hk);
   const T* const vbase = at<T>(a.v, b, 0, hk);
   auto load = [&](int t, int stage) {
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
     L::template load<S::KEYS, 256>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.v.direct);
     if (a.kdoc && wave == 0) load_words((GR_LDS float*)(shared + 64 + stage * S::KEYS), a.kdocs + b * padded_rows(a.M) + k0, lane, S::KEYS);
   };
-  int t = find.next(0, tiles, lane), stage = 0;
+  int t = find.next(split * per, tiles, lane), stage = 0;
   if (t < tiles) load(t, 0);
   while (t < tiles) {
     const int after = find.next(t + 1, tiles, lane);
@@ -158,6 +159,18 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   }
   finished(o);
   if (!valid) return;
+  if (a.splits > 1) {
+    // (splits, B * HK, N * G, DP)
+    float* const to = a.part_o + (((int64_t)split * pairs + place.pair) * R + row) * DP;
+#pragma unroll
+    for (int d = 0; d < L::BLOCKS; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 x = {o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+        *(f32x4*)(to + d * 32 + 2 * r + 4 * hi) = x;
+      }
+    return;
+  }
   T* const dq = at<T>(a.dq, b, i, h);
 #pragma unroll
   for (int d = 0; d < L::BLOCKS; ++d)

@@ -130,6 +130,8 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
         whole = whole && one;
       }
       const int tcol = S::TIGHT ? fresh(col) : col, tlane = S::TIGHT ? fresh(lane) : lane;
+      // (the wave that multiplies goes first: its next product is what the other one's exponentials run beside)
+      __builtin_amdgcn_s_setprio(1);
       f32x16 s[S::KB];
 #pragma unroll
       for (int kb = 0; kb < S::KB; ++kb) {
@@ -137,6 +139,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
         for (int st = 0; st < L::STEPS; ++st) s[kb] = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s[kb]);
       }
+      __builtin_amdgcn_s_setprio(0);
       if constexpr (S::KB == 2) finished(s[0], s[1]);
       else finished(s[0]);
       if constexpr (MODE != 0) {
@@ -184,20 +187,23 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
         for (int d = 0; d < L::BLOCKS; ++d) o[d] *= by;
       }
-      const float less = m == -INF ? 0.0f : m;
+      float less = m == -INF ? 0.0f : m;
       // (scores of 2^20 and more: m is rounded by as much as an exponent counts, so the difference is taken before the product)
-      const bool huge = __any(__builtin_fabsf(less) > 1048576.0f);
+      if (__any(__builtin_fabsf(less) > 1048576.0f)) {
+        const float by = my == -INF ? 0.0f : my;
+        less = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < S::KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] -= by;
+      }
 #pragma unroll
       for (int kb = 0; kb < S::KB; ++kb) {
-        if (huge) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = exp2_((s[kb][r] - (my == -INF ? 0.0f : my)) * c);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = exp2_(__builtin_fmaf(s[kb][r], c, -less));
+        for (int r = 0; r < 16; ++r) {
+          s[kb][r] = exp2_(__builtin_fmaf(s[kb][r], c, -less));
+          l += s[kb][r];
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) l += s[kb][r];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
           F p, low;

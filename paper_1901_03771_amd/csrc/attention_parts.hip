@@ -111,24 +111,34 @@ __global__ __launch_bounds__(256) void gr_attention_statistics_kernel(const Args
   a.delta[to] = x;
 }
 
-// dk and dv from the parts of the splits of the queries, in the order of the splits.
-template <class T>
+// dq (WHICH = 0), or dk and dv (1), from the parts of the splits, in the order of the splits.  A thread has four values of a row.
+template <class T, int WHICH>
 __global__ __launch_bounds__(256) void gr_attention_sum_parts_kernel(const Args a, int dp) {
-  const int quads = dp / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.B * a.HK * a.M, plane = rows * dp;
+  const int quads = dp / 4, each = WHICH == 0 ? a.N * a.G : a.M;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.B * a.HK * each, plane = rows * dp;
   const int64_t row = id / quads;
   const int d = (int)(id - row * quads) * 4;
   if (row >= rows) return;
-  f32x4 k = (f32x4)0.0f, v = (f32x4)0.0f;
-  for (int s = 0; s < a.splits; ++s) {
-    k += *(const f32x4*)(a.part_o + 2 * s * plane + row * dp + d);
-    v += *(const f32x4*)(a.part_o + (2 * s + 1) * plane + row * dp + d);
+  const float* const p = a.part_o + row * dp + d;
+  const float by = a.scale * UNLIFT;
+  const int64_t pair = row / each, n = row - pair * each, b = pair / a.HK, hk = pair - b * a.HK;
+  f32x4 x = (f32x4)0.0f, y = (f32x4)0.0f;
+  if constexpr (WHICH == 0) {
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) x += *(const f32x4*)(p + s * plane);
+    const float q[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    const int64_t i = n / a.G;
+    store4(at<T>(a.dq, b, i, hk * a.G + (n - i * a.G)), d, a.D, q, a.dq.aligned);
+  } else {
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+      x += *(const f32x4*)(p + 2 * s * plane);
+      y += *(const f32x4*)(p + (2 * s + 1) * plane);
+    }
+    const float k[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by}, v[4] = {y[0] * UNLIFT, y[1] * UNLIFT, y[2] * UNLIFT, y[3] * UNLIFT};
+    store4(at<T>(a.dk, b, n, hk), d, a.D, k, a.dk.aligned);
+    store4(at<T>(a.dv, b, n, hk), d, a.D, v, a.dv.aligned);
   }
-  const int64_t pair = row / a.M;
-  const int64_t key = row - pair * a.M, b = pair / a.HK, hk = pair - b * a.HK;
-  const float by = a.scale * UNLIFT, x[4] = {k[0] * by, k[1] * by, k[2] * by, k[3] * by}, y[4] = {v[0] * UNLIFT, v[1] * UNLIFT, v[2] * UNLIFT, v[3] * UNLIFT};
-  store4(at<T>(a.dk, b, key, hk), d, a.D, x, a.dk.aligned);
-  store4(at<T>(a.dv, b, key, hk), d, a.D, y, a.dv.aligned);
 }
 
 static dim3 blocks_of(int64_t threads) { return dim3((unsigned)((threads + 255) / 256)); }
@@ -155,10 +165,15 @@ hipError_t statistics(const Args& a, int type, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t sum_parts(const Args& a, int type, int dp, hipStream_t stream) {
-  const dim3 grid = blocks_of((int64_t)a.B * a.HK * a.M * (dp / 4));
-  if (type == TYPE_BF16) gr_attention_sum_parts_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, dp);
-  else gr_attention_sum_parts_kernel<float><<<grid, dim3(256), 0, stream>>>(a, dp);
+hipError_t sum_parts(const Args& a, int type, int dp, bool queries, hipStream_t stream) {
+  const dim3 grid = blocks_of((int64_t)a.B * a.HK * (queries ? (int64_t)a.N * a.G : a.M) * (dp / 4));
+  if (type == TYPE_BF16) {
+    if (queries) gr_attention_sum_parts_kernel<__bf16, 0><<<grid, dim3(256), 0, stream>>>(a, dp);
+    else gr_attention_sum_parts_kernel<__bf16, 1><<<grid, dim3(256), 0, stream>>>(a, dp);
+  } else {
+    if (queries) gr_attention_sum_parts_kernel<float, 0><<<grid, dim3(256), 0, stream>>>(a, dp);
+    else gr_attention_sum_parts_kernel<float, 1><<<grid, dim3(256), 0, stream>>>(a, dp);
+  }
   return hipGetLastError();
 }
 
