@@ -17,7 +17,7 @@
 namespace gr {
 namespace attn {
 
-constexpr int64_t LIMIT = (int64_t(1) << 31) - 512;   // rows of queries of one head of k, and keys
+constexpr int64_t LIMIT = (int64_t(1) << 30) - 512;   // rows of queries of one head of k, and keys
 
 struct Call {
   gr_ctx* ctx;
@@ -142,11 +142,11 @@ struct Call {
     if (n->shape[r - 1] > 1 && v.strides[r - 1] != 1) return error(GR_ERR_UNSUPPORTED, std::string(what) + ": the values of a row are not neighbours");
     t->p = v.data;
     t->sb = step(0);
-    t->sn = r == 4 ? step(1) : 0;
+    t->sn = r == 4 ? (n->shape[1] > 1 ? v.strides[1] : (n->shape[r - 1] + each - 1) / each * each) : 0;   // (a single row: any step)
     t->sh = step(r - 2);
     const int64_t D = n->shape[r - 1], rows = 128;
     t->aligned = (uintptr_t)v.data % 16 == 0 && t->sb % each == 0 && t->sn % each == 0 && t->sh % each == 0 && D % each == 0;
-    t->direct = t->aligned && t->sn >= 0 && t->sn < (int64_t(1) << 30) && (t->sn * rows + D) * size < (int64_t(1) << 31) - 64;
+    t->direct = t->aligned && t->sn >= D && t->sn < (int64_t(1) << 30) && (t->sn * rows + D) * size < (int64_t(1) << 31) - 64;
     return GR_OK;
   }
 
@@ -254,7 +254,7 @@ static gr_status extents(Call& c, gr_array q, gr_array k, int rank, int* type, A
   const int64_t B = x->shape[0], N = rank == 4 ? x->shape[1] : 1, H = x->shape[rank - 2], D = x->shape[rank - 1], M = y->shape[1], HK = y->shape[2];
   if (D < 1 || D > 256) return c.error(GR_ERR_UNSUPPORTED, "heads have 1 to 256 values");
   if (HK < 1 || H < 1 || H % HK) return c.error(GR_ERR_SHAPE, "the heads of q are not a multiple of those of k");
-  if (B > LIMIT || H > LIMIT || M > LIMIT || N > LIMIT || N * (H / HK) > LIMIT || B * HK > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^31 rows");
+  if (B > LIMIT || H > LIMIT || M > LIMIT || N > LIMIT || N * (H / HK) > LIMIT || B * HK > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^30 rows");
   *type = x->dtype == GR_BF16 ? TYPE_BF16 : TYPE_F32;
   a->B = (int)B; a->N = (int)N; a->H = (int)H; a->D = (int)D; a->M = (int)M; a->HK = (int)HK; a->G = (int)(H / HK);
   return GR_OK;
@@ -287,6 +287,7 @@ static int fill_scores(Call& c, const gr_scores* s, int type, Args* a) {
   a->qdoc = c.whole(s->q_documents, &a->qdoc_sb, &a->qdoc_sn);
   a->kdoc = c.whole(s->k_documents, &a->kdoc_sb, &a->kdoc_sn);
   a->position = s->position;
+  a->place = (int)std::max<int64_t>(-(int64_t(1) << 30), std::min<int64_t>(s->position, int64_t(1) << 30));
   a->causal = s->causal;
   const double log2e = 1.4426950408889634;
   a->scale = (float)s->scale;
@@ -317,7 +318,7 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   a.blocks = (int)((rows + (divided ? 31 : 127)) / (divided ? 32 : 128));
   a.splits = splits_of(pairs * a.blocks, ((int64_t)a.M + keys - 1) / keys, MAX_SPLITS);
   const int64_t blocks = (int64_t)a.blocks * a.splits;
-  if (blocks * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
+  if (blocks * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0;
   const size_t kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
@@ -444,7 +445,7 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   const int64_t units = (((int64_t)a.N + tile - 1) / tile) * a.G;
   int ksplits = splits_of(pairs * kblocks, units, 16);
   if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));
-  if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 8) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
+  if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
   const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0, qr = a.kdoc ? rounded((size_t)a.B * ((a.N + 31) / 32) * 8) : 0;
   const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0, kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
@@ -493,7 +494,7 @@ static gr_status rotary_call(gr_ctx* ctx, gr_array x, gr_array positions, int64_
   if (!std::isfinite(factor)) return c.error(GR_ERR_ARG, "factor must be finite");
   if (position < -(int64_t(1) << 40) || position > (int64_t(1) << 40)) return c.error(GR_ERR_ARG, "position beyond 2^40");
   for (int i = 0; i < pairs; ++i) if (!std::isfinite(frequencies[i])) return c.error(GR_ERR_ARG, "a frequency is not finite");
-  if (B > LIMIT || N > LIMIT || D > LIMIT || B * N > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^31 tokens or values of a head");
+  if (B > LIMIT || N > LIMIT || D > LIMIT || B * N > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^30 tokens or values of a head");
   TRY(c.take(x, "x", dt, {B, N, H, D}, false));
   if (positions) TRY(c.take(positions, "positions", GR_I32, {B, N}, false));
   TRY(c.take(out, "out", dt, {B, N, H, D}, true));
@@ -509,7 +510,7 @@ static gr_status rotary_call(gr_ctx* ctx, gr_array x, gr_array positions, int64_
   r.factor = (float)factor;
   for (int i = 0; i < pairs; ++i) r.turns[i] = frequencies[i] * 0.15915494309189535;   // 1 / (2 pi)
   if (B * N * H * D == 0) return GR_OK;
-  if (H > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^31 heads");
+  if (H > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^30 heads");
   r.H = (int)H;
   // Tokens of a workgroup: enough vectors for its 256 threads, and no more than 32 KiB of sines; for few tokens fewer, and runs of heads.
   const int64_t vectors = std::max<int64_t>(1, D * (int64_t)itemsize((gr_dtype)dt) / 32), tokens = B * N;

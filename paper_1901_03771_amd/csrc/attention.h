@@ -14,7 +14,7 @@ struct Tensor {
   void* p = nullptr;
   int64_t sb = 0, sn = 0, sh = 0;
   int aligned = 0;  // address and strides are multiples of 16 bytes, and so are d elements: whole vectors
-  int direct = 0;   // ... and a tile's rows lie within 2^31 bytes going up: buffer loads straight into LDS
+  int direct = 0;   // ... and rows follow one another without overlap, those of a tile within 2^31 bytes: buffer loads straight into LDS
 };
 
 struct Args {
@@ -38,6 +38,7 @@ struct Args {
   int* qranges = nullptr;        // (B, ceil(N / 32), 2), the same of 32 queries
   int *qdocs = nullptr, *kdocs = nullptr;   // (B, NP) and (B, MP), the documents of queries and keys side by side, -1 behind the last
   int64_t position = 0;          // of query 0
+  int place = 0;                 // the same within 2^30 of key 0: all that masks can tell (N and M are smaller)
   int B = 0, N = 0, M = 0, H = 0, HK = 0, G = 0, D = 0;
   int causal = 0, step = 0;      // step: a query stands at its sequence's last key
   int splits = 1, blocks = 0;    // splits of the keys (for dk and dv: of the queries), blocks of rows (of keys) of a head

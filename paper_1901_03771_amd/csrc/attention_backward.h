@@ -190,7 +190,7 @@ struct ShapeKV {
   static constexpr int STATS = 4 * ROWS;                     // less, delta and document of every row
   static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
   static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
-    static constexpr int PER_CU = REGS <= 240 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+    static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 240 : 200) && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
 template <class T, int DP, int MODE, int WHICH>
@@ -212,11 +212,10 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   const int block0 = kblock * S::KEYS, key0 = block0 + wave * 32, key = key0 + col;
   const bool valid = key < len;
 
-  int doc = -1, lo = 0, up = 0, w_doc = -1;
+  int lo = 0, up = 0, w_doc = -1;
   bool w_one = false;
   const int kpieces = (a.M + 31) / 32, qpieces = (a.N + 31) / 32;
   if (a.kdoc) {
-    if (valid) doc = a.kdoc[b * a.kdoc_sb + key * a.kdoc_sn];
     lo = 0x7fffffff; up = -1;
     const int* kr = a.kranges + (int64_t)b * kpieces * 2;
     for (int e = block0 / 32; e < block0 / 32 + 4 && e < kpieces; ++e) {
@@ -248,24 +247,11 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   // The queries that see a key of the block: all from the first one that does, since what a query sees grows with its place.
   int first = 0;
   if (block0 >= len) first = a.N;
-  else if (a.causal && block0 >= pre) {
-    const int64_t f = (int64_t)block0 - a.position;
-    first = f < 0 ? 0 : f < a.N ? (int)f : a.N;
-  }
+  else if (a.causal && block0 >= pre) first = min(first_seeing(a, block0), a.N);
   const int t0 = first / S::ROWS, tiles = (a.N + S::ROWS - 1) / S::ROWS, span = first < a.N ? tiles - t0 : 0;
   // units: tiles of the first head, of the second, ..; a split takes a run of them
   const int64_t units = (int64_t)span * a.G;
   const int u0 = (int)(units * split / a.splits), u1 = (int)(units * (split + 1) / a.splits);
-  // the first query that sees this lane's key
-  int from = 0x7fffffff;
-  if (valid) {
-    from = 0;
-    if (a.causal && key >= pre) {
-      const int64_t f = (int64_t)key - a.position;
-      from = f < 0 ? 0 : f < a.N ? (int)f : 0x7fffffff;
-    }
-  }
-
   struct Unit { int u, g, t; };   // running number, head of the group, tile
   Finder<S::ROWS / 32> find{ranges, qpieces, lo, up};
   // the unit at or after x that has something to do
@@ -306,14 +292,17 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     const GR_LDS char* const dt = qt + S::TILE;
     const GR_LDS float* const st = stats + stage * S::STATS;
     const float slope = MODE & MODE_BIAS ? scalar_float(a.slopes, h * a.slopes_s) * LOG2E : 0.0f;
-    const float away = MODE & MODE_BIAS ? (float)(a.position + t * S::ROWS - key) : 0.0f;   // from this lane's key to the tile's first query
+    
 #pragma unroll 1
     for (int rb = 0; rb < S::ROWS / 32; ++rb) {
       const int i0 = t * S::ROWS + rb * 32;
       if (i0 >= a.N) break;
       const int see_last = keys_seen(a, min(i0 + 31, a.N - 1), len, pre);
       if (see_last <= key0) continue;
-      const int fcol = fresh(col), flane = fresh(lane);
+      // from this lane's key to the tile's first query
+      const float away = MODE & MODE_BIAS ? (float)(a.position + t * S::ROWS - key0 - (fresh(tid) & 31)) : 0.0f;
+      // (registers are full: what depends on the lane is formed here)
+      const int flane = fresh(tid) & 63, fcol = flane & 31, fhi = flane >> 5;
       // (rows behind the last query need no mask: their lse is none)
       bool whole = keys_seen(a, i0, len, pre) >= key0 + 32, one = true;
       if (ranges) {
@@ -323,14 +312,14 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int x = 0; x < L::STEPS; ++x) {
-        s = mma(L::row(qt, rb * 32 + fcol, x, hi), kf[x], s);
-        if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + fcol, x, hi), vf[x], dp);
+        s = mma(L::row(qt, rb * 32 + fcol, x, fhi), kf[x], s);
+        if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + fcol, x, fhi), vf[x], dp);
       }
       if constexpr (WANT_K) finished(s, dp);
       else finished(s);
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
-        const int rr = rb * 32 + 8 * r4 + 4 * hi;
+        const int rr = rb * 32 + 8 * r4 + 4 * fhi;
         const f32x4 less = *(const GR_LDS f32x4*)(st + rr), delta = *(const GR_LDS f32x4*)(st + S::ROWS + rr);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -347,7 +336,10 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
         }
       }
       if (!whole) {
-        const int i = i0 + 4 * hi;
+        // the first query that sees this lane's key
+        const int key = key0 + fcol, i = i0 + 4 * fhi;
+        int from = a.causal && key >= pre ? first_seeing(a, key) : 0;
+        from = key < len ? from : 0x7fffffff;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool seen = i + (r & 3) + 8 * (r >> 2) >= from;
@@ -355,9 +347,10 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
           if constexpr (WANT_K) dp[r] = seen ? dp[r] : 0.0f;
         }
         if (!one) {
+          const int doc = key < a.M ? a.kdocs[b * padded_rows(a.M) + key] : -1;
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
-            const i32x4 docs = *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rb * 32 + 8 * r4 + 4 * hi);
+            const i32x4 docs = *(const GR_LDS i32x4*)(st + 2 * S::ROWS + rb * 32 + 8 * r4 + 4 * fhi);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const bool seen = (docs[e] == doc) & (doc >= 0);
@@ -387,15 +380,16 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   }
   if constexpr (WANT_K) finished(ok);
   if constexpr (WANT_V) finished(ov);
-  if (key >= a.M) return;
+  const int lane_ = fresh(tid) & 63, key_ = key0 + (lane_ & 31), hi_ = lane_ >> 5;
+  if (key_ >= a.M) return;
   if (a.splits > 1) {
     // (splits, 2, B * HK, M, DP)
-    const int64_t plane = (int64_t)pairs * a.M * DP, to = ((int64_t)place.pair * a.M + key) * DP + 2 * split * plane;
+    const int64_t plane = (int64_t)pairs * a.M * DP, to = ((int64_t)place.pair * a.M + key_) * DP + 2 * split * plane;
 #pragma unroll
     for (int d = 0; d < L::BLOCKS; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int n = d * 32 + 2 * r + 4 * hi;
+        const int n = d * 32 + 2 * r + 4 * hi_;
         if constexpr (WANT_K) { const f32x4 x = {ok[d][r], ok[d][r + 1], ok[d][r + 2], ok[d][r + 3]}; *(f32x4*)(a.part_o + to + n) = x; }
         if constexpr (WANT_V) { const f32x4 x = {ov[d][r], ov[d][r + 1], ov[d][r + 2], ov[d][r + 3]}; *(f32x4*)(a.part_o + plane + to + n) = x; }
       }
@@ -405,14 +399,14 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   for (int d = 0; d < L::BLOCKS; ++d)
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
-      const int n = d * 32 + 2 * r + 4 * hi;
+      const int n = d * 32 + 2 * r + 4 * hi_;
       if constexpr (WANT_K) {
         const float by = a.scale * UNLIFT, x[4] = {ok[d][r] * by, ok[d][r + 1] * by, ok[d][r + 2] * by, ok[d][r + 3] * by};
-        store4(at<T>(a.dk, b, key, hk), n, a.D, x, a.dk.aligned);
+        store4(at<T>(a.dk, b, key_, hk), n, a.D, x, a.dk.aligned);
       }
       if constexpr (WANT_V) {
         const float x[4] = {ov[d][r] * UNLIFT, ov[d][r + 1] * UNLIFT, ov[d][r + 2] * UNLIFT, ov[d][r + 3] * UNLIFT};
-        store4(at<T>(a.dv, b, key, hk), n, a.D, x, a.dv.aligned);
+        store4(at<T>(a.dv, b, key_, hk), n, a.D, x, a.dv.aligned);
       }
     }
 }
@@ -429,7 +423,7 @@ static hipError_t grad_kv_part(const Args& a, unsigned grid, hipStream_t stream)
 }
 template <class T, int DP, int MODE>
 static hipError_t grad_kv_one(const Args& a, unsigned grid, hipStream_t stream) {
-    if constexpr (sizeof(T) * DP >= 1024) {
+    if constexpr (DP == 256) {
     const hipError_t e = grad_kv_part<T, DP, MODE, ONLY_V>(a, grid, stream);
     return e != hipSuccess ? e : grad_kv_part<T, DP, MODE, ONLY_K>(a, grid, stream);
   } else {

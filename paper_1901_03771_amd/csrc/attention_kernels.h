@@ -134,15 +134,23 @@ struct Tile {
     constexpr int N = ROWS * CHUNKS / THREADS;
     static_assert(N * THREADS == ROWS * CHUNKS, "whole chunks for every thread");
     if (direct) {
+      // (the buffer ends with its last valid row: rows do not overlap, see Tensor::direct)
       const uint64_t b = (uint64_t)base;
-      i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), 0x7fffffff, 0x00027000};
       const int sbytes = (int)stride * (int)sizeof(T);
+      const int bytes = valid > 0 ? (valid - 1) * sbytes + D * (int)sizeof(T) : 0;
+      i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), __builtin_amdgcn_readfirstlane(bytes), 0x00027000};
       const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile + (tid & ~63) * 16);
+      // a thread's chunks are STEP rows apart; the twist comes back after 16 rows
+      constexpr int STEP = THREADS / CHUNKS, PERIOD = STEP >= 16 ? 1 : 16 / STEP;
+      uint32_t first[PERIOD];
+#pragma unroll
+      for (int n = 0; n < PERIOD && n < N; ++n) {
+        const int r = n * STEP + tid / CHUNKS, c = (tid % CHUNKS) ^ twist(r);
+        first[n] = c * EACH < D ? (uint32_t)(r * sbytes + c * 16) : 0x80000000u;
+      }
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const int i = n * THREADS + tid, r = i / CHUNKS, c = (i % CHUNKS) ^ twist(r);
-        uint32_t off = (uint32_t)(r * sbytes + c * 16);
-        off = (r < valid) & (c * EACH < D) ? off : 0x80000000u;
+        const uint32_t off = first[n % PERIOD] + (uint32_t)(n / PERIOD * PERIOD * STEP * sbytes);
         // (the statement leaves the scalar condition code alone; wait states: M0, and a base that a vector instruction wrote)
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off), "s"(rsrc), "s"(lds0 + n * THREADS * 16) : "memory", "m0");
       }
@@ -232,8 +240,13 @@ static __device__ __forceinline__ float capped(float s, float cin) {
 // How many keys a query sees at most: its causal part, the prefix and the length are beginnings of the row of keys.
 static __device__ __forceinline__ int keys_seen(const Args& a, int i, int len, int pre) {
   if (!a.causal) return len;
-  const int64_t own = a.position + i + 1, most = own > pre ? own : pre;
-  return most < 0 ? 0 : most < len ? (int)most : len;
+  return min(max(max(a.place + i + 1, pre), 0), len);
+}
+
+// The first query whose causal part holds `key`; 2^31 - 1 if none does.
+static __device__ __forceinline__ int first_seeing(const Args& a, int key) {
+  const int f = max(key - a.place, 0);
+  return f < a.N ? f : 0x7fffffff;
 }
 
 static __device__ __forceinline__ int length_of(const Args& a, int b) {
