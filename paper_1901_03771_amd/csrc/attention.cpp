@@ -309,6 +309,14 @@ static int splits_of(int64_t groups, int64_t tiles, int most) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / groups, tiles / 2), most));
 }
 
+// The same for calls of at most 32 rows per head, which read k and v at the rate of the memory: four workgroups per compute unit, which fit it
+// together (32 sequences on 8 heads: 1, 2, 4, 8, 16 splits take 260, 177, 173, 179, 190 us; one sequence of 65537 keys on one head: 64, 128, 256
+// take 31, 22, 20), but none for a walk of 8 tiles, which is over before the parts would be joined (4 sequences of 512 keys on 16 heads: 16.6 us, 20 with 2).
+static int token_splits_of(int64_t groups, int64_t tiles) {
+  if (tiles <= 8 || groups < 1) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((1024 + groups - 1) / groups, tiles / 2), MAX_SPLITS));
+}
+
 static gr_status forward(Call& c, Args& a, int type, int mode) {
   const int size = type == TYPE_BF16 ? 2 : 4, dp = padded(a.D);
   const int64_t rows = (int64_t)a.N * a.G, pairs = (int64_t)a.B * a.HK;
@@ -316,7 +324,8 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   const bool divided = rows <= 32;
   const int keys = keys_of(divided, size, dp);
   a.blocks = (int)((rows + (divided ? 31 : 127)) / (divided ? 32 : 128));
-  a.splits = splits_of(pairs * a.blocks, ((int64_t)a.M + keys - 1) / keys, MAX_SPLITS);
+  const int64_t tiles = ((int64_t)a.M + keys - 1) / keys;
+  a.splits = divided ? token_splits_of(pairs * a.blocks, tiles) : splits_of(pairs * a.blocks, tiles, MAX_SPLITS);
   const int64_t blocks = (int64_t)a.blocks * a.splits;
   if (blocks * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;

@@ -55,8 +55,11 @@ constexpr int64_t padded_rows(int64_t n) { return (n + 127) / 128 * 128; }   // 
 // Sizes that host and kernels share, for an element of `size` bytes and heads padded to `dp` values.
 constexpr int row_values(int dp) { return dp <= 64 ? 64 : dp <= 128 ? 128 : 256; }                 // of a row in LDS
 constexpr int tile_rows(int size, int dp) { return size * row_values(dp) <= 256 ? 64 : 32; }       // of a tile that waves share
-constexpr int MAX_SPLITS = 128;
-constexpr int shared_waves(int size, int dp) { return size * row_values(dp) <= 256 ? 4 : size * row_values(dp) <= 512 ? 2 : 1; }  // that divide a tile's keys
+constexpr int MAX_SPLITS = 256;
+// Waves that divide a tile's keys.  bfloat16: tiles of 16 KiB, so that two workgroups and more fit a compute unit and one's loads are under way
+// while another multiplies (32 sequences of 4096 to 8192 keys, 128 values: 200 us with one workgroup of four waves per compute unit, 172 so).  float32,
+// where the matrix cores are the bound: 32 KiB, for fewer parts to join (65537 keys, 64 values: 23 and 20 us).
+constexpr int shared_waves(int size, int dp) { return (size == 2 ? 16384 : 32768) / (32 * size * row_values(dp)) > 4 ? 4 : (size == 2 ? 16384 : 32768) / (32 * size * row_values(dp)); }
 
 // Workgroups that place_of (attention_kernels.h) deals `blocks` of each of `pairs` heads to.
 static inline unsigned grid_of(int pairs, int64_t blocks) {
