@@ -317,6 +317,25 @@ static int token_splits_of(int64_t groups, int64_t tiles) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((1024 + groups - 1) / groups, tiles / 2), MAX_SPLITS));
 }
 
+// What ranges() prepares of the documents.
+struct Documents {
+  size_t kr = 0, qr = 0, kd = 0, qd = 0, bytes = 0;
+  explicit Documents(const Args& a) {
+    if (!a.kdoc) return;
+    kr = rounded((size_t)a.B * ((a.M + 31) / 32) * 8);
+    qr = rounded((size_t)a.B * ((a.N + 31) / 32) * 8);
+    kd = rounded((size_t)a.B * padded_rows(a.M) * 4);
+    qd = rounded((size_t)a.B * padded_rows(a.N) * 4);
+    bytes = kr + qr + kd + qd;
+  }
+  void place(Args* a, char* at) const {
+    a->kranges = (int*)at;
+    a->qranges = (int*)(at + kr);
+    a->kdocs = (int*)(at + kr + qr);
+    a->qdocs = (int*)(at + kr + qr + kd);
+  }
+};
+
 static gr_status forward(Call& c, Args& a, int type, int mode) {
   const int size = type == TYPE_BF16 ? 2 : 4, dp = padded(a.D);
   const int64_t rows = (int64_t)a.N * a.G, pairs = (int64_t)a.B * a.HK;
@@ -329,15 +348,12 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   const int64_t blocks = (int64_t)a.blocks * a.splits;
   if (blocks * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
-  const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0;
-  const size_t kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
+  Documents docs(a);
   char* ws;
-  TRY(c.space(sums + ml + kr + kd, &ws));
+  TRY(c.space(sums + ml + docs.bytes, &ws));
   a.part_o = (float*)ws;
   a.part_ml = (float*)(ws + sums);
-  a.kranges = (int*)(ws + sums + ml);
-  a.kdocs = (int*)(ws + sums + ml + kr);
-  a.qranges = nullptr;
+  docs.place(&a, ws + sums + ml);
   if (a.kdoc && a.M > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   const unsigned grid = grid_of((int)pairs, blocks);
   TRY(c.launch(a.step ? "gr_attention_step" : "gr_attention", [&] {
@@ -456,18 +472,14 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));
   if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
-  const size_t kr = a.kdoc ? rounded((size_t)a.B * ((a.M + 31) / 32) * 8) : 0, qr = a.kdoc ? rounded((size_t)a.B * ((a.N + 31) / 32) * 8) : 0;
-  const size_t qd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.N) * 4) : 0, kd = a.kdoc ? rounded((size_t)a.B * padded_rows(a.M) * 4) : 0;
+  Documents docs(a);
   const size_t parts = std::max(ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0, qsplits > 1 ? rounded((size_t)qsplits * pairs * rows * dp * 4) : 0);
   char* ws;
-  TRY(c.space(2 * st + kr + qr + qd + kd + parts, &ws));
+  TRY(c.space(2 * st + docs.bytes + parts, &ws));
   a.less = (float*)ws;
   a.delta = (float*)(ws + st);
-  a.kranges = (int*)(ws + 2 * st);
-  a.qranges = (int*)(ws + 2 * st + kr);
-  a.qdocs = (int*)(ws + 2 * st + kr + qr);
-  a.kdocs = (int*)(ws + 2 * st + kr + qr + qd);
-  a.part_o = (float*)(ws + 2 * st + kr + qr + qd + kd);
+  docs.place(&a, ws + 2 * st);
+  a.part_o = (float*)(ws + 2 * st + docs.bytes);
   if (a.kdoc && a.M > 0 && a.N > 0) TRY(c.launch("gr_attention_ranges", [&] { return ranges(a, c.ctx->stream); }));
   if (a.N > 0) {
     TRY(c.launch("gr_attention_statistics", [&] { return statistics(a, type, c.ctx->stream); }));

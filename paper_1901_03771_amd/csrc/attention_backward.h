@@ -48,23 +48,18 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   const int end = keys_seen(a, i_last, len, pre);
   const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
   const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
-  int doc = -1, w_lo = 0x7fffffff, w_hi = -1, w_all = 0x7fffffff, lo = 0, up = 0;
+  // documents: this lane's, and what the pieces of the wave's and the workgroup's queries hold
+  int doc = -1;
+  Span w = {0, 0, true}, all = {0, 0, true};
   if (a.kdoc) {
+    const int* const qr = a.qranges + (int64_t)b * ((a.N + 31) / 32) * 2;
     if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
-    w_lo = doc >= 0 ? doc : 0x7fffffff; w_hi = doc; w_all = valid ? doc : 0x7fffffff;
-    for (int m = 16; m; m >>= 1) {
-      w_lo = min(w_lo, __shfl_xor(w_lo, m)); w_hi = max(w_hi, __shfl_xor(w_hi, m)); w_all = min(w_all, __shfl_xor(w_all, m));
-    }
-    w_lo = __builtin_amdgcn_readfirstlane(w_lo); w_hi = __builtin_amdgcn_readfirstlane(w_hi); w_all = __builtin_amdgcn_readfirstlane(w_all);
-    if (lane == 0) { shared[2 * wave] = w_lo; shared[2 * wave + 1] = w_hi; }
-    __syncthreads();
-    lo = 0x7fffffff; up = -1;
-    for (int w = 0; w < 4; ++w) { lo = min(lo, shared[2 * w]); up = max(up, shared[2 * w + 1]); }
-    lo = __builtin_amdgcn_readfirstlane(lo); up = __builtin_amdgcn_readfirstlane(up);
+    all = span_of(qr, row0 / a.G, i_last);
+    w = span_of(qr, min(wrow0, R - 1) / a.G, min(wrow0 + 31, R - 1) / a.G);
   }
   const int pieces = (a.M + 31) / 32;
   const int* const ranges = a.kdoc ? a.kranges + (int64_t)b * pieces * 2 : nullptr;
-  Finder<S::KEYS / 32> find{ranges, pieces, lo, up};
+  Finder<S::KEYS / 32> find{ranges, pieces, all.lo, all.hi};
 
   F qf[L::STEPS], df[L::STEPS];
   {
@@ -82,7 +77,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
 #pragma unroll
   for (int d = 0; d < L::BLOCKS; ++d) o[d] = (f32x16)0.0f;
 
-  const int all = (end + S::KEYS - 1) / S::KEYS, per = (all + a.splits - 1) / a.splits, tiles = min(all, (split + 1) * per);
+  const int most = (end + S::KEYS - 1) / S::KEYS, per = (most + a.splits - 1) / a.splits, tiles = min(most, (split + 1) * per);
   const T* const kbase = at<T>(a.k, b, 0, hk);
   const T* const vbase = at<T>(a.v, b, 0, hk);
   auto load = [&](int t, int stage) {
@@ -106,7 +101,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
       if (key0 >= w_last) break;
       bool whole = key0 + 32 <= w_first, one = true;
       if (ranges) {
-        one = (scalar(ranges, 2 * (key0 / 32)) == w_hi) & (scalar(ranges, 2 * (key0 / 32) + 1) == w_hi) & (w_all == w_hi) & (w_hi >= 0);
+        one = w.one & (scalar(ranges, 2 * (key0 / 32)) == w.hi) & (scalar(ranges, 2 * (key0 / 32) + 1) == w.hi);
         whole = whole && one;
       }
       const int tcol = S::TIGHT ? fresh(col) : col, tlane = S::TIGHT ? fresh(lane) : lane;

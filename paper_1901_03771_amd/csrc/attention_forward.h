@@ -63,24 +63,18 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
   const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
 
-  // documents: this lane's, the wave's and the workgroup's smallest and largest
-  int doc = -1, w_lo = 0x7fffffff, w_hi = -1, w_all = 0x7fffffff, lo = 0, up = 0;
+  // documents: this lane's, and what the pieces of the wave's and the workgroup's queries hold
+  int doc = -1;
+  Span w = {0, 0, true}, all = {0, 0, true};
   if (a.kdoc) {
+    const int* const qr = a.qranges + (int64_t)b * ((a.N + 31) / 32) * 2;
     if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
-    w_lo = doc >= 0 ? doc : 0x7fffffff; w_hi = doc; w_all = valid ? doc : 0x7fffffff;
-    for (int m = 16; m; m >>= 1) {
-      w_lo = min(w_lo, __shfl_xor(w_lo, m)); w_hi = max(w_hi, __shfl_xor(w_hi, m)); w_all = min(w_all, __shfl_xor(w_all, m));
-    }
-    w_lo = __builtin_amdgcn_readfirstlane(w_lo); w_hi = __builtin_amdgcn_readfirstlane(w_hi); w_all = __builtin_amdgcn_readfirstlane(w_all);
-    if (lane == 0) { shared[2 * wave] = w_lo; shared[2 * wave + 1] = w_hi; }
-    __syncthreads();
-    lo = 0x7fffffff; up = -1;
-    for (int w = 0; w < S::WAVES; ++w) { lo = min(lo, shared[2 * w]); up = max(up, shared[2 * w + 1]); }
-    lo = __builtin_amdgcn_readfirstlane(lo); up = __builtin_amdgcn_readfirstlane(up);
+    all = span_of(qr, row0 / a.G, i_last);
+    w = span_of(qr, min(wrow0, R - 1) / a.G, min(wrow0 + 31, R - 1) / a.G);
   }
   const int pieces = (a.M + 31) / 32;
   const int* const ranges = a.kdoc ? a.kranges + (int64_t)b * pieces * 2 : nullptr;
-  Finder<S::KEYS / 32> find{ranges, pieces, lo, up};
+  Finder<S::KEYS / 32> find{ranges, pieces, all.lo, all.hi};
 
   // the rows' operands
   F qf[L::STEPS];
@@ -125,7 +119,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb) {
           const int e = min(key0 / 32 + kb, pieces - 1);
-          one &= (scalar(ranges, 2 * e) == w_hi) & (scalar(ranges, 2 * e + 1) == w_hi) & (w_all == w_hi) & (w_hi >= 0);
+          one &= w.one & (scalar(ranges, 2 * e) == w.hi) & (scalar(ranges, 2 * e + 1) == w.hi);
         }
         whole = whole && one;
       }

@@ -263,34 +263,60 @@ static __device__ __forceinline__ Place place_of(unsigned id, int pairs, int blo
   return {(int)(id / (unsigned)blocks), (int)(id % (unsigned)blocks)};
 }
 
-// Tiles of 32 * UNIT entries of a row of document numbers that hold a number between lo and hi, 64 at a time.
+// Tiles of 32 * UNIT entries of a row of document numbers that hold a number between lo and hi, found 256 at a time.
 template <int UNIT>
 struct Finder {
   const int* ranges;   // nullptr: every tile
   int count;           // 32-entry pieces
   int lo, hi;          // lo > hi: none
   int base = -1;
-  uint64_t mask = 0;
+  uint64_t mask[4] = {0, 0, 0, 0};
+  __device__ __forceinline__ void look(int t, int end, int lane) {
+    base = t;
+    int l[4][UNIT], u[4][UNIT];
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int x = 0; x < UNIT; ++x) {
+        const int i = min((t + 64 * w + lane) * UNIT + x, count - 1);
+        l[w][x] = ranges[2 * i];
+        u[w][x] = ranges[2 * i + 1];
+      }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      bool some = false;
+#pragma unroll
+      for (int x = 0; x < UNIT; ++x) some |= (l[w][x] <= hi) & (u[w][x] >= lo);
+      mask[w] = __ballot(some & (t + 64 * w + lane < end) & (lo <= hi));
+    }
+  }
   __device__ __forceinline__ int next(int t, int end, int lane) {
     if (!ranges) return t < end ? t : end;
     while (t < end) {
-      if (base < 0 || t < base || t >= base + 64) {
-        base = t;
-        bool some = false;
-#pragma unroll
-        for (int u = 0; u < UNIT; ++u) {
-          const int i = (t + lane) * UNIT + u;
-          if (t + lane < end && i < count) some |= ranges[2 * i] <= hi && ranges[2 * i + 1] >= lo;
-        }
-        mask = __ballot(some && lo <= hi);
-      }
-      const uint64_t m = mask >> (t - base);
+      if (base < 0 || t < base || t >= base + 256) look(t, end, lane);
+      const int w = (t - base) >> 6;
+      const uint64_t m = (w == 0 ? mask[0] : w == 1 ? mask[1] : w == 2 ? mask[2] : mask[3]) >> ((t - base) & 63);
       if (m) { const int f = t + __builtin_ctzll(m); return f < end ? f : end; }
-      t = base + 64;
+      t = base + (w + 1) * 64;
     }
     return end;
   }
 };
+
+// Smallest (below zero counts as none: 0) and largest document of the 32-entry pieces that entries first .. last lie in, and whether all of
+// them are one document's.
+struct Span { int lo, hi; bool one; };
+static __device__ __forceinline__ Span span_of(const int* ranges, int first, int last) {
+  Span s = {0x7fffffff, -1, true};
+  int all = 0x7fffffff;
+  for (int e = first / 32; e <= last / 32; ++e) {
+    const int l = scalar(ranges, 2 * e), u = scalar(ranges, 2 * e + 1);
+    all = min(all, l);
+    if (u >= 0) { s.lo = min(s.lo, max(l, 0)); s.hi = max(s.hi, u); }
+  }
+  s.one = all == s.hi && s.hi >= 0;
+  return s;
+}
 
 // Four neighbouring values of a row of a tensor (of those below D).
 template <class T>

@@ -55,17 +55,22 @@ __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a,
   if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
 }
 
-// Smallest and largest document number of 32 neighbours, half a wave each; `rows` gets the numbers themselves side by side, in rows of a
-// multiple of 128.
-__global__ __launch_bounds__(256) void gr_attention_ranges_kernel(const int* docs, int64_t sb, int64_t sn, int B, int N, int* to, int* rows) {
-  const int pieces = (N + 31) / 32;
-  const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
-  if (id >= (int64_t)B * pieces) return;
+// Smallest and largest document number of 32 neighbours, half a wave each, and the numbers themselves side by side in rows of a multiple of
+// 128: of the keys, then of the queries.
+__global__ __launch_bounds__(256) void gr_attention_ranges_kernel(const Args a, int64_t key_pieces) {
+  int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
+  const bool keys = id < key_pieces;
+  if (!keys) id -= key_pieces;
+  const int N = keys ? a.M : a.N, pieces = (N + 31) / 32;
+  if (id >= (int64_t)a.B * pieces) return;
+  const int64_t sb = keys ? a.kdoc_sb : a.qdoc_sb, sn = keys ? a.kdoc_sn : a.qdoc_sn, np = padded_rows(N);
+  const int* const docs = keys ? a.kdoc : a.qdoc;
   const int b = (int)(id / pieces), n = (int)(id - (int64_t)b * pieces) * 32 + (threadIdx.x & 31);
+  int* const rows = (keys ? a.kdocs : a.qdocs) + b * np;
+  int* const to = keys ? a.kranges : a.qranges;
   int lo = n < N ? docs[b * sb + n * sn] : 0x7fffffff, hi = n < N ? lo : -1;
-  const int64_t np = padded_rows(N);
-  rows[b * np + n] = hi;
-  for (int64_t r = n + 32; r >= (int64_t)pieces * 32 && r < np; r += 32) rows[b * np + r] = -1;
+  rows[n] = hi;
+  for (int64_t r = n + 32; r >= (int64_t)pieces * 32 && r < np; r += 32) rows[r] = -1;
   for (int m = 16; m; m >>= 1) { lo = min(lo, __shfl_xor(lo, m)); hi = max(hi, __shfl_xor(hi, m)); }
   if ((threadIdx.x & 31) == 0) { to[2 * id] = lo; to[2 * id + 1] = hi; }
 }
@@ -151,10 +156,8 @@ hipError_t combine(const Args& a, int type, int dp, hipStream_t stream) {
 }
 
 hipError_t ranges(const Args& a, hipStream_t stream) {
-  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.M + 31) / 32) * 32), dim3(256), 0, stream>>>(a.kdoc, a.kdoc_sb, a.kdoc_sn, a.B, a.M, a.kranges, a.kdocs);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.qranges) return e;
-  gr_attention_ranges_kernel<<<blocks_of((int64_t)a.B * ((a.N + 31) / 32) * 32), dim3(256), 0, stream>>>(a.qdoc, a.qdoc_sb, a.qdoc_sn, a.B, a.N, a.qranges, a.qdocs);
+  const int64_t keys = (int64_t)a.B * ((a.M + 31) / 32), queries = (int64_t)a.B * ((a.N + 31) / 32);
+  gr_attention_ranges_kernel<<<blocks_of((keys + queries) * 32), dim3(256), 0, stream>>>(a, keys);
   return hipGetLastError();
 }
 
