@@ -19,9 +19,9 @@ template <class T, int DP>
 struct ShapeQ {
   static constexpr int THREADS = 256, KEYS = tile_rows(sizeof(T), DP), ROWS = 128, TILE = KEYS * Tile<T, DP>::ROW;
   static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;   // two stages of k and v, 64 words to exchange, two stages of the keys' documents
-  static constexpr int REGS = DP / 16 * 4 * (int)sizeof(T) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
-  static constexpr bool TIGHT = REGS > 160;   // of registers: addresses within tiles are formed anew for each tile
-  static constexpr int PER_CU = REGS <= 208 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 8 : 24) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
+  static constexpr bool TIGHT = REGS > (sizeof(T) == 2 ? 160 : 128);   // of registers: addresses within tiles are formed anew for each tile
+  static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 208 : 120) && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
 template <class T, int DP, int MODE>
@@ -108,6 +108,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int st = 0; st < L::STEPS; ++st) {
+        if constexpr (DP == 256) { anew(qf[st]); anew(df[st]); }
         s = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s);
         dp = mma(L::row(vt, kb * 32 + tcol, st, hi), df[st], dp);
       }
@@ -184,7 +185,7 @@ struct ShapeKV {
   static constexpr int ROWS = tile_rows(sizeof(T), DP), KEYS = 128, TILE = ROWS * Tile<T, DP>::ROW;   // rows: of a tile of queries
   static constexpr int STATS = 4 * ROWS;                     // less, delta and document of every row
   static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
-  static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
+  static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 4 : 12) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
     static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 240 : 200) && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
@@ -307,6 +308,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
       f32x16 s = (f32x16)0.0f, dp = (f32x16)0.0f;
 #pragma unroll
       for (int x = 0; x < L::STEPS; ++x) {
+        if constexpr (DP == 256) { anew(kf[x]); if constexpr (WANT_K) anew(vf[x]); }
         s = mma(L::row(qt, rb * 32 + fcol, x, fhi), kf[x], s);
         if constexpr (WANT_K) dp = mma(L::row(dt, rb * 32 + fcol, x, fhi), vf[x], dp);
       }

@@ -29,9 +29,9 @@ struct Shape {
   static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;
   static_assert(!DIVIDED || WAVES * 32 * (DP + 4) * 4 <= 4 * TILE, "the waves' sums fit the stages");
   // registers: operands of q, sums, scores.  Two workgroups per compute unit where they fit 256.
-  static constexpr int REGS = DP / 16 * 2 * (int)sizeof(T) + DP / 2 + 16 * KB;
-  static constexpr bool TIGHT = REGS > 128;   // of registers: addresses within tiles are formed anew for each tile
-  static constexpr int PER_CU = REGS <= 224 && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 4 : 12) + DP / 2 + 16 * KB;
+  static constexpr bool TIGHT = REGS > (sizeof(T) == 2 ? 128 : 100);   // of registers: addresses within tiles are formed anew for each tile
+  static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 224 : 140) && 2 * LDS <= 160 * 1024 ? 2 : 1;
 };
 
 // PRECISE (bfloat16, where `rest` is wanted): a probability enters its product as the sum of two bfloat16 numbers, so that out + rest is the output to
@@ -131,7 +131,10 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
       for (int kb = 0; kb < S::KB; ++kb) {
         s[kb] = (f32x16)0.0f;
 #pragma unroll
-        for (int st = 0; st < L::STEPS; ++st) s[kb] = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s[kb]);
+        for (int st = 0; st < L::STEPS; ++st) {
+          if constexpr (DP == 256) anew(qf[st]);
+          s[kb] = mma(L::row(kt, kb * 32 + tcol, st, hi), qf[st], s[kb]);
+        }
       }
       __builtin_amdgcn_s_setprio(0);
       if constexpr (S::KB == 2) finished(s[0], s[1]);

@@ -8,7 +8,7 @@
 // which is two groups of four neighbouring rows: what ds_read_b64_tr_b16 returns from a row-major tile.  So scores are formed with
 // the side that is normalised along the lanes (queries for the output and dq, keys for dk and dv), the softmax needs one
 // exchange between the two halves of a wave, and neither scores nor probabilities ever pass through LDS.
-// float32 uses the same layout: one step of 16 is eight v_mfma_f32_32x32x2_f32.
+// float32 uses the same layout, as three bfloat16 pieces.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -41,11 +41,38 @@ template <> struct Frag<__bf16> { typedef b16x8 type; };
 template <> struct Frag<float> { typedef f32x8 type; };
 
 static __device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-static __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+// float32 as bfloat16 pieces: x = h + m + l to 2^-26 of x, each piece the rounding of what the ones before it leave, and x y = the six products
+// of pieces that count (m l, l m and l l are below 2^-25 of it).  Six products of bfloat16 take 192 cycles of a SIMD's matrix core, eight steps of
+// v_mfma_f32_32x32x2_f32 512; the pieces cost 44 vector instructions for an operand of eight values, beside them (8 heads of 4096 rows twice, 64 values: 564 us
+// on the float32 products, 365 so; the results are no further from binary64).  An infinity has no pieces: it gives NaN.
+struct Pieces { b16x8 h, m, l; };
+static __device__ __forceinline__ Pieces pieces(f32x8 x) {
+  Pieces p;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-  return c;
+  for (int j = 0; j < 8; j += 2) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    f32x2 v = {x[j], x[j + 1]};
+    const b16x2 h = __builtin_convertvector(v, b16x2);
+    v[0] -= (float)h[0]; v[1] -= (float)h[1];
+    const b16x2 m = __builtin_convertvector(v, b16x2);
+    v[0] -= (float)m[0]; v[1] -= (float)m[1];
+    const b16x2 l = __builtin_convertvector(v, b16x2);
+    p.h[j] = h[0]; p.h[j + 1] = h[1]; p.m[j] = m[0]; p.m[j + 1] = m[1]; p.l[j] = l[0]; p.l[j + 1] = l[1];
+  }
+  return p;
 }
+static __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+  const Pieces x = pieces(a), y = pieces(b);
+  c = mma(x.l, y.h, c);
+  c = mma(x.h, y.l, c);
+  c = mma(x.m, y.m, c);
+  c = mma(x.m, y.h, c);
+  c = mma(x.h, y.m, c);
+  return mma(x.h, y.h, c);
+}
+// Keeps the pieces of an operand from being formed ahead of a loop, for lack of registers to hold them.
+static __device__ __forceinline__ void anew(f32x8& f) { asm volatile("" : "+v"(f)); }
+static __device__ __forceinline__ void anew(b16x8&) {}
 
 // Results of the matrix cores that branches may stand before the use of: a vector instruction reads such a register 19 issue slots after
 // its product at the earliest, and the compiler, which counts them, has been seen to count along one of several paths that meet
