@@ -40,20 +40,15 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
   const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + wave * 32;
   const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
-  const int row = wrow0 + col;
-  const bool valid = row < R;
-  const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
-  const int see = valid ? keys_seen(a, i, len, pre) : 0;
+  const Row mine = row_of(a, hk, wrow0 + col);   // (not kept beyond the operands: registers are full)
   const int i_last = (row0 + S::ROWS <= R ? row0 + S::ROWS - 1 : R - 1) / a.G;
   const int end = keys_seen(a, i_last, len, pre);
   const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
   const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
-  // documents: this lane's, and what the pieces of the wave's and the workgroup's queries hold
-  int doc = -1;
+  // documents: what the pieces of the wave's and the workgroup's queries hold
   Span w = {0, 0, true}, all = {0, 0, true};
   if (a.kdoc) {
     const int* const qr = a.qranges + (int64_t)b * ((a.N + 31) / 32) * 2;
-    if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
     all = span_of(qr, row0 / a.G, i_last);
     w = span_of(qr, min(wrow0, R - 1) / a.G, min(wrow0 + 31, R - 1) / a.G);
   }
@@ -63,15 +58,15 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
 
   F qf[L::STEPS], df[L::STEPS];
   {
-    const T* q = at<T>(a.q, b, i, h);
-    const T* d = at<T>(a.dout, b, i, h);
+    const T* q = at<T>(a.q, b, mine.i, mine.h);
+    const T* d = at<T>(a.dout, b, mine.i, mine.h);
 #pragma unroll
-    for (int s = 0; s < L::STEPS; ++s) { qf[s] = L::fetch(q, s, hi, a.D, valid, a.q.aligned); df[s] = L::fetch(d, s, hi, a.D, valid, a.dout.aligned); }
+    for (int s = 0; s < L::STEPS; ++s) { qf[s] = L::fetch(q, s, hi, a.D, mine.valid, a.q.aligned); df[s] = L::fetch(d, s, hi, a.D, mine.valid, a.dout.aligned); }
   }
-  const int64_t stat = ((int64_t)b * a.H + h) * padded_rows(a.N) + i;
-  const float less = valid ? a.less[stat] : INF, delta = valid ? a.delta[stat] : 0.0f;
-  const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
-  const float pos = MODE & MODE_BIAS ? (float)(a.position + i) : 0.0f;
+  const int64_t stat = ((int64_t)b * a.H + mine.h) * padded_rows(a.N) + mine.i;
+  const float less = mine.valid ? a.less[stat] : INF, delta = mine.valid ? a.delta[stat] : 0.0f;
+  const float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
+  const int64_t pos = MODE & MODE_BIAS ? a.position + mine.i : 0;
 
   f32x16 o[L::BLOCKS];
 #pragma unroll
@@ -113,12 +108,12 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
         dp = mma(L::row(vt, kb * 32 + tcol, st, hi), df[st], dp);
       }
       finished(s, dp);
+      const float away = MODE & MODE_BIAS ? (float)(pos - key0 - 4 * (tlane >> 5)) : 0.0f;   // from the first key of this half
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int key = key0 + (r & 3) + 8 * (r >> 2) + 4 * hi;
         float y = s[r], bend = 1.0f;
         if constexpr (MODE & MODE_CAP) { y = capped<T, MODE>(y, a.cin); bend = __builtin_fmaf(-y, y, 1.0f); }
-        if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf(pos - (float)key), -less));
+        if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf(away - (float)((r & 3) + 8 * (r >> 2))), -less));
         else y = __builtin_fmaf(y, a.c, -less);
         s[r] = y;
         dp[r] -= delta;
@@ -127,13 +122,14 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]) * dp[r];
       if (!whole) {
+        const int flane = fresh(lane);
+        const Row me = row_of(a, hk, wrow0 + (flane & 31));
+        const int see = (me.valid ? keys_seen(a, me.i, len, pre) : 0) - key0 - 4 * (flane >> 5);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = key0 + (r & 3) + 8 * (r >> 2) + 4 * hi;
-          s[r] = key < see ? s[r] : 0.0f;
-        }
+        for (int r = 0; r < 16; ++r) s[r] = (r & 3) + 8 * (r >> 2) < see ? s[r] : 0.0f;
         if (!one) {
-          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + kb * 32 + 4 * hi;
+          const int doc = me.valid ? a.qdocs[b * padded_rows(a.N) + me.i] : -1;
+          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + kb * 32 + 4 * (flane >> 5);
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
             const i32x4 n = *(const GR_LDS i32x4*)(kd + 8 * r4);
@@ -154,10 +150,11 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
     stage ^= 1;
   }
   finished(o);
-  if (!valid) return;
+  const Row me = row_of(a, hk, wrow0 + col);
+  if (!me.valid) return;
   if (a.splits > 1) {
     // (splits, B * HK, N * G, DP)
-    float* const to = a.part_o + (((int64_t)split * pairs + place.pair) * R + row) * DP;
+    float* const to = a.part_o + (((int64_t)split * pairs + place.pair) * R + wrow0 + col) * DP;
 #pragma unroll
     for (int d = 0; d < L::BLOCKS; ++d)
 #pragma unroll
@@ -167,7 +164,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
       }
     return;
   }
-  T* const dq = at<T>(a.dq, b, i, h);
+  T* const dq = at<T>(a.dq, b, me.i, me.h);
 #pragma unroll
   for (int d = 0; d < L::BLOCKS; ++d)
 #pragma unroll

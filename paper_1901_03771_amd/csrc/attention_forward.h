@@ -53,22 +53,17 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   const int b = place.pair / a.HK, hk = place.pair - b * a.HK;
   const int R = a.N * a.G, row0 = rb * S::ROWS, wrow0 = row0 + (DIVIDED ? 0 : wave * 32);
   const int len = length_of(a, b), pre = a.prefix ? scalar(a.prefix, b * a.prefix_s) : 0;
-  const int row = wrow0 + col;
-  const bool valid = row < R;
-  const int i = (valid ? row : R - 1) / a.G, g = (valid ? row : R - 1) - i * a.G, h = hk * a.G + g;
-  const int see = valid ? keys_seen(a, i, len, pre) : 0;
+  const Row mine = row_of(a, hk, wrow0 + col);   // (not kept beyond the operands: registers are full)
   // of the workgroup's rows, and of this wave's: how many keys the last one sees, the first one
   const int i_last = (row0 + S::ROWS <= R ? row0 + S::ROWS - 1 : R - 1) / a.G;
   const int end = keys_seen(a, i_last, len, pre);
   const int w_first = wrow0 < R ? keys_seen(a, wrow0 / a.G, len, pre) : 0;
   const int w_last = wrow0 < R ? keys_seen(a, (wrow0 + 31 < R ? wrow0 + 31 : R - 1) / a.G, len, pre) : 0;
 
-  // documents: this lane's, and what the pieces of the wave's and the workgroup's queries hold
-  int doc = -1;
+  // documents: what the pieces of the wave's and the workgroup's queries hold
   Span w = {0, 0, true}, all = {0, 0, true};
   if (a.kdoc) {
     const int* const qr = a.qranges + (int64_t)b * ((a.N + 31) / 32) * 2;
-    if (valid) doc = a.qdoc[b * a.qdoc_sb + i * a.qdoc_sn];
     all = span_of(qr, row0 / a.G, i_last);
     w = span_of(qr, min(wrow0, R - 1) / a.G, min(wrow0 + 31, R - 1) / a.G);
   }
@@ -79,12 +74,12 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   // the rows' operands
   F qf[L::STEPS];
   {
-    const T* q = at<T>(a.q, b, i, h);
+    const T* q = at<T>(a.q, b, mine.i, mine.h);
 #pragma unroll
-    for (int s = 0; s < L::STEPS; ++s) qf[s] = L::fetch(q, s, hi, a.D, valid, a.q.aligned);
+    for (int s = 0; s < L::STEPS; ++s) qf[s] = L::fetch(q, s, hi, a.D, mine.valid, a.q.aligned);
   }
-  const float slope = MODE & MODE_BIAS ? a.slopes[h * a.slopes_s] * LOG2E : 0.0f;
-  const float pos = MODE & MODE_BIAS ? (float)(a.step ? (int64_t)len - 1 : a.position + i) : 0.0f;
+  const float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
+  const int64_t pos = MODE & MODE_BIAS ? (a.step ? (int64_t)len - 1 : a.position + mine.i) : 0;
   const float c = MODE & MODE_BIAS ? 1.0f : a.c;
 
   f32x16 o[L::BLOCKS];
@@ -140,26 +135,28 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
       if constexpr (S::KB == 2) finished(s[0], s[1]);
       else finished(s[0]);
       if constexpr (MODE != 0) {
+        const float away = MODE & MODE_BIAS ? (float)(pos - key0 - 4 * (tlane >> 5)) : 0.0f;   // from the first key of this half
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             float y = s[kb][r];
             if constexpr (MODE & MODE_CAP) y = capped<T, MODE>(y, a.cin);
-            if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, -slope * __builtin_fabsf(pos - (float)(key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi)));
+            if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, -slope * __builtin_fabsf(away - (float)(kb * 32 + (r & 3) + 8 * (r >> 2))));
             s[kb][r] = y;
           }
       }
       if (!whole) {
+        const int flane = fresh(lane);
+        const Row me = row_of(a, hk, wrow0 + (flane & 31));
+        const int see = (me.valid ? keys_seen(a, me.i, len, pre) : 0) - key0 - 4 * (flane >> 5);
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = key0 + kb * 32 + (r & 3) + 8 * (r >> 2) + 4 * hi;
-            s[kb][r] = key < see ? s[kb][r] : -INF;
-          }
+          for (int r = 0; r < 16; ++r) s[kb][r] = kb * 32 + (r & 3) + 8 * (r >> 2) < see ? s[kb][r] : -INF;
         if (!one) {
-          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + (DIVIDED ? wave * 32 : 0) + 4 * hi;
+          const int doc = me.valid ? a.qdocs[b * padded_rows(a.N) + me.i] : -1;
+          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + (DIVIDED ? wave * 32 : 0) + 4 * (flane >> 5);
 #pragma unroll
           for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
@@ -266,10 +263,11 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
     l = total;
   }
 
-  if (!valid) return;
-  const bool mine = !DIVIDED || wave == 0;
+  const Row me = row_of(a, hk, wrow0 + col);
+  if (!me.valid) return;
+  const bool first = !DIVIDED || wave == 0;
   if (a.splits > 1) {
-    const int64_t at_row = ((int64_t)split * pairs + place.pair) * R + row;
+    const int64_t at_row = ((int64_t)split * pairs + place.pair) * R + wrow0 + col;
     float* const po = a.part_o + at_row * DP;
 #pragma unroll
     for (int d = 0; d < L::BLOCKS; ++d) {
@@ -280,13 +278,13 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
         *(f32x4*)(po + d * 32 + 2 * r + 4 * hi) = x;
       }
     }
-    if (mine && hi == 0) { a.part_ml[2 * at_row] = m; a.part_ml[2 * at_row + 1] = l; }
+    if (first && hi == 0) { a.part_ml[2 * at_row] = m; a.part_ml[2 * at_row + 1] = l; }
     return;
   }
   // a row that sees nothing: out = 0, lse = -inf
   const float inv = m == -INF ? 0.0f : 1.0f / l;
-  T* const out = at<T>(a.out, b, i, h);
-  T* const rest = a.rest.p ? at<T>(a.rest, b, i, h) : nullptr;
+  T* const out = at<T>(a.out, b, me.i, me.h);
+  T* const rest = a.rest.p ? at<T>(a.rest, b, me.i, me.h) : nullptr;
 #pragma unroll
   for (int d = 0; d < L::BLOCKS; ++d) {
     if (DIVIDED && d % S::WAVES != wave) continue;
@@ -299,7 +297,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
       if (rest) store4(rest, d * 32 + 2 * r + 4 * hi, a.D, y, a.rest.aligned);
     }
   }
-  if (a.lse && mine && hi == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
+  if (a.lse && first && hi == 0) a.lse[((int64_t)b * a.H + me.h) * a.N + me.i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
 }
 
 template <class T, int DP, int MODE, bool DIVIDED>

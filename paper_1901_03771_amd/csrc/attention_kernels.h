@@ -281,6 +281,18 @@ static __device__ __forceinline__ int length_of(const Args& a, int b) {
   return n < 0 ? 0 : n < a.M ? n : a.M;
 }
 
+// A row of the queries of one head of k: query and head of q (a row behind the last stands for the last).
+struct Row { int i, h; bool valid; };
+static __device__ __forceinline__ Row row_of(const Args& a, int hk, int row) {
+  const int R = a.N * a.G;
+  Row r;
+  r.valid = row < R;
+  const int n = r.valid ? row : R - 1;
+  r.i = n / a.G;
+  r.h = hk * a.G + (n - r.i * a.G);
+  return r;
+}
+
 // Which (batch, head of k) and which block of it a workgroup takes.  Workgroups go round the eight XCDs in turn, each with an L2 of its
 // own: those of one head stay on one XCD (or on 8 / pairs of them) where the number of heads allows it.
 struct Place { int pair, block; };
