@@ -303,10 +303,12 @@ static int fill_scores(Call& c, const gr_scores* s, int type, Args* a) {
 
 static int keys_of(bool divided, int size, int dp) { return divided ? 32 * shared_waves(size, dp) : tile_rows(size, dp); }
 
-// Splits of a long dimension: two workgroups for each of the 256 compute units, as long as every split has two tiles of its own.
-static int splits_of(int64_t groups, int64_t tiles, int most) {
+// Splits of a long dimension where there are fewer groups than compute units: as many workgroups as fit the 256 compute units at once, each with a
+// tile at least.  More wait for a second turn (6 heads of 777 rows of float32, one workgroup per compute unit: forward and gradient 138 us with 6 splits
+// of 42 groups, 152 with 8), fewer walk longer (1 head of 448 rows: 1, 2, 4, 8 splits take 151, 117, 86, 70 us).
+static int splits_of(int64_t groups, int64_t tiles, int most, int per_cu) {
   if (groups >= 256 || groups < 1) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / groups, tiles / 2), most));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 * per_cu / groups, tiles), most));
 }
 
 // The same for calls of at most 32 rows per head, which read k and v at the rate of the memory: four workgroups per compute unit, which fit it
@@ -344,7 +346,7 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   const int keys = keys_of(divided, size, dp);
   a.blocks = (int)((rows + (divided ? 31 : 127)) / (divided ? 32 : 128));
   const int64_t tiles = ((int64_t)a.M + keys - 1) / keys;
-  a.splits = divided ? token_splits_of(pairs * a.blocks, tiles) : splits_of(pairs * a.blocks, tiles, MAX_SPLITS);
+  a.splits = divided ? token_splits_of(pairs * a.blocks, tiles) : splits_of(pairs * a.blocks, tiles, MAX_SPLITS, forward_per_cu(size, dp));
   const int64_t blocks = (int64_t)a.blocks * a.splits;
   if (blocks * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
@@ -464,11 +466,11 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   if (pairs == 0) return GR_OK;
   const int64_t qblocks = (rows + 127) / 128, kblocks = ((int64_t)a.M + 127) / 128;
   const int64_t tile = tile_rows(size, dp);
-  const int qsplits = splits_of(pairs * qblocks, ((int64_t)a.M + tile - 1) / tile, 16);
+  const int qsplits = splits_of(pairs * qblocks, ((int64_t)a.M + tile - 1) / tile, 16, grad_q_per_cu(size, dp));
   // For dk and dv, where a workgroup walks the queries of G heads, from every place on to the end: more and shorter walks even out what causal
   // masks and documents leave of them.
   const int64_t units = (((int64_t)a.N + tile - 1) / tile) * a.G;
-  int ksplits = splits_of(pairs * kblocks, units, 16);
+  int ksplits = splits_of(pairs * kblocks, units, 16, grad_kv_per_cu(size, dp));
   if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));
   if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);

@@ -55,6 +55,10 @@ constexpr int64_t padded_rows(int64_t n) { return (n + 127) / 128 * 128; }   // 
 // Sizes that host and kernels share, for an element of `size` bytes and heads padded to `dp` values.
 constexpr int row_values(int dp) { return dp <= 64 ? 64 : dp <= 128 ? 128 : 256; }                 // of a row in LDS
 constexpr int tile_rows(int size, int dp) { return size * row_values(dp) <= 256 ? 64 : 32; }       // of a tile that waves share
+// Workgroups of a kernel that fit a compute unit together: two where a wave's operands, sums and scores leave 256 registers enough.
+constexpr int forward_per_cu(int size, int dp) { return size == 2 || dp <= 96 ? 2 : 1; }
+constexpr int grad_q_per_cu(int size, int dp) { return size == 2 && dp <= 128 ? 2 : 1; }
+constexpr int grad_kv_per_cu(int size, int dp) { return size == 2 ? (dp <= 128 ? 2 : 1) : (dp <= 64 ? 2 : 1); }
 constexpr int MAX_SPLITS = 256;
 // Waves that divide a tile's keys.  bfloat16: tiles of 16 KiB, so that two workgroups and more fit a compute unit and one's loads are under way
 // while another multiplies (32 sequences of 4096 to 8192 keys, 128 values: 200 us with one workgroup of four waves per compute unit, 172 so).  float32,

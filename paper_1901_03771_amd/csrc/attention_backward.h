@@ -21,7 +21,8 @@ struct ShapeQ {
   static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;   // two stages of k and v, 64 words to exchange, two stages of the keys' documents
   static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 8 : 24) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
   static constexpr bool TIGHT = REGS > (sizeof(T) == 2 ? 160 : 128);   // of registers: addresses within tiles are formed anew for each tile
-  static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 208 : 120) && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr int PER_CU = grad_q_per_cu(sizeof(T), DP);
+  static_assert(PER_CU * LDS <= 160 * 1024, "LDS of a compute unit");
 };
 
 template <class T, int DP, int MODE>
@@ -182,8 +183,8 @@ struct ShapeKV {
   static constexpr int ROWS = tile_rows(sizeof(T), DP), KEYS = 128, TILE = ROWS * Tile<T, DP>::ROW;   // rows: of a tile of queries
   static constexpr int STATS = 4 * ROWS;                     // less, delta and document of every row
   static constexpr int LDS = 4 * TILE + 2 * STATS * 4;       // two stages of q and dout, and of these
-  static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 4 : 12) * (WHICH == ONLY_V ? 1 : 2) + DP / 2 * (WHICH == BOTH ? 2 : 1) + 32;
-    static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 240 : 200) && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr int PER_CU = WHICH == ONLY_V && sizeof(T) == 2 ? 2 : grad_kv_per_cu(sizeof(T), DP);
+  static_assert(PER_CU * LDS <= 160 * 1024, "LDS of a compute unit");
 };
 
 template <class T, int DP, int MODE, int WHICH>

@@ -28,10 +28,11 @@ struct Shape {
   // two stages of a tile of k and one of v (the joining waves' sums lie over them), 64 words to exchange, two stages of the keys' documents
   static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;
   static_assert(!DIVIDED || WAVES * 32 * (DP + 4) * 4 <= 4 * TILE, "the waves' sums fit the stages");
-  // registers: operands of q, sums, scores.  Two workgroups per compute unit where they fit 256.
+  // registers: operands of q, sums, scores
   static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 4 : 12) + DP / 2 + 16 * KB;
   static constexpr bool TIGHT = REGS > (sizeof(T) == 2 ? 128 : 100);   // of registers: addresses within tiles are formed anew for each tile
-  static constexpr int PER_CU = REGS <= (sizeof(T) == 2 ? 224 : 140) && 2 * LDS <= 160 * 1024 ? 2 : 1;
+  static constexpr int PER_CU = forward_per_cu(sizeof(T), DP);
+  static_assert(DIVIDED || PER_CU * LDS <= 160 * 1024, "LDS of a compute unit");
 };
 
 // PRECISE (bfloat16, where `rest` is wanted): a probability enters its product as the sum of two bfloat16 numbers, so that out + rest is the output to

@@ -4,9 +4,42 @@
 namespace gr {
 namespace attn {
 
-// out and lse of a row from the splits' (m, l, sums): each scaled to the largest m, added in the order of the splits.  A workgroup has one
-// row: its threads read the splits' (m, l) once, a split each, then 256 / quads runs of splits are summed side by side for every four
+// out and lse of a row from the splits' (m, l, sums): each scaled to the largest m, added in the order of the splits.  With more than 16 splits a
+// workgroup has one row: its threads read the splits' (m, l) once, a split each, then 256 / quads runs of splits are summed side by side for every four
 // values and joined in order.  (Threads that each walked all splits of four values took 68 us for 128 splits of 8 rows, a chain of 128 reads.)
+template <class T>
+static __device__ __forceinline__ void finish_row(const Args& a, int64_t row, int d, const f32x4& x, float m, float l) {
+  const int R = a.N * a.G;
+  const int pair = (int)(row / R), r = (int)(row - (int64_t)pair * R), i = r / a.G, g = r - i * a.G, b = pair / a.HK, h = (pair - b * a.HK) * a.G + g;
+  const float inv = m == -INF ? 0.0f : 1.0f / l;
+  float o[4], y[4];
+  for (int e = 0; e < 4; ++e) { o[e] = x[e] * inv; y[e] = o[e] - (float)(T)o[e]; }
+  store4(at<T>(a.out, b, i, h), d, a.D, o, a.out.aligned);
+  if (a.rest.p) store4(at<T>(a.rest, b, i, h), d, a.D, y, a.rest.aligned);
+  if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void gr_attention_combine_few_kernel(const Args a, int dp) {
+  const int quads = dp / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = (int64_t)a.B * a.HK * a.N * a.G;
+  const int64_t row = id / quads;
+  const int d = (int)(id - row * quads) * 4;
+  if (row >= rows) return;
+  float m = -INF, l = 0.0f;
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) m = __builtin_fmaxf(m, a.part_ml[2 * (s * rows + row)]);
+  f32x4 x = (f32x4)0.0f;
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) {
+    const float ms = a.part_ml[2 * (s * rows + row)], by = ms == -INF ? 0.0f : exp2_(ms - m);
+    l = __builtin_fmaf(a.part_ml[2 * (s * rows + row) + 1], by, l);
+    const f32x4 p = *(const f32x4*)(a.part_o + (s * rows + row) * dp + d);
+    for (int e = 0; e < 4; ++e) x[e] = by == 0.0f ? x[e] : __builtin_fmaf(p[e], by, x[e]);
+  }
+  finish_row<T>(a, row, d, x, m, l);
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a, int dp) {
   __shared__ float by_[MAX_SPLITS];
@@ -46,13 +79,7 @@ __global__ __launch_bounds__(256) void gr_attention_combine_kernel(const Args a,
   __syncthreads();
   if (run != 0) return;
   for (int u = 1; u < runs; ++u) x += sums[u * quads + tid];
-  const int pair = (int)(row / R), r = (int)(row - (int64_t)pair * R), i = r / a.G, g = r - i * a.G, b = pair / a.HK, h = (pair - b * a.HK) * a.G + g;
-  const float inv = m == -INF ? 0.0f : 1.0f / l;
-  float o[4], y[4];
-  for (int e = 0; e < 4; ++e) { o[e] = x[e] * inv; y[e] = o[e] - (float)(T)o[e]; }
-  store4(at<T>(a.out, b, i, h), d, a.D, o, a.out.aligned);
-  if (a.rest.p) store4(at<T>(a.rest, b, i, h), d, a.D, y, a.rest.aligned);
-  if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
+  finish_row<T>(a, row, d, x, m, l);
 }
 
 // Smallest and largest document number of 32 neighbours, half a wave each, and the numbers themselves side by side in rows of a multiple of
@@ -149,9 +176,16 @@ __global__ __launch_bounds__(256) void gr_attention_sum_parts_kernel(const Args 
 static dim3 blocks_of(int64_t threads) { return dim3((unsigned)((threads + 255) / 256)); }
 
 hipError_t combine(const Args& a, int type, int dp, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.HK * a.N * a.G));
-  if (type == TYPE_BF16) gr_attention_combine_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, dp);
-  else gr_attention_combine_kernel<float><<<grid, dim3(256), 0, stream>>>(a, dp);
+  const int64_t rows = (int64_t)a.B * a.HK * a.N * a.G;
+  if (a.splits <= 16) {
+    const dim3 grid = blocks_of(rows * (dp / 4));
+    if (type == TYPE_BF16) gr_attention_combine_few_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, dp);
+    else gr_attention_combine_few_kernel<float><<<grid, dim3(256), 0, stream>>>(a, dp);
+  } else {
+    const dim3 grid((unsigned)rows);
+    if (type == TYPE_BF16) gr_attention_combine_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(a, dp);
+    else gr_attention_combine_kernel<float><<<grid, dim3(256), 0, stream>>>(a, dp);
+  }
   return hipGetLastError();
 }
 
