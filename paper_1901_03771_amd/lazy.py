@@ -829,8 +829,10 @@ def _result_array(ctx: Context, given, shape, dtype: int) -> "Array":
     if given is not None:
         return given
     torch = _torch()
-    return ctx.array(torch.empty(shape, device=f"cuda:{ctx.device}",
-                                 dtype={GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]))
+    a = ctx.array(torch.empty(shape, device=f"cuda:{ctx.device}",
+                              dtype={GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]))
+    a._view = True   # nobody else holds the tensor: the handle keeps it through materialize() and torch()
+    return a
 
 
 def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=None, rest=None):

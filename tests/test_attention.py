@@ -554,3 +554,50 @@ def test_far_offsets(ctx):
         gr.attention(ctx.array(qb), lk, lv, ctx.scores(), out=ctx.array(out), lse=False)
         ref = plain.attention(qb, kv[0].view(shape), kv[1].view(shape))
         plain.check(dict(out=out), ref, BF16, 64, shape[1], 4, 2, "far")
+
+
+@pytest.mark.gpu
+def test_layer_trains_and_generates():
+    """The example layer against the same layer in binary64 torch with automatic differentiation."""
+    from paper_1901_03771_amd import attention_layer as al
+    c = gr.Context()
+    layer = al.AttentionLayer(c, width=48, heads=4, shared=2, values=24, cap=8.0, seed=4)
+    ids, places = al.packed_documents(2, 70, "cuda", seed=5)
+    g = torch.Generator().manual_seed(6)
+    x, target = torch.randn(2, 70, 48, generator=g).cuda(), torch.randn(2, 70, 48, generator=g).cuda()
+    w = {n: t.cpu().double().requires_grad_() for n, t in layer.weights.items()}
+
+    def turned(t):
+        a = places.cpu().double()[..., None, None] * torch.tensor(list(layer.frequencies), dtype=torch.float64)
+        lo, hi = t[..., :12], t[..., 12:]
+        return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+
+    xd = x.cpu().double()
+    q, k, v = turned((xd @ w["q"]).view(2, 70, 4, 24)), turned((xd @ w["k"]).view(2, 70, 2, 24)), (xd @ w["v"]).view(2, 70, 2, 24)
+    k, v = k.repeat_interleave(2, 2), v.repeat_interleave(2, 2)
+    s = torch.einsum("bihd,bjhd->bhij", q, k) * 24 ** -0.5
+    s = 8.0 * torch.tanh(s / 8.0)
+    d = ids.cpu()
+    see = (torch.arange(70)[:, None] >= torch.arange(70)) & (d[:, :, None] == d[:, None, :])
+    p = torch.softmax(s.masked_fill(~see[:, None], -math.inf), -1)
+    y = torch.einsum("bhij,bjhd->bihd", p, v).reshape(2, 70, 96) @ w["o"]
+    loss = ((y - target.cpu().double()) ** 2).mean()
+    loss.backward()
+    before = {n: t.cpu().double() for n, t in layer.weights.items()}
+    got = layer.train_step(x, target, c.array(places), c.array(ids), rate=1.0)
+    # sums of up to 140 rows or 96 values in a handful of products one after another: each is off by at most (rows + values) 2^-24 of its terms' sizes,
+    # which are below 16 times the result's norm here
+    bar = 6 * (140 + 96) * 2.0 ** -24 * 16
+    assert abs(got - loss.item()) <= bar * loss.item()
+    for n, t in layer.weights.items():
+        step = before[n] - t.cpu().double()
+        assert (step - w[n].grad).norm() <= bar * w[n].grad.norm() + 2.0 ** -24 * before[n].norm(), n
+    # generation: the same rows as a forward pass over one sequence, with a cache that holds NaN where nothing was written
+    one = x[:, :20].contiguous()
+    whole = layer.forward(one, 0, None)[0].torch().view(2, 20, 48)
+    cache = [torch.full((2, 30, 2, 24), math.nan, device="cuda") for _ in range(2)]
+    lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for i in range(20):
+        y1 = layer.step(one[:, i].contiguous(), *cache, lengths)
+        assert (y1 - whole[:, i]).norm() <= bar * whole[:, i].norm(), i
+    c.close()
