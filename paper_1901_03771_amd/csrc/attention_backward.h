@@ -65,8 +65,8 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
     for (int s = 0; s < L::STEPS; ++s) { qf[s] = L::fetch(q, s, hi, a.D, mine.valid, a.q.aligned); df[s] = L::fetch(d, s, hi, a.D, mine.valid, a.dout.aligned); }
   }
   const int64_t stat = ((int64_t)b * a.H + mine.h) * padded_rows(a.N) + mine.i;
-  const float less = mine.valid ? a.less[stat] : INF, delta = mine.valid ? a.delta[stat] : 0.0f;
-  const float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
+  float less = mine.valid ? a.less[stat] : INF, delta = mine.valid ? a.delta[stat] : 0.0f;
+  float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
   const int64_t pos = MODE & MODE_BIAS ? a.position + mine.i : 0;
 
   f32x16 o[L::BLOCKS];
@@ -85,6 +85,11 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   };
   int t = find.next(split * per, tiles, lane), stage = 0;
   if (t < tiles) load(t, 0);
+  loaded(qf);
+  loaded(df);
+  loaded(less);
+  loaded(delta);
+  if constexpr (MODE & MODE_BIAS) loaded(slope);
   while (t < tiles) {
     const int after = find.next(t + 1, tiles, lane);
     arrive();
@@ -277,6 +282,8 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
   now = next(now);
   int stage = 0;
   if (now.u < u1) load(now, 0);
+  loaded(kf);
+  if constexpr (WANT_K) loaded(vf);
   while (now.u < u1) {
     const Unit after = next({now.u + 1, now.g, now.t + 1});
     arrive();

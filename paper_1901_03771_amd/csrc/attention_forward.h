@@ -79,7 +79,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
 #pragma unroll
     for (int s = 0; s < L::STEPS; ++s) qf[s] = L::fetch(q, s, hi, a.D, mine.valid, a.q.aligned);
   }
-  const float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
+  float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
   const int64_t pos = MODE & MODE_BIAS ? (a.step ? (int64_t)len - 1 : a.position + mine.i) : 0;
   const float c = MODE & MODE_BIAS ? 1.0f : a.c;
 
@@ -102,6 +102,8 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   };
   int t = find.next(split * per, t1, lane), stage = 0;
   if (t < t1) load(t, 0);
+  loaded(qf);
+  if constexpr (MODE & MODE_BIAS) loaded(slope);
   while (t < t1) {
     const int after = find.next(t + 1, t1, lane);
     arrive();

@@ -94,6 +94,15 @@ static __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn
 // loop at the price of registers that are full.
 static __device__ __forceinline__ int fresh(int x) { asm volatile("" : "+v"(x)); return x; }
 
+// Makes the compiler wait here for values that it has loaded, before a loop: it knows nothing of the loads into LDS of the statements below, and a wait of its own
+// within the loop, for what was loaded before it, would be for all of those too.
+static __device__ __forceinline__ void loaded(float& x) { asm volatile("" : "+v"(x)); }
+template <class F, int N>
+static __device__ __forceinline__ void loaded(F (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
+}
+
 constexpr float INF = __builtin_inff();
 
 // The value of the lane's partner in the other half of the wave.
