@@ -2,8 +2,9 @@
 //   lo' = factor (lo cos - hi sin),  hi' = factor (hi cos + lo sin);
 // the gradient is the same turn backwards.  A read and a write of the tensor bound it.
 //
-// A workgroup takes a few tokens and a run of heads.  It forms their sines and cosines once, in LDS, for all its heads, then moves whole
-// 16-byte vectors.  The angle is formed in turns, in 64 bits, and its whole turns are taken off there: at position 10^6 an angle
+// A workgroup takes a few tokens and a run of heads.  It forms their sines and cosines once, in LDS, for all its heads, and where the tokens
+// lie, then moves whole 16-byte vectors: a thread has a place in the heads and goes through the tokens with it, so that nothing is divided
+// on the way (4611 tokens of 12 heads of 80 float32 values: 13.6 us with three divisions a vector).  The angle is formed in turns, in 64 bits, and its whole turns are taken off there: at position 10^6 an angle
 // held in 32 bits is off by 0.06.  What is left, an eighth of a turn at most around a quarter, is small enough for Taylor's
 // polynomials in 32 bits (sine to x^9: 2e-9 off at pi / 4; cosine to x^10: 1e-10).
 #include "attention_kernels.h"
@@ -37,18 +38,26 @@ static __device__ __forceinline__ void turn(double turns, float& c, float& s) {
 // VECTORS: rows of whole aligned vectors, halves (or neighbouring pairs) and the part behind them of whole vectors too
 template <class T, bool VECTORS>
 __global__ __launch_bounds__(256) void gr_rotary_kernel(const Rotary r) {
-  extern __shared__ float table[];   // [token][cos of the pairs, sin of the pairs]
-  const int tid = threadIdx.x;
+  // [token] offset in x, in y, position; then [token][cos of the pairs, sin of the pairs]
+  extern __shared__ int64_t places[];
+  int64_t* const to = places + r.tokens;
+  int64_t* const pos = to + r.tokens;
+  float* const table = (float*)(pos + r.tokens);
+  const int tid = threadIdx.x, P = r.pairs;
   const int64_t token0 = (int64_t)blockIdx.x * r.tokens, all = (int64_t)r.B * r.N;
   const int tokens = (int)(all - token0 < r.tokens ? all - token0 : r.tokens);
   const int head0 = blockIdx.y * r.heads, heads = r.H - head0 < r.heads ? r.H - head0 : r.heads;
-  const int P = r.pairs;
+  for (int n = tid; n < tokens; n += 256) {
+    const int t = (int)token0 + n, b = t / r.N, i = t - b * r.N;
+    places[n] = b * r.x.sb + i * r.x.sn;
+    to[n] = b * r.y.sb + i * r.y.sn;
+    pos[n] = r.positions ? (int64_t)r.positions[b * r.positions_sb + i * r.positions_sn] : r.position + i;
+  }
+  __syncthreads();
   for (int k = tid; k < tokens * P; k += 256) {
     const int n = k / P, i = k - n * P;
-    const int64_t t = token0 + n, b = t / r.N, at_n = t - b * r.N;
-    const int64_t pos = r.positions ? (int64_t)r.positions[b * r.positions_sb + at_n * r.positions_sn] : r.position + at_n;
     float c, s;
-    turn((double)pos * r.turns[i], c, s);
+    turn((double)pos[n] * r.turns[i], c, s);
     table[2 * n * P + i] = c * r.factor;
     table[2 * n * P + P + i] = r.inverse ? -s * r.factor : s * r.factor;
   }
@@ -58,48 +67,55 @@ __global__ __launch_bounds__(256) void gr_rotary_kernel(const Rotary r) {
   // units of a head: pairs (V at a time, V / 2 where pairs are neighbours), then what is not turned
   const int turned = r.interleaved ? (VECTORS ? 2 * P / V : P) : P / V, units = turned + (r.D - 2 * P) / V;
   const bool in_place = r.x.p == r.y.p;
-  for (int k = tid; k < tokens * heads * units; k += 256) {
-    const int u = k % units, nh = k / units, n = nh / heads, h = head0 + nh - n * heads;
-    const int64_t t = token0 + n, b = t / r.N, at_n = t - b * r.N;
-    const T* x = at<T>(r.x, b, at_n, h);
-    T* y = at<T>(r.y, b, at_n, h);
-    const float* cs = table + 2 * n * P;
-    const float* sn = cs + P;
-    if constexpr (VECTORS) {
-      if (u >= turned) {
-        const int d = 2 * P + (u - turned) * V;
-        if (!in_place) *(vec*)(y + d) = *(const vec*)(x + d);
-      } else if (r.interleaved) {
-        const vec v = *(const vec*)(x + u * V);
-        vec w;
+  // the threads side by side over the units of the heads, and over tokens where those are fewer
+  const int wide = heads * units, side = wide < 256 ? wide : 256, rows = 256 / side, row = tid / side;
+  if (row >= rows) return;
+  for (int k = tid - row * side; k < wide; k += side) {
+    const int h = k / units, u = k - h * units;
+    const T* const xh = (const T*)r.x.p + (head0 + h) * r.x.sh;
+    T* const yh = (T*)r.y.p + (head0 + h) * r.y.sh;
+#pragma unroll 2
+    for (int n = row; n < tokens; n += rows) {
+      const T* x = xh + places[n];
+      T* y = yh + to[n];
+      const float* cs = table + 2 * n * P;
+      const float* sn = cs + P;
+      if constexpr (VECTORS) {
+        if (u >= turned) {
+          const int d = 2 * P + (u - turned) * V;
+          if (!in_place) *(vec*)(y + d) = *(const vec*)(x + d);
+        } else if (r.interleaved) {
+          const vec v = *(const vec*)(x + u * V);
+          vec w;
 #pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const float c = cs[u * (V / 2) + e / 2], s = sn[u * (V / 2) + e / 2], lo = (float)v[e], hi = (float)v[e + 1];
-          w[e] = (T)__builtin_fmaf(lo, c, -hi * s);
-          w[e + 1] = (T)__builtin_fmaf(hi, c, lo * s);
-        }
-        *(vec*)(y + u * V) = w;
-      } else {
-        const vec v = *(const vec*)(x + u * V), w = *(const vec*)(x + P + u * V);
-        vec p, q;
+          for (int e = 0; e < V; e += 2) {
+            const float c = cs[u * (V / 2) + e / 2], s = sn[u * (V / 2) + e / 2], lo = (float)v[e], hi = (float)v[e + 1];
+            w[e] = (T)__builtin_fmaf(lo, c, -hi * s);
+            w[e + 1] = (T)__builtin_fmaf(hi, c, lo * s);
+          }
+          *(vec*)(y + u * V) = w;
+        } else {
+          const vec v = *(const vec*)(x + u * V), w = *(const vec*)(x + P + u * V);
+          vec p, q;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float c = cs[u * V + e], s = sn[u * V + e], lo = (float)v[e], hi = (float)w[e];
-          p[e] = (T)__builtin_fmaf(lo, c, -hi * s);
-          q[e] = (T)__builtin_fmaf(hi, c, lo * s);
+          for (int e = 0; e < V; ++e) {
+            const float c = cs[u * V + e], s = sn[u * V + e], lo = (float)v[e], hi = (float)w[e];
+            p[e] = (T)__builtin_fmaf(lo, c, -hi * s);
+            q[e] = (T)__builtin_fmaf(hi, c, lo * s);
+          }
+          *(vec*)(y + u * V) = p;
+          *(vec*)(y + P + u * V) = q;
         }
-        *(vec*)(y + u * V) = p;
-        *(vec*)(y + P + u * V) = q;
-      }
-    } else {
-      if (u >= turned) {
-        const int d = 2 * P + u - turned;
-        if (!in_place) y[d] = x[d];
       } else {
-        const int a = r.interleaved ? 2 * u : u, c = r.interleaved ? 2 * u + 1 : P + u;
-        const float lo = (float)x[a], hi = (float)x[c];
-        y[a] = (T)__builtin_fmaf(lo, cs[u], -hi * sn[u]);
-        y[c] = (T)__builtin_fmaf(hi, cs[u], lo * sn[u]);
+        if (u >= turned) {
+          const int d = 2 * P + u - turned;
+          if (!in_place) y[d] = x[d];
+        } else {
+          const int a = r.interleaved ? 2 * u : u, c = r.interleaved ? 2 * u + 1 : P + u;
+          const float lo = (float)x[a], hi = (float)x[c];
+          y[a] = (T)__builtin_fmaf(lo, cs[u], -hi * sn[u]);
+          y[c] = (T)__builtin_fmaf(hi, cs[u], lo * sn[u]);
+        }
       }
     }
   }
@@ -111,7 +127,7 @@ static hipError_t rotary_of(Rotary r, hipStream_t stream) {
   const bool vectors = r.x.aligned && r.y.aligned && (r.interleaved ? 2 * r.pairs % V == 0 : r.pairs % V == 0);
   const int64_t tokens = (int64_t)r.B * r.N;
   const dim3 grid((unsigned)((tokens + r.tokens - 1) / r.tokens), (unsigned)((r.H + r.heads - 1) / r.heads));
-  const size_t lds = (size_t)r.tokens * r.pairs * 8;
+  const size_t lds = (size_t)r.tokens * (24 + r.pairs * 8);
   if (vectors) gr_rotary_kernel<T, true><<<grid, dim3(256), lds, stream>>>(r);
   else gr_rotary_kernel<T, false><<<grid, dim3(256), lds, stream>>>(r);
   return hipGetLastError();

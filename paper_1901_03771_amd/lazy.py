@@ -12,6 +12,7 @@ unchanged with this module passed in its place.
 """
 from __future__ import annotations
 
+from array import array as _array
 import builtins
 import atexit
 import ctypes
@@ -109,7 +110,7 @@ def lib():
         "gr_stream_copy": [P, P, P, SZ], "gr_stream_read": [P, P, SZ, P],
         "gr_attention": [P, PP(_Scores)] + [U64] * 6, "gr_attention_grad": [P, PP(_Scores)] + [U64] * 10,
         "gr_attention_step": [P, PP(_Scores)] + [U64] * 4,
-        "gr_rotary": [P, U64, U64, I64, PP(ctypes.c_double), I, I, I, ctypes.c_double, U64],
+        "gr_rotary": [P, U64, U64, I64, P, I, I, I, ctypes.c_double, U64],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -911,7 +912,8 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
     hx = _tensor(ctx, x)
     n = len(frequencies)
     if not isinstance(frequencies, ctypes.Array):
-        frequencies = (ctypes.c_double * builtins.max(n, 1))(*frequencies)
+        kept = _array("d", frequencies)   # (alive until the call is over)
+        frequencies = kept.buffer_info()[0]
     out = _result_array(ctx, out, x.shape if out is None else None, x.dtype_code if out is None else 0)
     arr = isinstance(positions, Array)
     st = lib().gr_rotary(ctx._p, hx, _tensor(ctx, positions) if arr else 0, 0 if arr else int(positions), frequencies, n,
