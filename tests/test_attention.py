@@ -601,3 +601,124 @@ def test_layer_trains_and_generates():
         y1 = layer.step(one[:, i].contiguous(), *cache, lengths)
         assert (y1 - whole[:, i]).norm() <= bar * whole[:, i].norm(), i
     c.close()
+
+
+def test_random_calls_are_refused_or_run(dry):
+    """Random, mostly invalid arguments: every call answers with a status, and what is refused launches nothing."""
+    import random
+    r = random.Random(11)
+    L, P = gr.lib(), dry._p
+    s = Specs(dry)
+
+    def tensor(rank=None):
+        rank = r.choice([3, 4, 4, 4, 2, 1]) if rank is None else rank
+        shape = [r.choice([0, 1, 2, 2, 2, 4, 64, 300]) for _ in range(rank)]
+        shape[-1] = r.choice([0, 1, 8, 64, 64, 100, 256, 257])
+        strides = None
+        if r.random() < 0.3:
+            strides = [r.choice([0, 1, -64, 64, 4096, 1 << 31]) for _ in range(rank)]
+            if r.random() < 0.7:
+                strides[-1] = 1
+        return s(shape, r.choice([gr.GR_F32, gr.GR_F32, gr.GR_BF16, gr.GR_I32]), strides)
+
+    whole = [s((2, 2, 2, 64), d) for d in (gr.GR_F32, gr.GR_BF16) for _ in range(8)]
+    pool = [tensor() for _ in range(60)] + whole + \
+        [s((2, 2, 2)) for _ in range(3)] + [s((2,), gr.GR_I32), s((2, 2), gr.GR_I32), s((2,)), s((2, 2, 2, 64)) + 1.0, dry.scalar(3.0)]
+    whole = [a.h for a in whole[:8]]
+    h = lambda: r.choice([0, 1 << 50] + [a.h for a in pool] * 4)  # noqa: E731
+    fine = lambda x: x if r.random() < 0.9 else r.choice([math.nan, math.inf, -1.0, 0.0, 1e300])  # noqa: E731
+    f = (ctypes.c_double * 300)(*[r.choice([0.0, 1.0, 1e300]) for _ in range(300)])
+    codes = set()
+    for _ in range(6000):
+        sc = gr._Scores(fine(0.5), fine(r.choice([0.0, 30.0])), r.choice([0, 0, h()]), r.choice([0, 1, 1, 7]), r.choice([0, 5, -(1 << 40)]),
+                        r.choice([0, 0, 0, h()]), r.choice([0, 0, 0, h()]), r.choice([0, 0, 0, h()]), r.choice([0, 0, h()]))
+        ref = ctypes.byref(sc) if r.random() < 0.98 else None
+        before = dry.stats()["kernel_launches"]
+        k = r.randrange(4)
+        g = (lambda: r.choice(whole)) if r.random() < 0.5 else h
+        if k == 0:
+            st = L.gr_attention(P, ref, g(), g(), g(), g(), r.choice([0, h()]), r.choice([0, 0, h()]))
+        elif k == 1:
+            st = L.gr_attention_grad(P, ref, g(), g(), g(), g(), r.choice([0, 0, h()]), h(), g(), g(), g(), g())
+        elif k == 2:
+            st = L.gr_attention_step(P, ref, h(), g(), g(), h())
+        else:
+            st = L.gr_rotary(P, g(), r.choice([0, h()]), r.choice([0, 7, 1 << 50]), f if r.random() < 0.95 else None, r.choice([-1, 0, 4, 32, 128, 257]), r.choice([0, 1, 5]),
+                             r.choice([0, 1]), fine(1.0), g())
+        assert 0 <= st <= 11
+        codes.add(st)
+        assert st == 0 or dry.stats()["kernel_launches"] == before or st == 9
+    assert {0, 1, 2, 3, 5, 6, 10} <= codes, codes
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,M", [(40, 17003), (17003, 40)])
+def test_documents_far_apart(ctx, N, M):
+    """Documents whose pieces lie more than 256 tiles apart, in heads enough that no split shortens the walk; the heads share their inputs."""
+    H = 256
+    g = torch.Generator().manual_seed(9)
+    q, k, v, d = (normal(70 + i, 1, n, 1, 64, dtype=BF16) for i, n in enumerate((N, M, M, N)))
+    qd, kd = torch.full((1, N), 3, dtype=torch.int32), torch.full((1, M), 3, dtype=torch.int32)
+    long, n = (kd, M) if M > N else (qd, N)
+    long[:] = torch.randint(10, 20, (1, n), generator=g, dtype=torch.int32)
+    long[0, 50:70] = 3
+    long[0, 16500:16510] = 3
+    long[0, -1] = 3
+    wide = lambda t: t.expand(t.shape[0], t.shape[1], H, 64)  # noqa: E731
+    sc = ctx.scores(documents=(ctx.array(qd.cuda()), ctx.array(kd.cuda())))
+    A = ctx.array
+    out, rest = (torch.empty(1, N, H, 64, dtype=BF16, device="cuda") for _ in range(2))
+    lse = torch.empty(1, H, N, device="cuda")
+    dq, dk, dv = (torch.empty(1, m, H, 64, dtype=BF16, device="cuda") for m in (N, M, M))
+    gr.attention(A(wide(q)), A(wide(k)), A(wide(v)), sc, out=A(out), lse=A(lse), rest=A(rest))
+    gr.attention_grad(A(wide(d)), A(wide(q)), A(wide(k)), A(wide(v)), sc, A(out), A(lse), rest=A(rest), dq=A(dq), dk=A(dk), dv=A(dv))
+    torch.cuda.synchronize()
+    ref = plain.attention(q, k, v, d, documents=(qd, kd))
+    for h in (0, 100, 255):
+        got = dict(out=out[:, :, h:h + 1], lse=lse[:, h:h + 1], dq=dq[:, :, h:h + 1], dk=dk[:, :, h:h + 1], dv=dv[:, :, h:h + 1])
+        plain.check(got, ref, BF16, 64, M, N, 1, f"head {h}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+def test_strided_masks_and_no_rest(ctx, dtype):
+    """Masks, lengths, slopes and positions with steps of their own, and a gradient without what out lost in rounding."""
+    B, N, H, HK, D = 2, 130, 4, 2, 64
+    c = dict(B=B, N=N, M=N, H=H, HK=HK, D=D, dtype=dtype)
+    q, k, v, d = tensors(c)
+    g = torch.Generator().manual_seed(21)
+    ids = torch.sort(torch.randint(0, 3, (B, N), generator=g, dtype=torch.int32), 1)[0]
+    lengths, prefix = torch.tensor([100, 130], dtype=torch.int32), torch.tensor([7, 50], dtype=torch.int32)
+    slopes = torch.tensor([0.5, 0.25, 0.0, -0.01])
+
+    def spread(t, steps):
+        big = torch.zeros([n * s for n, s in zip(t.shape, steps)], dtype=t.dtype, device="cuda")
+        view = big[tuple(slice(None, None, s) for s in steps)]
+        view.copy_(t)
+        return ctx.array(view)
+
+    sc = ctx.scores(causal=True, prefix=spread(prefix, (3,)), lengths=spread(lengths, (2,)), slopes=spread(slopes, (5,)), documents=spread(ids, (1, 3)))
+    A = ctx.array
+    out, lse = gr.attention(A(q), A(k), A(v), sc)
+    dq, dk, dv = gr.attention_grad(A(d), A(q), A(k), A(v), sc, out, lse)
+    ref = plain.attention(q, k, v, d, causal=True, prefix=prefix, lengths=lengths, slopes=slopes, documents=ids)
+    got = dict(out=out.torch(), lse=lse.torch(), dq=dq.torch(), dk=dk.torch(), dv=dv.torch())
+    plain.check(got, ref, dtype, D, N, N, H // HK, "strided masks")
+    # positions transposed, and rotary through them
+    pos = torch.randint(0, 5000, (N, B), generator=g, dtype=torch.int32).cuda().T
+    f = gr.rotary_frequencies(D)
+    y = gr.rotary(A(q), f, A(pos)).torch().cpu().double()
+    want = plain.rotary(q, f, pos.cpu().numpy())
+    assert ((y - want).abs() <= plain.HALF[dtype] * want.abs() + 1e-5 * q.abs().max().item()).all()
+
+
+@pytest.mark.gpu
+def test_many_rows_against_plain(ctx):
+    """A long row whose walks have many tiles, heads shared and not, every option at once."""
+    for dtype, D, H, HK in ((BF16, 128, 4, 2), (F32, 64, 2, 2)):
+        c = dict(B=1, N=2500, M=2500, H=H, HK=HK, D=D, dtype=dtype, grad=True, cap=15.0, causal=True, slopes=True, prefix=True, documents=3)
+        q, k, v, d = tensors(c)
+        kw = options(c)
+        got = run_case(ctx, c, q, k, v, d, kw)
+        ref = plain.attention(q, k, v, d, **kw)
+        plain.check(got, ref, dtype, D, 2500, 2500, H // HK, f"{D}", cap=15.0)
