@@ -8,6 +8,9 @@
 // still count in the gradients of keys that every query all but ignores; there is room for it above.
 // They form q k^T and dout v^T twice, 7 products of the size of q k^T where a single kernel would have 5 and an addition to dq in memory
 // per tile.
+//
+// Measured, bfloat16, 16 heads of 8192 causal rows of 128 values, a beginning seen whole: dq 0.45 ms (matrix cores busy 53 % of the cycles), dk and dv 0.73 ms (42 %, waiting 49 %: operands of
+// both sides and both sums fill 256 registers a lane, nothing is read ahead from LDS).
 #pragma once
 
 #include "attention_kernels.h"
