@@ -18,6 +18,8 @@ namespace gr {
 namespace attn {
 
 constexpr int64_t LIMIT = (int64_t(1) << 30) - 512;   // rows of queries of one head of k, and keys
+constexpr int64_t THREADS = int64_t(1) << 32;         // what a launch may not reach
+constexpr int64_t GROUPS = THREADS / 512 - 8;         // workgroups of the largest size (and what grid_of rounds up)
 
 struct Call {
   gr_ctx* ctx;
@@ -276,6 +278,7 @@ static gr_status take_scores(Call& c, const gr_scores* s, Args* a, bool step) {
   if (s->q_documents) {
     TRY(c.take(s->q_documents, "q_documents", GR_I32, {a->B, a->N}, false));
     TRY(c.take(s->k_documents, "k_documents", GR_I32, {a->B, a->M}, false));
+    if (a->B * (padded_rows(a->M) + padded_rows(a->N)) >= THREADS) return c.error(GR_ERR_UNSUPPORTED, "more than 2^32 document numbers");
   }
   return GR_OK;
 }
@@ -348,7 +351,7 @@ static gr_status forward(Call& c, Args& a, int type, int mode) {
   const int64_t tiles = ((int64_t)a.M + keys - 1) / keys;
   a.splits = divided ? token_splits_of(pairs * a.blocks, tiles) : splits_of(pairs * a.blocks, tiles, MAX_SPLITS, forward_per_cu(size, dp));
   const int64_t blocks = (int64_t)a.blocks * a.splits;
-  if (blocks * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
+  if (blocks * pairs > GROUPS) return c.error(GR_ERR_UNSUPPORTED, "more than 2^23 blocks of rows");
   const size_t sums = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * dp * 4) : 0, ml = a.splits > 1 ? rounded((size_t)a.splits * pairs * rows * 8) : 0;
   Documents docs(a);
   char* ws;
@@ -472,7 +475,7 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   const int64_t units = (((int64_t)a.N + tile - 1) / tile) * a.G;
   int ksplits = splits_of(pairs * kblocks, units, 16, grad_kv_per_cu(size, dp));
   if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));
-  if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > LIMIT / 4) return c.error(GR_ERR_UNSUPPORTED, "more than 2^28 blocks of rows");
+  if (std::max(qblocks * qsplits, kblocks * ksplits) * pairs > GROUPS || a.B * padded_rows(a.N) * a.H * 16 >= THREADS) return c.error(GR_ERR_UNSUPPORTED, "more than 2^23 blocks of rows");
   const size_t st = rounded((size_t)a.B * a.H * padded_rows(a.N) * 4);
   Documents docs(a);
   const size_t parts = std::max(ksplits > 1 ? rounded((size_t)ksplits * 2 * pairs * a.M * dp * 4) : 0, qsplits > 1 ? rounded((size_t)qsplits * pairs * rows * dp * 4) : 0);

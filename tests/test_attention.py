@@ -124,6 +124,29 @@ def test_refusals(dry):
     assert L.gr_attention(None, None, u(1), u(1), u(1), u(1), u(0), u(0)) == 6
 
 
+def test_calls_beyond_a_launch_are_refused(dry):
+    """2^24 heads and documents of 2^32 entries: no launch holds them; nothing is launched."""
+    a = lambda B, N, H, t=gr.GR_F32: dry.from_device(1 << 40, t, (B, N, H, 64))  # noqa: E731
+    at = [1 << 41]
+
+    def result(*shape):
+        at[0] += 1 << 44
+        return dry.from_device(at[0], gr.GR_F32, shape)
+
+    n = dry.stats()["kernel_launches"]
+    B = 1 << 24
+    refused("GR_ERR_UNSUPPORTED", gr.attention, a(B, 1, 1), a(B, 1, 1), a(B, 1, 1), dry.scores(), out=result(B, 1, 1, 64), lse=result(B, 1, 1))
+    refused("GR_ERR_UNSUPPORTED", gr.attention_step, dry.from_device(1 << 40, gr.GR_F32, (B, 1, 64)), a(B, 1, 1), a(B, 1, 1), dry.scores(lengths=dry.from_device(1 << 40, gr.GR_I32, (B,))),
+            out=result(B, 1, 64))
+    B = 1 << 21
+    refused("GR_ERR_UNSUPPORTED", gr.attention_grad, *[a(B, 1, 1)] * 4, dry.scores(), a(B, 1, 1), dry.from_device(1 << 40, gr.GR_F32, (B, 1, 1)),
+            **{w: result(B, 1, 1, 64) for w in ("dq", "dk", "dv")})
+    ids = lambda n: dry.from_device(1 << 40, gr.GR_I32, (1 << 20, n), (0, 1))  # noqa: E731
+    wide = lambda n: dry.from_device(1 << 40, gr.GR_F32, (1 << 20, n, 1, 64), (0, 64, 64, 1))  # noqa: E731
+    refused("GR_ERR_UNSUPPORTED", gr.attention, wide(1), wide(8192), wide(8192), dry.scores(documents=(ids(1), ids(8192))), out=result(1 << 20, 1, 1, 64), lse=result(1 << 20, 1, 1))
+    assert dry.stats()["kernel_launches"] == n
+
+
 def test_without_a_device_arguments_are_checked_first():
     c = gr.Context(device=-1)
     s = Specs(c)
