@@ -471,7 +471,8 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   const int64_t tile = tile_rows(size, dp);
   const int qsplits = splits_of(pairs * qblocks, ((int64_t)a.M + tile - 1) / tile, 16, grad_q_per_cu(size, dp));
   // For dk and dv, where a workgroup walks the queries of G heads, from every place on to the end: more and shorter walks even out what causal
-  // masks and documents leave of them.
+  // masks and documents leave of them (2 x 4096 rows in 6 documents, 16 heads on 4 of 128 bfloat16 values, 256 blocks: 746 us in one part, 267 in four
+  // with their sum).  From 1024 blocks on there are several turns of them anyway, and the parts cost what they give.
   const int64_t units = (((int64_t)a.N + tile - 1) / tile) * a.G;
   int ksplits = splits_of(pairs * kblocks, units, 16, grad_kv_per_cu(size, dp));
   if (pairs * kblocks >= 256 && pairs * kblocks < 1024 && (a.causal || a.kdoc)) ksplits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / (pairs * kblocks), units / 16));

@@ -164,6 +164,7 @@ class Context:
             self._cell = _fastbind.Cell()  # what the C fast paths read; 0 once closed
             self._cell.address = self._p.value or 0
         self.device = int(device)
+        self._stream = stream or 0
         self._programs = set()  # recorded requests (Program): they die with the context
         _LIVE.add(self)
 
@@ -228,6 +229,7 @@ class Context:
 
     def set_stream(self, stream: int):
         self.check(lib().gr_ctx_set_stream(self._p, ctypes.c_void_p(stream)))
+        self._stream = stream or 0
 
     def sync(self):
         self.check(lib().gr_sync(self._p))
@@ -826,12 +828,18 @@ def _tensor(ctx: Context, a: "Array") -> int:
 
 
 def _result_array(ctx: Context, given, shape, dtype: int) -> "Array":
-    """The array that a call writes: the caller's, or a new one over memory from torch."""
+    """The array that a call writes: the caller's, or a new one over memory from torch, which hands a stream the memory that work queued on
+    that stream was the last to use: it is taken for the stream of the context, whichever is torch's at the time."""
     if given is not None:
         return given
     torch = _torch()
-    a = ctx.array(torch.empty(shape, device=f"cuda:{ctx.device}",
-                              dtype={GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]))
+    dtype = {GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]
+    if ctx.device < 0 or torch.cuda.current_stream(ctx.device).cuda_stream == ctx._stream:
+        t = torch.empty(shape, device=f"cuda:{ctx.device}", dtype=dtype)
+    else:
+        with torch.cuda.stream(torch.cuda.ExternalStream(ctx._stream, ctx.device)):
+            t = torch.empty(shape, device=f"cuda:{ctx.device}", dtype=dtype)
+    a = ctx.array(t)
     a._view = True   # nobody else holds the tensor: the handle keeps it through materialize() and torch()
     return a
 

@@ -745,3 +745,32 @@ def test_many_rows_against_plain(ctx):
         got = run_case(ctx, c, q, k, v, d, kw)
         ref = plain.attention(q, k, v, d, **kw)
         plain.check(got, ref, dtype, D, 2500, 2500, H // HK, f"{D}", cap=15.0)
+
+
+@pytest.mark.gpu
+def test_new_results_belong_to_the_stream_of_the_context():
+    """A context on a stream of its own, called while torch's is another: the memory of its results is not what torch's stream still works on."""
+    x = normal(5, 2, 64, 4, 64)
+    torch.cuda.synchronize()
+    f = gr.rotary_frequencies(64)
+    side = torch.cuda.Stream()
+    for ours, theirs in ((side, torch.cuda.default_stream()), (torch.cuda.default_stream(), side)):
+        with torch.cuda.stream(ours):
+            c = gr.Context()
+        with torch.cuda.stream(theirs):
+            big = torch.ones(4096, 4096, device="cuda")
+            old = torch.empty_like(x)
+            at = old.data_ptr()
+            for _ in range(20):
+                big = big @ big * 2.0 ** -12
+            old.fill_(9.0)   # still queued when the memory goes back to torch
+            del old
+            y = gr.rotary(c.array(x), f, 3)
+            q = c.array(x)
+            out, lse = gr.attention(q, q, q, c.scores())
+            assert at not in (y.data_ptr()[0], out.data_ptr()[0])   # (torch() would copy, into memory of its own)
+        torch.cuda.synchronize()
+        ref = plain.rotary(x, f, torch.arange(64).numpy()[None] + 3)
+        assert ((y.torch().cpu().double() - ref).abs() <= plain.HALF[F32] * ref.abs() + 8 * 2.0 ** -24 * x.abs().amax().item()).all()
+        plain.check(dict(out=out.torch(), lse=lse.torch()), plain.attention(x, x, x), F32, 64, 64, 64, 1, "stream")
+        c.close()
