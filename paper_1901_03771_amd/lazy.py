@@ -919,7 +919,7 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
     ctx = x.ctx
     hx = _tensor(ctx, x)
     n = len(frequencies)
-    if not isinstance(frequencies, ctypes.Array):
+    if not (isinstance(frequencies, ctypes.Array) and frequencies._type_ is ctypes.c_double):
         kept = _array("d", frequencies)   # (alive until the call is over)
         frequencies = kept.buffer_info()[0]
     out = _result_array(ctx, out, x.shape if out is None else None, x.dtype_code if out is None else 0)

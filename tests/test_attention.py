@@ -195,6 +195,14 @@ def test_frequencies():
         gr.rotary_frequencies(7)
 
 
+@pytest.mark.parametrize("of", [list, tuple, lambda f: (ctypes.c_float * len(f))(*f), lambda f: torch.tensor(f), lambda f: torch.tensor(f).numpy()])
+def test_frequencies_of_every_kind_are_read_as_numbers(dry, of):
+    """Also arrays of single precision, which are half as long: what is not finite in them is found, what is finite is taken."""
+    x = Specs(dry)((1, 4, 2, 64))
+    gr.rotary(x, of([0.5] * 32), 5, out=x)
+    refused("GR_ERR_ARG", gr.rotary, x, of([math.inf] * 32), 5, out=x)
+
+
 def test_reference_gradient_against_differences():
     """The formulas that the kernels are compared with, against central differences of the plain output."""
     g = torch.Generator().manual_seed(3)
