@@ -3,6 +3,7 @@
 #include "attention.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -518,7 +519,7 @@ static gr_status rotary_call(gr_ctx* ctx, gr_array x, gr_array positions, int64_
   if (pairs < 0 || pairs > MAX_PAIRS || (pairs > 0 && !frequencies)) return c.error(GR_ERR_ARG, "0 to 256 pairs, with a frequency each");
   if (2 * (int64_t)pairs > D) return c.error(GR_ERR_SHAPE, "a head has fewer than 2 pairs values");
   if ((interleaved != 0 && interleaved != 1) || (inverse != 0 && inverse != 1)) return c.error(GR_ERR_ARG, "interleaved and inverse must be 0 or 1");
-  if (!std::isfinite(factor)) return c.error(GR_ERR_ARG, "factor must be finite");
+  if (!(std::fabs(factor) <= FLT_MAX)) return c.error(GR_ERR_ARG, "factor must be a finite float32");
   if (position < -(int64_t(1) << 40) || position > (int64_t(1) << 40)) return c.error(GR_ERR_ARG, "position beyond 2^40");
   for (int i = 0; i < pairs; ++i) if (!std::isfinite(frequencies[i])) return c.error(GR_ERR_ARG, "a frequency is not finite");
   if (B > LIMIT || N > LIMIT || D > LIMIT || B * N > LIMIT) return c.error(GR_ERR_UNSUPPORTED, "more than 2^30 tokens or values of a head");

@@ -16,6 +16,7 @@ from array import array as _array
 import builtins
 import atexit
 import ctypes
+import operator
 import weakref
 import os
 from typing import Optional, Sequence
@@ -802,6 +803,14 @@ def min(a, axis=None, keepdims=False): return _reduce(34, a, axis, keepdims)  # 
 
 # ---- attention and rotary positions (include/grumpy_hip_attention.h) ----------------------------------------------------
 
+def _place(position) -> int:
+    """A position as the C calls take it, which check its range: none is cut to 64 bits on the way."""
+    position = operator.index(position)
+    if position.bit_length() > 63:
+        raise GrError(6, "a position beyond 64 bits")
+    return position
+
+
 class Scores:
     """gr_scores: the description that the calls below take.  Keeps the arrays it names."""
 
@@ -813,9 +822,11 @@ class Scores:
         self._keep = (slopes, prefix, qd, kd, lengths)
         h = [0 if a is None else _operand(ctx, a).h for a in self._keep]
         self._scale = scale
-        self._c = _Scores(0.0 if scale is None else scale, cap, h[0], builtins.bool(causal), position, h[1], h[2], h[3], h[4])
+        self._c = _Scores(0.0 if scale is None else scale, cap, h[0], builtins.bool(causal), _place(position), h[1], h[2], h[3], h[4])
 
-    def _for(self, d: int):
+    def _for(self, ctx: Context, d: int):
+        if self.ctx is not ctx:   # (its handles are numbers of that context, which may be other arrays' here)
+            raise ValueError("scores and arrays belong to different contexts")
         if self._scale is None:
             self._c.scale = builtins.max(d, 1) ** -0.5
         return ctypes.byref(self._c)
@@ -859,7 +870,7 @@ def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=
         lse = _result_array(ctx, None, (shape[0], shape[2], shape[1]), GR_F32)
     elif lse is False:
         lse = None
-    st = lib().gr_attention(ctx._p, scores._for(d), hq, hk, hv, _tensor(ctx, out), 0 if lse is None else _tensor(ctx, lse),
+    st = lib().gr_attention(ctx._p, scores._for(ctx, d), hq, hk, hv, _tensor(ctx, out), 0 if lse is None else _tensor(ctx, lse),
                             0 if rest is None else _tensor(ctx, rest))
     if st:
         ctx.check(st)
@@ -876,7 +887,7 @@ def attention_grad(dout: "Array", q: "Array", k: "Array", v: "Array", scores: Sc
     dq = _result_array(ctx, dq, q.shape if dq is None else None, q.dtype_code if dq is None else 0)
     dk = _result_array(ctx, dk, k.shape if dk is None else None, k.dtype_code if dk is None else 0)
     dv = _result_array(ctx, dv, v.shape if dv is None else None, v.dtype_code if dv is None else 0)
-    st = lib().gr_attention_grad(ctx._p, scores._for(q.shape[-1] if scores._scale is None else 0), *h,
+    st = lib().gr_attention_grad(ctx._p, scores._for(ctx, q.shape[-1] if scores._scale is None else 0), *h,
                                  _tensor(ctx, dq), _tensor(ctx, dk), _tensor(ctx, dv))
     if st:
         ctx.check(st)
@@ -888,7 +899,7 @@ def attention_step(q: "Array", k: "Array", v: "Array", scores: Scores, out=None)
     ctx = q.ctx
     h = [_tensor(ctx, a) for a in (q, k, v)]
     out = _result_array(ctx, out, q.shape if out is None else None, q.dtype_code if out is None else 0)
-    st = lib().gr_attention_step(ctx._p, scores._for(q.shape[-1] if scores._scale is None else 0), *h, _tensor(ctx, out))
+    st = lib().gr_attention_step(ctx._p, scores._for(ctx, q.shape[-1] if scores._scale is None else 0), *h, _tensor(ctx, out))
     if st:
         ctx.check(st)
     return out
@@ -924,7 +935,7 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
         frequencies = kept.buffer_info()[0]
     out = _result_array(ctx, out, x.shape if out is None else None, x.dtype_code if out is None else 0)
     arr = isinstance(positions, Array)
-    st = lib().gr_rotary(ctx._p, hx, _tensor(ctx, positions) if arr else 0, 0 if arr else int(positions), frequencies, n,
+    st = lib().gr_rotary(ctx._p, hx, _tensor(ctx, positions) if arr else 0, 0 if arr else _place(positions), frequencies, n,
                          builtins.bool(interleaved), builtins.bool(inverse), factor, _tensor(ctx, out))
     if st:
         ctx.check(st)

@@ -203,6 +203,38 @@ def test_frequencies_of_every_kind_are_read_as_numbers(dry, of):
     refused("GR_ERR_ARG", gr.rotary, x, of([math.inf] * 32), 5, out=x)
 
 
+def test_numbers_are_not_cut_to_fit(dry):
+    x = Specs(dry)((1, 4, 2, 64))
+    f = gr.rotary_frequencies(64)
+    for p in (1 << 64, 1 << 70, -(1 << 64), 1 << 41):
+        refused("GR_ERR_ARG", gr.rotary, x, f, p, out=x)
+    for p in (1 << 64, -(1 << 70)):
+        refused("GR_ERR_ARG", dry.scores, position=p)
+    for p in (2.5, "3"):
+        with pytest.raises(TypeError):
+            gr.rotary(x, f, p, out=x)
+        with pytest.raises(TypeError):
+            dry.scores(position=p)
+    for factor in (1e39, -1e300, math.inf, math.nan):
+        refused("GR_ERR_ARG", gr.rotary, x, f, 5, factor=factor, out=x)
+
+
+def test_scores_of_another_context(dry):
+    """Handles are numbers of a context: the same number names another array in the next."""
+    other = gr.Context(device=-1)
+    s = Specs(dry)
+    q, o, lse = s((1, 4, 2, 64)), s((1, 4, 2, 64)), s((1, 2, 4))
+    slopes = Specs(other)((2,))
+    for sc in (other.scores(slopes=slopes), other.scores()):
+        with pytest.raises(ValueError):
+            gr.attention(q, q, q, sc, out=o, lse=lse)
+        with pytest.raises(ValueError):
+            gr.attention_grad(q, q, q, q, sc, q, lse, dq=o, dk=s((1, 4, 2, 64)), dv=s((1, 4, 2, 64)))
+        with pytest.raises(ValueError):
+            gr.attention_step(s((1, 2, 64)), q, q, sc, out=s((1, 2, 64)))
+    other.close()
+
+
 def test_reference_gradient_against_differences():
     """The formulas that the kernels are compared with, against central differences of the plain output."""
     g = torch.Generator().manual_seed(3)
