@@ -38,9 +38,9 @@ extern "C" {
  * at position j (gr_attention_step: p = lengths[b] - 1).
  *   score = scale * (q . k);  capped: cap * tanh(score / cap);  then - slopes[h] * |p - j|
  *   key j is seen if (not causal, or j <= p, or j < prefix[b]), and j < lengths[b], and the documents are the same
- * What stands in a place that no query sees has no say: rows of k and v from lengths[b] on are not read, a score that is
- * masked is replaced whatever it is.  (Where one query sees a key and another does not, a v, or in the gradient a
- * k or v, that is infinite or NaN may reach both, as 0 * inf does in a plain product.) */
+ * Rows of k and v from lengths[b] on are not read, and a score that is masked is replaced whatever it is: a k that is infinite
+ * or NaN has no say in out and lse of the queries that do not see it.  (A v below lengths[b], or in the gradient a k, v, q or dout, that
+ * is infinite or NaN may reach rows of its tile that do not see it, as 0 * inf does in a plain product.) */
 typedef struct {
   double scale;         /* > 0 and finite */
   double cap;           /* 0 = none; > 0 and finite */

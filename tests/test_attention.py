@@ -814,3 +814,26 @@ def test_new_results_belong_to_the_stream_of_the_context():
         assert ((y.torch().cpu().double() - ref).abs() <= plain.HALF[F32] * ref.abs() + 8 * 2.0 ** -24 * x.abs().amax().item()).all()
         plain.check(dict(out=out.torch(), lse=lse.torch()), plain.attention(x, x, x), F32, 64, 64, 64, 1, "stream")
         c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_masked_scores_are_replaced(ctx, dtype, bad):
+    """Keys that are not numbers where documents, causal order and capped or plain scores leave them unseen."""
+    c = dict(B=1, N=96, M=96, H=4, HK=2, D=64, dtype=dtype, grad=False)
+    q, k, v, d = tensors(c)
+    ids = torch.zeros(1, 96, dtype=torch.int32)
+    ids[0, 20:50] = -1
+    late = torch.tensor([90], dtype=torch.int32)
+    for kw in (dict(documents=(torch.zeros(1, 96, dtype=torch.int32), ids)), dict(documents=(torch.zeros(1, 96, dtype=torch.int32), ids), cap=10.0),
+               dict(causal=True, position=-10), dict(causal=True, position=-10, cap=10.0, prefix=late - 10)):
+        clean = run_case(ctx, c, q, k, v, d, kw)
+        dirty = k.clone()
+        if "documents" in kw:
+            dirty[0, 20:50] = bad
+        else:
+            dirty[0, 86:] = bad
+        got = run_case(ctx, c, q, dirty, v, d, kw)
+        for w in clean:
+            assert torch.equal(clean[w], got[w]), (kw, w)
