@@ -223,7 +223,8 @@ static bool resolved(gr_ctx* ctx, gr_array a) {
   return stored_view(lookup(ctx, a), &v);
 }
 
-// Operands that are stored already have rows whose values are neighbours (those still to be evaluated will).
+// Operands that are stored already have rows whose values are neighbours.  (Those still to be evaluated are looked at when they are: their own
+// storage is dense, but a view of an expression stays a view of it.)
 static gr_status rows_are_neighbours(Call& c, std::initializer_list<gr_array> arrays) {
   for (gr_array a : arrays) {
     Tensor t;
@@ -454,6 +455,7 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   if (rest) TRY(rows_are_neighbours(c, {rest}));
   if (resolved(ctx, lse)) TRY(contiguous_stats(c, lse));
   TRY(c.settle());
+  TRY(contiguous_stats(c, lse));   // (a view of an expression has its steps only now)
   TRY(c.tensor(q, "q", &a.q));
   TRY(c.tensor(k, "k", &a.k));
   TRY(c.tensor(v, "v", &a.v));

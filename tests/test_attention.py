@@ -147,6 +147,25 @@ def test_calls_beyond_a_launch_are_refused(dry):
     assert dry.stats()["kernel_launches"] == n
 
 
+@pytest.mark.parametrize("of", ["slice", "transpose", "scan"])
+def test_lazy_views_of_lse_are_looked_at_once_evaluated(dry, of):
+    """A view of an expression keeps its steps when the expression is evaluated: one that is not dense is refused, like one of a stored array."""
+    s = Specs(dry)
+    q, k, v, o, do = (s((1, 8, 2, 64)) for _ in range(5))
+    dense = lambda: gr.dot(s((2, 8)), s((8, 8)))  # noqa: E731
+    lse = {"slice": lambda: gr.reshape(gr.dot(s((2, 8)), s((8, 16))), (1, 2, 16))[:, :, :8],
+           "transpose": lambda: gr.reshape(gr.dot(s((8, 2)), s((2, 2))), (8, 2, 1)).T,
+           "scan": lambda: s((1, 2, 16)).cumsum(2)[:, :, :8]}[of]()
+    assert lse.shape == (1, 2, 8)
+    results = lambda: {w: s((1, 8, 2, 64)) for w in ("dq", "dk", "dv")}  # noqa: E731
+    refused("GR_ERR_UNSUPPORTED", gr.attention_grad, do, q, k, v, dry.scores(), o, lse, **results())
+    refused("GR_ERR_UNSUPPORTED", gr.attention_grad, do, q, k, v, dry.scores(), o, lse, **results())   # (stored by now)
+    gr.attention_grad(do, q, k, v, dry.scores(), o, gr.reshape(dense(), (1, 2, 8)), **results())
+    # values of a row that are not neighbours are refused likewise
+    wide = gr.reshape(gr.dot(s((8, 8)), s((8, 256))), (1, 8, 2, 128))[:, :, :, ::2]
+    refused("GR_ERR_UNSUPPORTED", gr.attention, wide, k, v, dry.scores(), out=s((1, 8, 2, 64)), lse=False)
+
+
 def test_without_a_device_arguments_are_checked_first():
     c = gr.Context(device=-1)
     s = Specs(c)
