@@ -40,7 +40,8 @@ extern "C" {
  *   key j is seen if (not causal, or j <= p, or j < prefix[b]), and j < lengths[b], and the documents are the same
  * Rows of k and v from lengths[b] on are not read, and a score that is masked is replaced whatever it is: a k that is infinite
  * or NaN has no say in out and lse of the queries that do not see it.  (A v below lengths[b], or in the gradient a k, v, q or dout, that
- * is infinite or NaN may reach rows of its tile that do not see it, as 0 * inf does in a plain product.) */
+ * is infinite or NaN may reach rows of its tile that do not see it, as 0 * inf does in a plain product.)
+ * A query that is NaN, or sees a score that is NaN or +inf, has NaN in out and lse, at every size. */
 typedef struct {
   double scale;         /* > 0 and finite */
   double cap;           /* 0 = none; > 0 and finite */

@@ -189,10 +189,12 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
         for (int d = 0; d < L::BLOCKS; ++d) o[d] *= by;
       }
       float less = m == -INF ? 0.0f : m;
-      // (scores of 2^20 and more: m is rounded by as much as an exponent counts, so the difference is taken before the product)
+      // (scores of 2^20 and more: m is rounded by as much as an exponent counts, so the difference is taken before the product; of those rows
+      // only, which leaves every row the bits that it would have beside any others)
       if (__any(__builtin_fabsf(less) > 1048576.0f)) {
-        const float by = my == -INF ? 0.0f : my;
-        less = 0.0f;
+        const bool far = __builtin_fabsf(less) > 1048576.0f;
+        const float by = far ? my : 0.0f;
+        less = far ? 0.0f : less;
 #pragma unroll
         for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
@@ -228,6 +230,9 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   }
   finished(o);
   l = sum_halves(l);
+  // A maximum passes over scores that are not numbers, the sum does not: where it is none, the maximum is made none too, so that a row or a part
+  // of one that saw NaN is told from one that saw nothing (m = -inf, l = 0) wherever they are joined.
+  if (l != l) m = l;
 
   if constexpr (DIVIDED) {
     // the waves' sums: each scaled to the largest maximum, added in the order of the waves
@@ -266,7 +271,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
         for (int e = 0; e < 4; ++e) o[d][r + e] = x[e];
       }
     }
-    m = top;
+    m = total != total ? total : top;
     l = total;
   }
 

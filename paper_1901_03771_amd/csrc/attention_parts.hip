@@ -7,16 +7,18 @@ namespace attn {
 // out and lse of a row from the splits' (m, l, sums): each scaled to the largest m, added in the order of the splits.  With more than 16 splits a
 // workgroup has one row: its threads read the splits' (m, l) once, a split each, then 256 / quads runs of splits are summed side by side for every four
 // values and joined in order.  (Threads that each walked all splits of four values took 68 us for 128 splits of 8 rows, a chain of 128 reads.)
+// A split that saw nothing has m = -inf and counts for nothing; one that saw NaN has m = l = NaN, which a maximum passes over and every sum keeps:
+// l = 0 is a row that saw nothing.
 template <class T>
 static __device__ __forceinline__ void finish_row(const Args& a, int64_t row, int d, const f32x4& x, float m, float l) {
   const int R = a.N * a.G;
   const int pair = (int)(row / R), r = (int)(row - (int64_t)pair * R), i = r / a.G, g = r - i * a.G, b = pair / a.HK, h = (pair - b * a.HK) * a.G + g;
-  const float inv = m == -INF ? 0.0f : 1.0f / l;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   float o[4], y[4];
   for (int e = 0; e < 4; ++e) { o[e] = x[e] * inv; y[e] = o[e] - (float)(T)o[e]; }
   store4(at<T>(a.out, b, i, h), d, a.D, o, a.out.aligned);
   if (a.rest.p) store4(at<T>(a.rest, b, i, h), d, a.D, y, a.rest.aligned);
-  if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = m == -INF ? -INF : (m + log2_(l)) * LN2;
+  if (a.lse && d == 0) a.lse[((int64_t)b * a.H + h) * a.N + i] = l == 0.0f ? -INF : (m + log2_(l)) * LN2;
 }
 
 template <class T>

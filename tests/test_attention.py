@@ -856,3 +856,87 @@ def test_masked_scores_are_replaced(ctx, dtype, bad):
         got = run_case(ctx, c, q, dirty, v, d, kw)
         for w in clean:
             assert torch.equal(clean[w], got[w]), (kw, w)
+
+
+# rows of queries, keys, heads, heads of k: calls of one part, of 2 to 16, of more, with a join of waves and without
+PARTS = [(40, 40, 4, 2), (40, 500, 4, 2), (3, 90, 2, 2), (3, 1500, 64, 8), (3, 6000, 2, 1), (150, 6000, 2, 1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("N,M,H,HK", PARTS)
+def test_nan_that_is_seen_stays(ctx, N, M, H, HK, dtype):
+    """A query, a key or a stretch of keys that is not a number: NaN in out and lse of the rows that see it, the same bits as before in all others,
+    however many parts the keys are divided into."""
+    D = 64
+    c = dict(B=2, N=N, M=M, H=H, HK=HK, D=D, dtype=dtype, grad=False)
+    q, k, v, d = tensors(c)
+    kw = dict(causal=True, position=M - N)
+    clean = run_case(ctx, c, q, k, v, d, kw)
+    assert torch.isfinite(clean["out"]).all() and torch.isfinite(clean["lse"]).all()
+    G = H // HK
+
+    def check(got, hit, what):   # hit (B, N, H): rows that have to be NaN
+        assert torch.isnan(got["out"][hit]).all() and torch.isnan(got["lse"].transpose(1, 2)[hit]).all(), what
+        assert torch.equal(got["out"][~hit], clean["out"][~hit]), what
+        assert torch.equal(got["lse"].transpose(1, 2)[~hit], clean["lse"].transpose(1, 2)[~hit]), what
+
+    for bad in (math.nan, math.inf):
+        t = q.clone()
+        t[1, N - 2, 1, 5] = bad
+        hit = torch.zeros(2, N, H, dtype=torch.bool, device="cuda")
+        hit[1, N - 2, 1] = True
+        check(run_case(ctx, c, t, k, v, d, kw), hit, f"query {bad}")
+    place = torch.arange(N, device="cuda") + M - N
+    for first, last in ((M - 2, M - 1), (0, 1), (M // 2, M - N)):   # a late key, the first one, and a stretch that fills whole parts
+        if first >= last:
+            continue
+        t = k.clone()
+        t[0, first:last, HK - 1] = math.nan
+        hit = torch.zeros(2, N, H, dtype=torch.bool, device="cuda")
+        hit[0, :, (HK - 1) * G:] = (place >= first)[:, None]
+        check(run_case(ctx, c, q, t, v, d, kw), hit, f"keys {first} .. {last}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("M", [40, 700, 40000])
+def test_nan_in_single_tokens_stays(ctx, M, dtype):
+    q, k, v = normal(1, 2, 4, 64, dtype=dtype), normal(2, 2, M, 1, 64, dtype=dtype), normal(3, 2, M, 1, 64, dtype=dtype)
+    lengths = torch.tensor([M, M - 3], dtype=torch.int32)
+
+    def step(q, k):
+        out = torch.full_like(q, 7.0)
+        gr.attention_step(ctx.array(q), ctx.array(k), ctx.array(v), on_gpu(ctx, dict(lengths=lengths)), out=ctx.array(out))
+        return out
+
+    clean = step(q, k)
+    assert torch.isfinite(clean).all()
+    t = q.clone()
+    t[1, 2, 9] = math.nan
+    got = step(t, k)
+    assert torch.isnan(got[1, 2]).all()
+    got[1, 2] = clean[1, 2]
+    assert torch.equal(got, clean)
+    t = k.clone()
+    t[0, M // 3:M // 2] = math.nan
+    got = step(q, t)
+    assert torch.isnan(got[0]).all() and torch.equal(got[1], clean[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+def test_gradient_of_a_nan_row(ctx, dtype):
+    """The rows and keys that a NaN query reaches are NaN in the gradient, the others are as they were; queries split and not."""
+    for N, M, H in ((40, 40, 2), (40, 2500, 1)):
+        c = dict(B=2, N=N, M=M, H=H, HK=H, D=64, dtype=dtype, grad=True)
+        q, k, v, d = tensors(c)
+        clean = run_case(ctx, c, q, k, v, d, {})
+        q[1, 7, 0] = math.nan
+        got = run_case(ctx, c, q, k, v, d, {})
+        assert torch.isnan(got["dq"][1, 7, 0]).all() and torch.isnan(got["dk"][1, :, 0]).all() and torch.isnan(got["dv"][1, :, 0]).all()
+        for w in ("dq", "dk", "dv"):
+            assert torch.equal(got[w][0], clean[w][0]), w
+            assert torch.equal(got[w][1, :, 1:], clean[w][1, :, 1:]), w
+        keep = torch.arange(N) != 7
+        assert torch.equal(got["dq"][1][keep], clean["dq"][1][keep])
