@@ -295,15 +295,16 @@ static int fill_scores(Call& c, const gr_scores* s, int type, Args* a) {
   a->place = (int)std::max<int64_t>(-(int64_t(1) << 30), std::min<int64_t>(s->position, int64_t(1) << 30));
   a->causal = s->causal;
   const double log2e = 1.4426950408889634;
+  const bool wide = type == TYPE_BF16 && s->cap > SHORT_CAP;
   a->scale = (float)s->scale;
   if (s->cap > 0.0) {
     a->c = (float)(s->cap * log2e);
-    // (bfloat16: what the hardware's power of two takes; float32: the argument of the tanh)
-    a->cin = (float)(type == TYPE_BF16 ? 2.0 * log2e * s->scale / s->cap : s->scale / s->cap);
+    // (the short form takes what the hardware's power of two does)
+    a->cin = (float)(type == TYPE_BF16 && !wide ? 2.0 * log2e * s->scale / s->cap : s->scale / s->cap);
   } else {
     a->c = (float)(s->scale * log2e);
   }
-  return (s->cap > 0.0 ? MODE_CAP : 0) | (s->slopes ? MODE_BIAS : 0);
+  return (s->cap > 0.0 ? MODE_CAP : 0) | (s->slopes ? MODE_BIAS : 0) | (wide ? MODE_WIDE : 0);
 }
 
 static int keys_of(bool divided, int size, int dp) { return divided ? 32 * shared_waves(size, dp) : tile_rows(size, dp); }

@@ -44,10 +44,11 @@ struct Args {
   int splits = 1, blocks = 0;    // splits of the keys (for dk and dv: of the queries), blocks of rows (of keys) of a head
   float scale = 1.0f;
   float c = 0.0f;                // binary logarithm units: scale * log2(e), or cap * log2(e) where scores are capped
-  float cin = 0.0f;              // argument of the tanh, in the unit that its form takes
+  float cin = 0.0f;              // a product times this is the argument of the tanh, in the unit that its form takes
 };
 
-enum { MODE_CAP = 1, MODE_BIAS = 2 };
+enum { MODE_CAP = 1, MODE_BIAS = 2, MODE_WIDE = 4 };   // wide: bfloat16 with a cap beyond SHORT_CAP, see capped() in attention_kernels.h
+constexpr double SHORT_CAP = 1024.0;
 enum { TYPE_F32 = 0, TYPE_BF16 = 1 };
 
 constexpr int64_t padded_rows(int64_t n) { return (n + 127) / 128 * 128; }   // no tile is taller

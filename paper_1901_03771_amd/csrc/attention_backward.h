@@ -436,21 +436,23 @@ static hipError_t grad_kv_one(const Args& a, unsigned grid, hipStream_t stream) 
   }
 }
 
+#define GR_BY_MODE(F, DP)                                                                                         \
+  switch (mode) {                                                                                                 \
+    case 0: return F<T, DP, 0>(a, grid, stream); case 1: return F<T, DP, 1>(a, grid, stream);                     \
+    case 2: return F<T, DP, 2>(a, grid, stream); case 3: return F<T, DP, 3>(a, grid, stream);                     \
+  }                                                                                                               \
+  if constexpr (sizeof(T) == 2) return mode == 5 ? F<T, DP, 5>(a, grid, stream) : F<T, DP, 7>(a, grid, stream);   \
+  return hipErrorInvalidValue;
 #define GR_BY_SHAPE(F)                                                                                            \
-  switch (dp * 4 + mode) {                                                                                        \
-    case 256: return F<T, 64, 0>(a, grid, stream); case 257: return F<T, 64, 1>(a, grid, stream);                 \
-    case 258: return F<T, 64, 2>(a, grid, stream); case 259: return F<T, 64, 3>(a, grid, stream);                 \
-    case 384: return F<T, 96, 0>(a, grid, stream); case 385: return F<T, 96, 1>(a, grid, stream);                 \
-    case 386: return F<T, 96, 2>(a, grid, stream); case 387: return F<T, 96, 3>(a, grid, stream);                 \
-    case 512: return F<T, 128, 0>(a, grid, stream); case 513: return F<T, 128, 1>(a, grid, stream);               \
-    case 514: return F<T, 128, 2>(a, grid, stream); case 515: return F<T, 128, 3>(a, grid, stream);               \
-    case 1024: return F<T, 256, 0>(a, grid, stream); case 1025: return F<T, 256, 1>(a, grid, stream);             \
-    case 1026: return F<T, 256, 2>(a, grid, stream); default: return F<T, 256, 3>(a, grid, stream);               \
+  switch (dp) {                                                                                                   \
+    case 64: { GR_BY_MODE(F, 64) } case 96: { GR_BY_MODE(F, 96) }                                                 \
+    case 128: { GR_BY_MODE(F, 128) } default: { GR_BY_MODE(F, 256) }                                              \
   }
 template <class T>
 static hipError_t grad_q_all(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream) { GR_BY_SHAPE(grad_q_one) }
 template <class T>
 static hipError_t grad_kv_all(const Args& a, int dp, int mode, unsigned grid, hipStream_t stream) { GR_BY_SHAPE(grad_kv_one) }
+#undef GR_BY_MODE
 #undef GR_BY_SHAPE
 
 }  // namespace attn

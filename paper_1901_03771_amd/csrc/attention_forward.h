@@ -330,8 +330,10 @@ static hipError_t forward_mode(const Args& a, int mode, unsigned grid, hipStream
     case 0: return forward_one<T, DP, 0, DIVIDED>(a, grid, stream);
     case 1: return forward_one<T, DP, 1, DIVIDED>(a, grid, stream);
     case 2: return forward_one<T, DP, 2, DIVIDED>(a, grid, stream);
-    default: return forward_one<T, DP, 3, DIVIDED>(a, grid, stream);
+    case 3: return forward_one<T, DP, 3, DIVIDED>(a, grid, stream);
   }
+  if constexpr (sizeof(T) == 2) return mode == 5 ? forward_one<T, DP, 5, DIVIDED>(a, grid, stream) : forward_one<T, DP, 7, DIVIDED>(a, grid, stream);
+  return hipErrorInvalidValue;
 }
 template <class T>
 static hipError_t forward_all(const Args& a, int dp, int mode, bool divided, unsigned grid, hipStream_t stream) {

@@ -940,3 +940,32 @@ def test_gradient_of_a_nan_row(ctx, dtype):
             assert torch.equal(got[w][1, :, 1:], clean[w][1, :, 1:]), w
         keep = torch.arange(N) != 7
         assert torch.equal(got["dq"][1][keep], clean["dq"][1][keep])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("cap", [1e3, 1024.0, 1025.0, 1e5, 1e7, 1e20])
+@pytest.mark.parametrize("N,M,H,HK,slopes", [(70, 200, 4, 2, False), (5, 900, 4, 2, True), (33, 70, 2, 2, True)])
+def test_caps_far_above_the_scores(ctx, N, M, H, HK, slopes, cap, dtype):
+    """A large cap leaves scores as they are: no error of the tanh is to be multiplied by it.  The score itself may be off by 2^-12 (a sixteenth of what rounding a
+    probability to bfloat16 may do) in bfloat16, whatever the cap, and by nothing but its own roundings in float32."""
+    c = dict(B=1, N=N, M=M, H=H, HK=HK, D=64, dtype=dtype, grad=True, cap=cap, slopes=slopes, causal=True, position=M - N)
+    q, k, v, d = tensors(c)
+    kw = options(c)
+    got = run_case(ctx, c, q, k, v, d, kw)
+    ref = plain.attention(q, k, v, d, **kw)
+    lse, low = got.pop("lse").cpu().double(), 2.0 ** -12 if dtype == BF16 else 0.0
+    off = (64 + 10) * 2.0 ** -24 * float(ref["score"].max())
+    bar = off + low + (M + 16) * 2.0 ** -24 + 4 * 2.0 ** -24 * ref["lse"].abs()
+    assert ((lse - ref["lse"]).abs() <= bar).all(), float((lse - ref["lse"]).abs().max())
+    plain.check(got, ref, dtype, 64, M, N, H // HK, f"cap {cap}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap", [500.0, 1e4, 1e7])
+def test_single_tokens_with_large_caps(ctx, cap):
+    q, k, v = normal(1, 2, 8, 128, dtype=BF16, by=2.0), normal(2, 2, 1000, 2, 128, dtype=BF16), normal(3, 2, 1000, 2, 128, dtype=BF16)
+    kw = dict(cap=cap, lengths=torch.tensor([1000, 333], dtype=torch.int32))
+    out = torch.full_like(q, 7.0)
+    gr.attention_step(ctx.array(q), ctx.array(k), ctx.array(v), on_gpu(ctx, kw), out=ctx.array(out))
+    plain.check(dict(out=out[:, None]), plain.attention(q[:, None], k, v, step=True, **kw), BF16, 128, 1000, 1, 4, "step")
