@@ -43,8 +43,8 @@ extern "C" {
  * is infinite or NaN may reach rows of its tile that do not see it, as 0 * inf does in a plain product.)
  * A query that is NaN, or sees a score that is NaN or +inf, has NaN in out and lse, at every size. */
 typedef struct {
-  double scale;         /* > 0 and finite */
-  double cap;           /* 0 = none; > 0 and finite */
+  double scale;         /* 1e-28 .. 1e30 */
+  double cap;           /* 0 = none; 1e-30 .. 1e30, and scale / cap 1e-37 .. 1e38 */
   gr_array slopes;      /* f32 (H), not trained: no gradient; 0 = none */
   int causal;           /* 1: a query sees keys up to its own position */
   int64_t position;     /* of query 0, -2^31 .. 2^31 */

@@ -266,8 +266,13 @@ static gr_status extents(Call& c, gr_array q, gr_array k, int rank, int* type, A
 
 static gr_status take_scores(Call& c, const gr_scores* s, Args* a, bool step) {
   if (!s) return c.error(GR_ERR_ARG, "NULL scores");
-  if (!(s->scale > 0.0) || !std::isfinite(s->scale) || !(s->scale < 1e30)) return c.error(GR_ERR_ARG, "scale must be positive and finite");
-  if (!(s->cap >= 0.0) || !std::isfinite(s->cap) || !(s->cap < 1e30) || (s->cap > 0.0 && !(s->cap > 1e-30))) return c.error(GR_ERR_ARG, "cap must be 0, or positive and finite");
+  // What the kernels take of them (scale log2(e), scale 2^-32, cap log2(e), 2 log2(e) scale / cap) are normal floats: a factor that is zero or infinite makes NaN of
+  // masked scores and of zeros.
+  if (!(s->scale > 1e-28 && s->scale < 1e30)) return c.error(GR_ERR_ARG, "scale must be between 1e-28 and 1e30");
+  if (s->cap != 0.0) {
+    if (!(s->cap > 1e-30 && s->cap < 1e30)) return c.error(GR_ERR_ARG, "cap must be 0, or between 1e-30 and 1e30");
+    if (!(s->scale / s->cap > 1e-37 && s->scale / s->cap < 1e38)) return c.error(GR_ERR_ARG, "scale / cap must be between 1e-37 and 1e38");
+  }
   if (s->causal != 0 && s->causal != 1) return c.error(GR_ERR_ARG, "causal must be 0 or 1");
   if (s->position < -(int64_t(1) << 31) || s->position > (int64_t(1) << 31)) return c.error(GR_ERR_ARG, "position beyond 2^31");
   if (s->prefix && !s->causal) return c.error(GR_ERR_ARG, "a prefix without a causal mask");

@@ -238,6 +238,20 @@ def test_numbers_are_not_cut_to_fit(dry):
         refused("GR_ERR_ARG", gr.rotary, x, f, 5, factor=factor, out=x)
 
 
+def test_scales_and_caps_that_no_float_holds_are_refused(dry):
+    """A factor that is zero or infinite as a float would make NaN of masked scores and of zeros."""
+    s = Specs(dry)
+    q, o, lse, d = s((1, 4, 2, 64)), s((1, 4, 2, 64)), s((1, 2, 4)), [s((1, 4, 2, 64)) for _ in range(3)]
+    one, to, n = s((1, 2, 64)), s((1, 2, 64)), s((1,), gr.GR_I32)
+    for kw in (dict(scale=1e-46), dict(scale=1e-320), dict(scale=1e-29), dict(scale=1e30), dict(scale=1e29, cap=1e-29), dict(scale=1e-27, cap=1e29), dict(cap=1e-31),
+               dict(cap=1e30), dict(cap=math.nan), dict(scale=math.inf)):
+        refused("GR_ERR_ARG", gr.attention, q, q, q, dry.scores(causal=True, **kw), out=o, lse=lse)
+        refused("GR_ERR_ARG", gr.attention_grad, q, q, q, q, dry.scores(causal=True, **kw), q, lse, dq=d[0], dk=d[1], dv=d[2])
+        refused("GR_ERR_ARG", gr.attention_step, one, q, q, dry.scores(lengths=n, **kw), out=to)
+    for kw in (dict(scale=1e-27), dict(scale=1e29), dict(scale=1e29, cap=1e-8), dict(cap=1e-29), dict(scale=1e-7, cap=9e29)):
+        gr.attention(q, q, q, dry.scores(causal=True, **kw), out=o, lse=lse)
+
+
 def test_scores_of_another_context(dry):
     """Handles are numbers of a context: the same number names another array in the next."""
     other = gr.Context(device=-1)
@@ -969,3 +983,20 @@ def test_single_tokens_with_large_caps(ctx, cap):
     out = torch.full_like(q, 7.0)
     gr.attention_step(ctx.array(q), ctx.array(k), ctx.array(v), on_gpu(ctx, kw), out=ctx.array(out))
     plain.check(dict(out=out[:, None]), plain.attention(q[:, None], k, v, step=True, **kw), BF16, 128, 1000, 1, 4, "step")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("kw", [dict(scale=1e-27), dict(scale=1e25), dict(scale=1e25, cap=1e-8), dict(scale=1e-7, cap=9e29), dict(cap=1e-25)])
+def test_scales_and_caps_at_the_ends(ctx, kw, dtype):
+    """Scores of one sign of zero, of a cap's size, or so far apart that one key has all: nothing but numbers, and masked keys have no say."""
+    c = dict(B=1, N=70, M=70, H=2, HK=1, D=64, dtype=dtype, grad=True, causal=True)
+    q, k, v, d = tensors(c)
+    got = run_case(ctx, c, q, k, v, d, dict(kw, causal=True))
+    for w, t in got.items():
+        assert torch.isfinite(t).all(), w
+    # the first query sees the first key alone
+    assert torch.equal(got["out"][:, 0], v[:, 0].expand(1, 2, 64))
+    if kw.get("cap", 1.0) < 1e-20 or kw.get("scale", 1.0) < 1e-20:   # all scores as good as zero: means of v
+        mean = v.double().cumsum(1) / torch.arange(1, 71, device="cuda").view(1, 70, 1, 1)
+        assert ((got["out"].double() - mean).abs() <= 2 * plain.HALF[dtype] * v.double().abs().cumsum(1) / torch.arange(1, 71, device="cuda").view(1, 70, 1, 1) + 1e-5).all()
