@@ -1000,3 +1000,20 @@ def test_scales_and_caps_at_the_ends(ctx, kw, dtype):
     if kw.get("cap", 1.0) < 1e-20 or kw.get("scale", 1.0) < 1e-20:   # all scores as good as zero: means of v
         mean = v.double().cumsum(1) / torch.arange(1, 71, device="cuda").view(1, 70, 1, 1)
         assert ((got["out"].double() - mean).abs() <= 2 * plain.HALF[dtype] * v.double().abs().cumsum(1) / torch.arange(1, 71, device="cuda").view(1, 70, 1, 1) + 1e-5).all()
+
+
+@pytest.mark.gpu
+def test_the_largest_floats(ctx):
+    """float32 values up to 2^128 - 2^119 are numbers, seen and unseen; those beyond count as infinite."""
+    c = dict(B=1, N=40, M=40, H=2, HK=1, D=64, dtype=F32, grad=False, causal=True)
+    q, k, v, d = tensors(c)
+    most = 2.0 ** 128 - 2.0 ** 119 - 2.0 ** 104   # the last float below
+    clean = run_case(ctx, c, q, k, v, d, options(c))
+    last = v.clone()
+    last[0, 39] = -most                            # seen by the last query alone
+    got = run_case(ctx, c, q, k, last, d, options(c))
+    assert torch.equal(got["out"][:, :39], clean["out"][:, :39])
+    plain.check(got, plain.attention(q, k, last, causal=True), F32, 64, 40, 40, 2, "largest")
+    last[0, 39, :, 3] = 2.0 ** 128 - 2.0 ** 119
+    got = run_case(ctx, c, q, k, last, d, options(c))
+    assert torch.isnan(got["out"][0, 39, :, 3]).all() and torch.equal(got["lse"], clean["lse"])
