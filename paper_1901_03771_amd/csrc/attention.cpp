@@ -473,6 +473,7 @@ static gr_status grad(gr_ctx* ctx, const gr_scores* s, gr_array q, gr_array k, g
   TRY(c.tensor(dv, "dv", &a.dv));
   a.lse = (float*)c.view(lse).data;
   const int mode = fill_scores(c, s, type, &a);
+  if (type == TYPE_F32) a.c *= 0.5f;   // (EXPONENT in attention_backward.h)
 
   const int64_t rows = (int64_t)a.N * a.G, pairs = (int64_t)a.B * a.HK;
   if (pairs == 0) return GR_OK;

@@ -20,7 +20,7 @@ struct Tensor {
 struct Args {
   Tensor q, k, v, out, rest, dout, dq, dk, dv;
   float* lse = nullptr;          // (B, H, N)
-  // of the gradient, (B, H, NP) with NP = N rounded up to whole tiles: less = lse in binary logarithms - LIFT (rows that see nothing, and
+  // of the gradient, (B, H, NP) with NP = N rounded up to whole tiles: less = lse in binary logarithms - LIFT, of float32 half of it without (rows that see nothing, and
   // rows behind the last: +inf), delta = sum over d of dout * out
   float *less = nullptr, *delta = nullptr;
   float* part_o = nullptr;       // (splits, B * HK, N * G, DP) unnormalised sums of a split's keys; parts of dq, or of dk and dv, likewise

@@ -4,8 +4,11 @@
 // (no atomic additions, the same bits from call to call):
 //   gr_attention_grad_q   walks the keys for 128 rows of queries, as the forward kernel does;
 //   gr_attention_grad_kv  walks the queries of all heads that share a head of k and v for a block of keys.
-// Probabilities are carried 2^32 times as large (LIFT, taken out of the sums in the end), so that those below float32's normal numbers
-// still count in the gradients of keys that every query all but ignores; there is room for it above.
+// Probabilities are carried 2^32 times as large (UNLIFT takes it out of the sums in the end), so that those below float32's normal numbers
+// still count in the gradients of keys that every query all but ignores; there is room for it above.  With bfloat16 tensors LIFT stands in the
+// exponent, which rounds it like a number near 32: 2^-20 of a probability that is rounded to 2^-8 next.  For float32 that would be the largest error of
+// all (a pass over 777 rows of 80 values 7.2e-7 from binary64 where a plain one is at 4.2e-7): there the kernels form e = 2^(half the exponent), which never
+// leaves the normal numbers, and the probability as (2^32 e) e.
 // They form q k^T and dout v^T twice, 7 products of the size of q k^T where a single kernel would have 5 and an addition to dq in memory
 // per tile.
 //
@@ -17,6 +20,15 @@
 
 namespace gr {
 namespace attn {
+
+// Of exponents, and what stands for them (less, c, slopes): the whole for bfloat16, the half for float32.
+template <class T> constexpr float EXPONENT = sizeof(T) == 4 ? 0.5f : 1.0f;
+template <class T>
+static __device__ __forceinline__ float lifted(float x) {
+  const float e = exp2_(x);
+  if constexpr (sizeof(T) == 4) return (e * 0x1p32f) * e;
+  else return e;
+}
 
 template <class T, int DP>
 struct ShapeQ {
@@ -69,7 +81,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   }
   const int64_t stat = ((int64_t)b * a.H + mine.h) * padded_rows(a.N) + mine.i;
   float less = mine.valid ? a.less[stat] : INF, delta = mine.valid ? a.delta[stat] : 0.0f;
-  float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * LOG2E : 0.0f;
+  float slope = MODE & MODE_BIAS ? a.slopes[mine.h * a.slopes_s] * (LOG2E * EXPONENT<T>) : 0.0f;
   const int64_t pos = MODE & MODE_BIAS ? a.position + mine.i : 0;
 
   f32x16 o[L::BLOCKS];
@@ -129,7 +141,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
         if constexpr (MODE & MODE_CAP) dp[r] *= bend;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]) * dp[r];
+      for (int r = 0; r < 16; ++r) s[r] = lifted<T>(s[r]) * dp[r];
       if (!whole) {
         const int flane = fresh(lane);
         const Row me = row_of(a, hk, wrow0 + (flane & 31));
@@ -295,7 +307,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
     const GR_LDS char* const qt = smem + 2 * stage * S::TILE;
     const GR_LDS char* const dt = qt + S::TILE;
     const GR_LDS float* const st = stats + stage * S::STATS;
-    const float slope = MODE & MODE_BIAS ? scalar_float(a.slopes, h * a.slopes_s) * LOG2E : 0.0f;
+    const float slope = MODE & MODE_BIAS ? scalar_float(a.slopes, h * a.slopes_s) * (LOG2E * EXPONENT<T>) : 0.0f;
     
 #pragma unroll 1
     for (int rb = 0; rb < S::ROWS / 32; ++rb) {
@@ -333,7 +345,7 @@ __global__ __launch_bounds__(256, (ShapeKV<T, DP, WHICH>::PER_CU)) void gr_atten
           if constexpr (MODE & MODE_CAP) { y = capped<T, MODE>(y, a.cin); bend = __builtin_fmaf(-y, y, 1.0f); }
           if constexpr (MODE & MODE_BIAS) y = __builtin_fmaf(y, a.c, __builtin_fmaf(-slope, __builtin_fabsf(away + (float)(rr + e)), -less[e]));
           else y = __builtin_fmaf(y, a.c, -less[e]);
-          s[r] = exp2_(y);
+          s[r] = lifted<T>(y);
           if constexpr (WANT_K) {
             dp[r] = s[r] * (dp[r] - delta[e]);
             if constexpr (MODE & MODE_CAP) dp[r] *= bend;

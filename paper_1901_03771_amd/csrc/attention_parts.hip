@@ -138,10 +138,10 @@ __global__ __launch_bounds__(256) void gr_attention_statistics_kernel(const Args
   for (int m = 8; m; m >>= 1) x += __shfl_xor(x, m);
   if (part != 0) return;
   const float e = a.lse[((int64_t)b * a.H + h) * a.N + i];
-  float less = e == -INF ? INF : e * LOG2E - LIFT;
+  float less = e == -INF ? INF : sizeof(T) == 4 ? e * LOG2E : e * LOG2E - LIFT;
   const float size = __builtin_fabsf(less);
   if (size >= 0x1p28f && size < INF) less += size * 0x1p-22f;
-  a.less[to] = less;
+  a.less[to] = sizeof(T) == 4 ? 0.5f * less : less;   // (see EXPONENT in attention_backward.h)
   a.delta[to] = x;
 }
 

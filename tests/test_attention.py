@@ -1017,3 +1017,29 @@ def test_the_largest_floats(ctx):
     last[0, 39, :, 3] = 2.0 ** 128 - 2.0 ** 119
     got = run_case(ctx, c, q, k, last, d, options(c))
     assert torch.isnan(got["out"][0, 39, :, 3]).all() and torch.equal(got["lse"], clean["lse"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("slopes", [False, True])
+def test_probabilities_of_the_float32_gradient(ctx, slopes):
+    """Every query sees one key, at a score of exactly zero, under an lse that the test gives: dv, dq and dk are single products with p = exp(-lse).  Roundings of
+    p, in units of 2^-24: lse in binary logarithms 0.7, a power of two of half the exponent, off by a unit in the last place at most, taken twice 4, two
+    products 1 each; of the result: two products more.  In the mean, a rounding of e at most being e / sqrt(3): sqrt(0.5 + 16 + 4) / sqrt(3) = 2.6, and the bar is 4, that is
+    2^-22.  An exponent rounded as a number near 32 would be off by 16 ln 2 / sqrt(3) = 6.4."""
+    N, D = 512, 64
+    g = torch.Generator().manual_seed(31)
+    q, k, v = torch.zeros(3, 1, N, 1, D).unbind(0)
+    q[..., :32], k[..., 32:], v[..., 0] = torch.randn(1, N, 1, 32, generator=g), torch.randn(1, N, 1, 32, generator=g), 1.0
+    do, lse = torch.randn(1, N, 1, D, generator=g), torch.rand(1, 1, N, generator=g) * 0.5 + 0.5
+    ids = torch.arange(N, dtype=torch.int32)[None]
+    A = lambda t: ctx.array(t.cuda())  # noqa: E731
+    sc = ctx.scores(scale=1.0, documents=A(ids), slopes=A(torch.tensor([3.0])) if slopes else None)   # (a key at the query's own place)
+    got = gr.attention_grad(A(do), A(q), A(k), A(v), sc, A(torch.zeros_like(q)), A(lse))
+    p = torch.exp(-lse.double())[0, 0].view(1, N, 1, 1)
+    ds = p * do.double()[..., :1]
+    for name, x, want in zip(("dq", "dk", "dv"), got, (ds * k.double(), ds * q.double(), p * do.double())):
+        x = x.torch().cpu().double()
+        some = want != 0
+        assert (x[~some] == 0).all(), name
+        off = x[some] / want[some] - 1
+        assert off.square().mean().sqrt() <= 2.0 ** -22, (name, float(off.square().mean().sqrt()))
