@@ -824,12 +824,24 @@ class Scores:
         self._scale = scale
         self._c = _Scores(0.0 if scale is None else scale, cap, h[0], builtins.bool(causal), _place(position), h[1], h[2], h[3], h[4])
 
-    def _for(self, ctx: Context, d: int):
-        if self.ctx is not ctx:   # (its handles are numbers of that context, which may be other arrays' here)
-            raise ValueError("scores and arrays belong to different contexts")
-        if self._scale is None:
-            self._c.scale = builtins.max(d, 1) ** -0.5
-        return ctypes.byref(self._c)
+def _scores_for(scores: Scores, q: "Array"):
+    """What the C calls take of `scores` for the queries `q`."""
+    if not isinstance(scores, Scores):
+        raise TypeError("expected the scores of the context (Context.scores)")
+    if scores.ctx is not q.ctx:   # (its handles are numbers of that context, which may be other arrays' here)
+        raise ValueError("scores and arrays belong to different contexts")
+    if scores._scale is None:
+        shape = q.shape
+        if not shape:
+            raise GrError(2, "q has no axes")
+        scores._c.scale = builtins.max(shape[-1], 1) ** -0.5
+    return ctypes.byref(scores._c)
+
+
+def _context_of(a: "Array") -> Context:
+    if not isinstance(a, Array):
+        raise TypeError("expected an Array of the context")
+    return a.ctx
 
 
 def _tensor(ctx: Context, a: "Array") -> int:
@@ -843,9 +855,13 @@ def _result_array(ctx: Context, given, shape, dtype: int) -> "Array":
     that stream was the last to use: it is taken for the stream of the context, whichever is torch's at the time."""
     if given is not None:
         return given
+    if dtype not in (GR_F32, GR_BF16):
+        raise GrError(3, "operands must be f32 or bf16")
+    if ctx.device < 0:
+        raise GrError(11, "the context has no device for a new result")
     torch = _torch()
-    dtype = {GR_F32: torch.float32, GR_BF16: torch.bfloat16}[dtype]
-    if ctx.device < 0 or torch.cuda.current_stream(ctx.device).cuda_stream == ctx._stream:
+    dtype = torch.float32 if dtype == GR_F32 else torch.bfloat16
+    if torch.cuda.current_stream(ctx.device).cuda_stream == ctx._stream:
         t = torch.empty(shape, device=f"cuda:{ctx.device}", dtype=dtype)
     else:
         with torch.cuda.stream(torch.cuda.ExternalStream(ctx._stream, ctx.device)):
@@ -859,10 +875,9 @@ def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=
     """softmax(scores) v (gr_attention) of q (B, N, H, D), k and v (B, M, HK, D), f32 or bf16; returns (out, lse).  out and
     lse are new arrays where none are given; lse=False: not wanted, returned as None.  rest (bf16, optional): gets what out lost in
     rounding, for attention_grad."""
-    ctx = q.ctx
-    hq, hk, hv = _tensor(ctx, q), _tensor(ctx, k), _tensor(ctx, v)
+    ctx = _context_of(q)
+    hq, hk, hv, sc = _tensor(ctx, q), _tensor(ctx, k), _tensor(ctx, v), _scores_for(scores, q)
     shape = q.shape if out is None or lse is None else None
-    d = q.shape[-1] if scores._scale is None else 0
     out = _result_array(ctx, out, shape, q.dtype_code if out is None else 0)
     if lse is None:
         if len(shape) != 4:
@@ -870,7 +885,7 @@ def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=
         lse = _result_array(ctx, None, (shape[0], shape[2], shape[1]), GR_F32)
     elif lse is False:
         lse = None
-    st = lib().gr_attention(ctx._p, scores._for(ctx, d), hq, hk, hv, _tensor(ctx, out), 0 if lse is None else _tensor(ctx, lse),
+    st = lib().gr_attention(ctx._p, sc, hq, hk, hv, _tensor(ctx, out), 0 if lse is None else _tensor(ctx, lse),
                             0 if rest is None else _tensor(ctx, rest))
     if st:
         ctx.check(st)
@@ -880,15 +895,14 @@ def attention(q: "Array", k: "Array", v: "Array", scores: Scores, out=None, lse=
 def attention_grad(dout: "Array", q: "Array", k: "Array", v: "Array", scores: Scores, out: "Array", lse: "Array", rest=None,
                    dq=None, dk=None, dv=None):
     """The gradients of q, k and v (gr_attention_grad) for the gradient of out; returns (dq, dk, dv)."""
-    ctx = q.ctx
-    h = [_tensor(ctx, a) for a in (q, k, v, out)]
+    ctx = _context_of(q)
+    h, sc = [_tensor(ctx, a) for a in (q, k, v, out)], _scores_for(scores, q)
     h.append(0 if rest is None else _tensor(ctx, rest))
     h += [_tensor(ctx, lse), _tensor(ctx, dout)]
     dq = _result_array(ctx, dq, q.shape if dq is None else None, q.dtype_code if dq is None else 0)
     dk = _result_array(ctx, dk, k.shape if dk is None else None, k.dtype_code if dk is None else 0)
     dv = _result_array(ctx, dv, v.shape if dv is None else None, v.dtype_code if dv is None else 0)
-    st = lib().gr_attention_grad(ctx._p, scores._for(ctx, q.shape[-1] if scores._scale is None else 0), *h,
-                                 _tensor(ctx, dq), _tensor(ctx, dk), _tensor(ctx, dv))
+    st = lib().gr_attention_grad(ctx._p, sc, *h, _tensor(ctx, dq), _tensor(ctx, dk), _tensor(ctx, dv))
     if st:
         ctx.check(st)
     return dq, dk, dv
@@ -896,10 +910,10 @@ def attention_grad(dout: "Array", q: "Array", k: "Array", v: "Array", scores: Sc
 
 def attention_step(q: "Array", k: "Array", v: "Array", scores: Scores, out=None):
     """One new token per sequence (gr_attention_step): q (B, H, D) against the first lengths[b] rows of k and v (B, M, HK, D)."""
-    ctx = q.ctx
-    h = [_tensor(ctx, a) for a in (q, k, v)]
+    ctx = _context_of(q)
+    h, sc = [_tensor(ctx, a) for a in (q, k, v)], _scores_for(scores, q)
     out = _result_array(ctx, out, q.shape if out is None else None, q.dtype_code if out is None else 0)
-    st = lib().gr_attention_step(ctx._p, scores._for(ctx, q.shape[-1] if scores._scale is None else 0), *h, _tensor(ctx, out))
+    st = lib().gr_attention_step(ctx._p, sc, *h, _tensor(ctx, out))
     if st:
         ctx.check(st)
     return out
@@ -927,7 +941,7 @@ def rotary_frequencies(values: int, base: float = 10000.0, stretch: float = 1.0,
 def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inverse: bool = False, factor: float = 1.0, out=None):
     """x (B, N, H, D) with the pairs of every head turned by position * frequencies (gr_rotary).  positions: an i32 array (B, N), or
     the position of the first token.  out: where to (x itself for in place); a new array if none is given."""
-    ctx = x.ctx
+    ctx = _context_of(x)
     hx = _tensor(ctx, x)
     n = len(frequencies)
     if not (isinstance(frequencies, ctypes.Array) and frequencies._type_ is ctypes.c_double):

@@ -252,6 +252,31 @@ def test_scales_and_caps_that_no_float_holds_are_refused(dry):
         gr.attention(q, q, q, dry.scores(causal=True, **kw), out=o, lse=lse)
 
 
+def test_what_python_is_given_wrong_is_said_so(dry):
+    """Element types, ranks and objects that do not fit, with and without results given; a context without a device has no memory for new ones."""
+    s = Specs(dry)
+    ok, f, i, none, lse = dry.scores(), s((1, 4, 2, 64)), s((1, 4, 2, 64), gr.GR_I32), s(()), s((1, 2, 4))
+    one = s((1, 2, 64))
+    refused("GR_ERR_DTYPE", gr.attention, i, i, i, ok)
+    refused("GR_ERR_DTYPE", gr.attention_step, s((1, 2, 64), gr.GR_I32), i, i, ok)
+    refused("GR_ERR_DTYPE", gr.attention_grad, i, i, i, i, ok, i, lse)
+    refused("GR_ERR_DTYPE", gr.rotary, i, gr.rotary_frequencies(64))
+    refused("GR_ERR_SHAPE", gr.attention, none, f, f, ok)
+    refused("GR_ERR_SHAPE", gr.attention, none, f, f, ok, out=s((1, 4, 2, 64)), lse=False)
+    refused("GR_ERR_SHAPE", gr.attention_step, none, f, f, ok, out=one)
+    refused("GR_ERR_SHAPE", gr.attention_grad, f, none, f, f, ok, f, lse, dq=s((1, 4, 2, 64)), dk=s((1, 4, 2, 64)), dv=s((1, 4, 2, 64)))
+    refused("GR_ERR_NODEVICE", gr.attention, f, f, f, ok)
+    refused("GR_ERR_NODEVICE", gr.rotary, f, gr.rotary_frequencies(64))
+    for q in (1.0, None, torch.ones(1, 4, 2, 64)):
+        for call in (lambda: gr.attention(q, f, f, ok), lambda: gr.attention(f, q, f, ok, out=one, lse=False), lambda: gr.attention_step(q, f, f, ok),
+                     lambda: gr.attention_grad(f, q, f, f, ok, f, lse), lambda: gr.rotary(q, gr.rotary_frequencies(64))):
+            with pytest.raises(TypeError):
+                call()
+    for sc in (None, 1.0, gr._Scores()):
+        with pytest.raises(TypeError):
+            gr.attention(f, f, f, sc, out=s((1, 4, 2, 64)), lse=False)
+
+
 def test_scores_of_another_context(dry):
     """Handles are numbers of a context: the same number names another array in the next."""
     other = gr.Context(device=-1)
