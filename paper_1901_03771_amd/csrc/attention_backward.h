@@ -33,7 +33,7 @@ static __device__ __forceinline__ float lifted(float x) {
 template <class T, int DP>
 struct ShapeQ {
   static constexpr int THREADS = 256, KEYS = tile_rows(sizeof(T), DP), ROWS = 128, TILE = KEYS * Tile<T, DP>::ROW;
-  static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;   // two stages of k and v, 64 words to exchange, two stages of the keys' documents
+  static constexpr int LDS = 4 * TILE + 2 * KEYS * 4;   // two stages of k and v, two stages of the keys' documents
   static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 8 : 24) + DP / 2 + 32;   // operands of q and dout, sums, two blocks of scores
   static constexpr bool TIGHT = REGS > (sizeof(T) == 2 ? 160 : 128);   // of registers: addresses within tiles are formed anew for each tile
   static constexpr int PER_CU = grad_q_per_cu(sizeof(T), DP);
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
   typedef typename Frag<T>::type F;
   extern __shared__ char smem_[];
   GR_LDS char* const smem = (GR_LDS char*)smem_;
-  GR_LDS int* const shared = (GR_LDS int*)(smem + 4 * S::TILE);
+  GR_LDS int* const documents = (GR_LDS int*)(smem + 4 * S::TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
   const int pairs = a.B * a.HK;
   const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
     const int rows = min(S::KEYS, len - (int)k0);
     L::template load<S::KEYS, 256>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.k.direct);
     L::template load<S::KEYS, 256>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.v.direct);
-    if (a.kdoc && wave == 0) load_words((GR_LDS float*)(shared + 64 + stage * S::KEYS), a.kdocs + b * padded_rows(a.M) + k0, lane, S::KEYS);
+    if (a.kdoc && wave == 0) load_words((GR_LDS float*)(documents + stage * S::KEYS), a.kdocs + b * padded_rows(a.M) + k0, lane, S::KEYS);
   };
   int t = find.next(split * per, tiles, lane), stage = 0;
   if (t < tiles) load(t, 0);
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256, (ShapeQ<T, DP>::PER_CU)) void gr_attention_gra
         for (int r = 0; r < 16; ++r) s[r] = (r & 3) + 8 * (r >> 2) < see ? s[r] : 0.0f;
         if (!one) {
           const int doc = me.valid ? a.qdocs[b * padded_rows(a.N) + me.i] : -1;
-          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + kb * 32 + 4 * (flane >> 5);
+          const GR_LDS int* const kd = documents + stage * S::KEYS + kb * 32 + 4 * (flane >> 5);
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
             const i32x4 n = *(const GR_LDS i32x4*)(kd + 8 * r4);
@@ -440,7 +440,7 @@ static hipError_t grad_kv_part(const Args& a, unsigned grid, hipStream_t stream)
 }
 template <class T, int DP, int MODE>
 static hipError_t grad_kv_one(const Args& a, unsigned grid, hipStream_t stream) {
-    if constexpr (DP == 256) {
+  if constexpr (DP == 256) {
     const hipError_t e = grad_kv_part<T, DP, MODE, ONLY_V>(a, grid, stream);
     return e != hipSuccess ? e : grad_kv_part<T, DP, MODE, ONLY_K>(a, grid, stream);
   } else {

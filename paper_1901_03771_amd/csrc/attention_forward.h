@@ -29,8 +29,8 @@ struct Shape {
   static constexpr int KB = DIVIDED ? 1 : KEYS / 32;                              // blocks of 32 keys a wave multiplies
   static constexpr int ROWS = DIVIDED ? 32 : 32 * WAVES;
   static constexpr int TILE = KEYS * Tile<T, DP>::ROW;
-  // two stages of a tile of k and one of v (the joining waves' sums lie over them), 64 words to exchange, two stages of the keys' documents
-  static constexpr int LDS = 4 * TILE + 256 + 2 * KEYS * 4;
+  // two stages of a tile of k and one of v (the joining waves' sums lie over them), two stages of the keys' documents
+  static constexpr int LDS = 4 * TILE + 2 * KEYS * 4;
   static_assert(!DIVIDED || WAVES * 32 * (DP + 4) * 4 <= 4 * TILE, "the waves' sums fit the stages");
   // registers: operands of q, sums, scores
   static constexpr int REGS = DP / 16 * (sizeof(T) == 2 ? 4 : 12) + DP / 2 + 16 * KB;
@@ -48,7 +48,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
   typedef typename Frag<T>::type F;
   extern __shared__ char smem_[];
   GR_LDS char* const smem = (GR_LDS char*)smem_;
-  GR_LDS int* const shared = (GR_LDS int*)(smem + 4 * S::TILE);
+  GR_LDS int* const documents = (GR_LDS int*)(smem + 4 * S::TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
   const int pairs = a.B * a.HK;
   const Place place = place_of(blockIdx.x, pairs, a.blocks * a.splits);
@@ -102,7 +102,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
     const int rows = min(S::KEYS, len - (int)k0);
     L::template load<S::KEYS, S::THREADS>(smem + 2 * stage * S::TILE, kbase + k0 * a.k.sn, a.k.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.k.direct);
     L::template load<S::KEYS, S::THREADS>(smem + (2 * stage + 1) * S::TILE, vbase + k0 * a.v.sn, a.v.sn, rows, a.D, S::TIGHT ? fresh(tid) : tid, a.v.direct);
-    if (a.kdoc && wave * 64 < S::KEYS) load_words((GR_LDS float*)(shared + 64 + stage * S::KEYS + wave * 64), a.kdocs + b * padded_rows(a.M) + k0 + wave * 64, lane, S::KEYS - wave * 64);
+    if (a.kdoc && wave * 64 < S::KEYS) load_words((GR_LDS float*)(documents + stage * S::KEYS + wave * 64), a.kdocs + b * padded_rows(a.M) + k0 + wave * 64, lane, S::KEYS - wave * 64);
   };
   int t = find.next(split * per, t1, lane), stage = 0;
   if (t < t1) load(t, 0);
@@ -163,7 +163,7 @@ __global__ __launch_bounds__((Shape<T, DP, DIVIDED>::THREADS), (Shape<T, DP, DIV
           for (int r = 0; r < 16; ++r) s[kb][r] = kb * 32 + (r & 3) + 8 * (r >> 2) < see ? s[kb][r] : -INF;
         if (!one) {
           const int doc = me.valid ? a.qdocs[b * padded_rows(a.N) + me.i] : -1;
-          const GR_LDS int* const kd = shared + 64 + stage * S::KEYS + (DIVIDED ? wave * 32 : 0) + 4 * (flane >> 5);
+          const GR_LDS int* const kd = documents + stage * S::KEYS + (DIVIDED ? wave * 32 : 0) + 4 * (flane >> 5);
 #pragma unroll
           for (int kb = 0; kb < S::KB; ++kb)
 #pragma unroll
