@@ -14,7 +14,8 @@
  *     f32 for lse and slopes.  bf16 arrays are leaves and views of leaves: no other call computes with them
  *     (GR_ERR_DTYPE).  Products of f32 are formed of three bf16 pieces of each value, right to 2^-24; a value that bf16 rounds
  *     to infinity (2^128 - 2^119 = 3.396e38 and more) counts as infinite and gives NaN.  Scores, probabilities, statistics and sums are
- *     f32; with bf16 tensors a probability, or a score's gradient, is rounded to bf16 where it enters the next product.  The gradient forms
+ *     f32; with bf16 tensors a probability, or a score's gradient, is rounded to bf16 where it enters the next product (not the probabilities of
+ *     gr_attention with rest, nor of calls of at most 32 queries times heads per head of k).  The gradient forms
  *     probabilities from lse, which f32 holds to |lse| 2^-24, and their relative error is as large; and it carries sums 2^32 times as large: dv, dq / scale and dk / scale
  *     (with no part of their sums) may not pass 2^95 in size, beyond it they are infinite or NaN.
  *   - Shapes: q, out, rest, dout, dq (B, N, H, D); k, v, dk, dv (B, M, HK, D) with H a multiple of HK: head h of q reads head
