@@ -820,7 +820,7 @@ class Scores:
         qd, kd = documents if isinstance(documents, (tuple, list)) else (documents, documents)
         self.ctx = ctx
         self._keep = (slopes, prefix, qd, kd, lengths)
-        h = [0 if a is None else _operand(ctx, a).h for a in self._keep]
+        h = [0 if a is None else _tensor(ctx, a) for a in self._keep]
         self._scale = scale
         self._c = _Scores(0.0 if scale is None else scale, cap, h[0], builtins.bool(causal), _place(position), h[1], h[2], h[3], h[4])
 

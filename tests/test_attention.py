@@ -272,6 +272,10 @@ def test_what_python_is_given_wrong_is_said_so(dry):
                      lambda: gr.attention_grad(f, q, f, f, ok, f, lse), lambda: gr.rotary(q, gr.rotary_frequencies(64))):
             with pytest.raises(TypeError):
                 call()
+    for bad in (0.5, torch.zeros(2), [1.0, 2.0]):
+        for name in ("slopes", "prefix", "lengths", "documents"):
+            with pytest.raises((TypeError, ValueError)):
+                dry.scores(**{name: bad, "causal": True})
     for sc in (None, 1.0, gr._Scores()):
         with pytest.raises(TypeError):
             gr.attention(f, f, f, sc, out=s((1, 4, 2, 64)), lse=False)
