@@ -41,6 +41,7 @@ extern "C" {
 /* How scores are formed and which keys a query sees.  The query of row i stands at position p = position + i, key j
  * at position j (gr_attention_step: p = lengths[b] - 1).
  *   score = scale * (q . k);  capped: cap * tanh(score / cap);  then - slopes[h] * |p - j|
+ *   (the distance as f32 holds it: beyond 2^24 neighbouring keys may share one)
  *   key j is seen if (not causal, or j <= p, or j < prefix[b]), and j < lengths[b], and the documents are the same
  * Rows of k and v from lengths[b] on are not read, and a score that is masked is replaced whatever it is: a k that is infinite
  * or NaN has no say in out and lse of the queries that do not see it.  (A v below lengths[b], or in the gradient a k, v, q or dout, that

@@ -12,8 +12,8 @@
 // Either may split the keys over workgroups as well (a.splits), which leaves (m, l, sums) for combine().
 //
 // Measured, bfloat16: 16 heads of 8192 causal rows of 128 values, a beginning seen whole, 0.40 ms (own rows: matrix cores busy 61 % of the cycles, vector units 55 %, the card's power
-// lowers the clock to 1.65 GHz); a capped prompt of 8192 rows of 256 values 0.73 ms (vector units 59 %: a tanh and an exponential per score); single tokens of
-// 32 sequences of 4096 to 8192 keys 0.16 ms (own keys: 4.9 TB/s of the 6.0 of a copy).
+// lowers the clock to 1.65 GHz); a capped prompt of 8192 rows of 256 values 0.70 to 0.73 ms (vector units 59 %: a tanh and an exponential per score; matrix cores 35 %, waves wait 42 %); single tokens of
+// 32 sequences of 4096 to 8192 keys 0.165 ms (own keys: 4.9 TB/s of the 6.0 of a copy).
 #pragma once
 
 #include "attention_kernels.h"
