@@ -16,7 +16,7 @@
  *     to infinity (2^128 - 2^119 = 3.396e38 and more) counts as infinite and gives NaN.  Scores, probabilities, statistics and sums are
  *     f32; with bf16 tensors a probability, or a score's gradient, is rounded to bf16 where it enters the next product (not the probabilities of
  *     gr_attention with rest, nor of calls of at most 32 queries times heads per head of k).  The gradient forms
- *     probabilities from lse, which f32 holds to |lse| 2^-24, and their relative error is as large; and it carries sums 2^32 times as large: dv, dq / scale and dk / scale
+ *     probabilities from lse, which f32 holds to |lse| 2^-24, and is off by as much relatively (keys all 10^6 away from a query under a slope of 1: 6 %); and it carries sums 2^32 times as large: dv, dq / scale and dk / scale
  *     (with no part of their sums) may not pass 2^95 in size, beyond it they are infinite or NaN.
  *   - Shapes: q, out, rest, dout, dq (B, N, H, D); k, v, dk, dv (B, M, HK, D) with H a multiple of HK: head h of q reads head
  *     h / (H / HK) of k and v.  1 <= D <= 256.  Any strides, as long as the D values of a row are neighbours
@@ -46,13 +46,13 @@ extern "C" {
  * Rows of k and v from lengths[b] on are not read, and a score that is masked is replaced whatever it is: a k that is infinite
  * or NaN has no say in out and lse of the queries that do not see it.  (A v below lengths[b], or in the gradient a k, v, q or dout, that
  * is infinite or NaN may reach rows of its tile that do not see it, as 0 * inf does in a plain product.)
- * A query that is NaN, or sees a score that is NaN or +inf, has NaN in out and lse, at every size. */
+ * A query that sees a score that is NaN or +inf (which a q that is NaN makes of all) has NaN in out and lse, at every size. */
 typedef struct {
   double scale;         /* 1e-28 .. 1e30 */
   double cap;           /* 0 = none; 1e-30 .. 1e30, and scale / cap 1e-37 .. 1e38 */
   gr_array slopes;      /* f32 (H), not trained: no gradient; 0 = none */
   int causal;           /* 1: a query sees keys up to its own position */
-  int64_t position;     /* of query 0, -2^31 .. 2^31 */
+  int64_t position;     /* of query 0, -2^31 .. 2^31; with slopes no further than 2^24 from where the keys begin and end */
   gr_array prefix;      /* i32 (B): keys before it are seen by every query; 0 = none.  Only with causal */
   gr_array q_documents; /* i32 (B, N) and (B, M): a query sees keys of its own document; numbers below zero stand for */
   gr_array k_documents; /*   no document: such rows see nothing, such keys are not seen.  0, 0 = none */

@@ -19,6 +19,7 @@ namespace gr {
 namespace attn {
 
 constexpr int64_t LIMIT = (int64_t(1) << 30) - 512;   // rows of queries of one head of k, and keys
+constexpr int64_t FAR = int64_t(1) << 24;             // of queries from the keys, where distances count
 constexpr int64_t THREADS = int64_t(1) << 32;         // what a launch may not reach
 constexpr int64_t GROUPS = THREADS / 512 - 8;         // workgroups of the largest size (and what grid_of rounds up)
 
@@ -279,6 +280,8 @@ static gr_status take_scores(Call& c, const gr_scores* s, Args* a, bool step) {
   if (!s->q_documents != !s->k_documents) return c.error(GR_ERR_ARG, "documents of queries and of keys are given together");
   if (step && (s->causal || s->position || s->prefix || s->q_documents)) return c.error(GR_ERR_ARG, "causal, position, prefix and documents have no meaning for a single token");
   if (step && !s->lengths) return c.error(GR_ERR_ARG, "lengths are missing");
+  // (behind 2^24 f32 holds neither single distances nor an lse of which a probability could be formed again)
+  if (s->slopes && !step && (s->position > a->M + FAR || s->position + a->N < -FAR)) return c.error(GR_ERR_ARG, "with slopes, the queries stand within 2^24 of the keys");
   if (s->slopes) TRY(c.take(s->slopes, "slopes", GR_F32, {a->H}, false));
   if (s->prefix) TRY(c.take(s->prefix, "prefix", GR_I32, {a->B}, false));
   if (s->lengths) TRY(c.take(s->lengths, "lengths", GR_I32, {a->B}, false));

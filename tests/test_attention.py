@@ -252,6 +252,22 @@ def test_scales_and_caps_that_no_float_holds_are_refused(dry):
         gr.attention(q, q, q, dry.scores(causal=True, **kw), out=o, lse=lse)
 
 
+def test_queries_far_from_all_keys_under_a_bias_are_refused(dry):
+    """Behind 2^24 positions f32 holds no single distance, and no lse of which the gradient could form a probability again."""
+    s = Specs(dry)
+    q, k, o, lse, slopes = s((1, 5, 2, 64)), s((1, 9, 2, 64)), s((1, 5, 2, 64)), s((1, 2, 5)), s((2,))
+    far = 1 << 24
+    for position, ok in ((9 + far, True), (10 + far, False), (-far - 5, True), (-far - 6, False), (-(1 << 31), False), (1 << 31, False)):
+        for sc, may in ((dry.scores(slopes=slopes, position=position), ok), (dry.scores(position=position), True)):
+            calls = [lambda: gr.attention(q, k, k, sc, out=o, lse=lse),
+                     lambda: gr.attention_grad(q, q, k, k, sc, q, lse, dq=o, dk=s((1, 9, 2, 64)), dv=s((1, 9, 2, 64)))]
+            for call in calls:
+                if may:
+                    call()
+                else:
+                    refused("GR_ERR_ARG", call)
+
+
 def test_what_python_is_given_wrong_is_said_so(dry):
     """Element types, ranks and objects that do not fit, with and without results given; a context without a device has no memory for new ones."""
     s = Specs(dry)
