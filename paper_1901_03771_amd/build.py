@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgrumpy_hip.so")
 SOURCES = ["recorder.cpp", "plan.cpp", "codegen.cpp", "runtime.cpp", "interp.cpp", "plancache.cpp", "stream_kernels.hip", "interp_kernel.hip", "static_scratch.hip",
-           "attention.cpp", "attention_parts.hip", "rotary.hip", "attention_forward_bf16.hip", "attention_forward_f32.hip", "attention_grad_q_bf16.hip", "attention_grad_q_f32.hip",
+           "attention.cpp", "scaled.cpp", "attention_parts.hip", "rotary.hip", "quantize.hip", "scaled_dot.hip", "norm.hip", "attention_forward_bf16.hip", "attention_forward_f32.hip", "attention_grad_q_bf16.hip", "attention_grad_q_f32.hip",
            "attention_grad_kv_bf16.hip", "attention_grad_kv_f32.hip"]
 
 

@@ -148,11 +148,11 @@ struct gr_ctx {
   size_t scan_cells_bytes = 0;
   uint32_t scan_epoch = 0;
 
-  // temporary memory of the attention calls, and blocks that a captured call has used and that were outgrown since
-  void* attention_space = nullptr;
-  size_t attention_space_bytes = 0;
-  bool attention_captured = false;
-  std::vector<std::pair<void*, size_t>> attention_kept;
+  // temporary memory of the calls that launch kernels of their own (call.h), and blocks that a captured call has used and that were outgrown since
+  void* call_space = nullptr;
+  size_t call_space_bytes = 0;
+  bool call_captured = false;
+  std::vector<std::pair<void*, size_t>> call_kept;
 
   // gr_materialize_into_static: this device's copy of the library's static device array, and the
   // part of it the running request has taken (static_mode is set for the duration of such a call)

@@ -167,7 +167,10 @@ struct NodeIdLess {
 };
 using NodeSet = std::set<const Node*, NodeIdLess>;
 
-inline size_t itemsize(gr_dtype dt) { return dt == GR_I64 ? 8 : dt == GR_BF16 ? 2 : 4; }
+inline size_t itemsize(gr_dtype dt) { return dt == GR_I64 ? 8 : dt == GR_BF16 ? 2 : dt == GR_E4M3 ? 1 : 4; }
+// Types that only the calls with kernels of their own compute with (attention.cpp, scaled.cpp): leaves and views of leaves.
+inline bool narrow(gr_dtype dt) { return dt == GR_BF16 || dt == GR_E4M3; }
+constexpr const char* NARROW_ONLY = "bf16 and e4m3 arrays are operands of the attention, rotary, norm and 8-bit calls only";
 
 // ---- plan --------------------------------------------------------------------
 

@@ -176,8 +176,8 @@ Plan::~Plan() {
 }
 
 gr_status make_plan(gr_ctx* c, Node* root, Plan* plan) {
-  // (no other operation records a node of this type: the root is all there is to check)
-  if (root->dtype == GR_BF16) return fail(c, GR_ERR_DTYPE, "bf16 arrays are operands of the attention and rotary calls only");
+  // (no other operation records a node of these types: the root is all there is to check)
+  if (narrow(root->dtype)) return fail(c, GR_ERR_DTYPE, NARROW_ONLY);
   if (!c->opt_plan_cache || root->kind == Kind::SCALAR) return make_plan_uncached(c, root, plan);
   // (the context's lists are taken out while they are in use: planning a request may plan another one)
   struct Taken {

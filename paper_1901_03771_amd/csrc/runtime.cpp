@@ -1197,8 +1197,8 @@ gr_status gr_ctx_destroy(gr_ctx* ctx) {
   while (!ctx->programs.empty()) program_free(ctx, ctx->programs.back());
   if (ctx->workspace) ctx_free(ctx, ctx->workspace, ctx->workspace_bytes);
   if (ctx->scan_cells) ctx_free(ctx, ctx->scan_cells, ctx->scan_cells_bytes);
-  if (ctx->attention_space) ctx_free(ctx, ctx->attention_space, ctx->attention_space_bytes);
-  for (auto& k : ctx->attention_kept) ctx_free(ctx, k.first, k.second);
+  if (ctx->call_space) ctx_free(ctx, ctx->call_space, ctx->call_space_bytes);
+  for (auto& k : ctx->call_kept) ctx_free(ctx, k.first, k.second);
   for (auto& kv : ctx->cache) if (kv.second.module) (void)hipModuleUnload(kv.second.module);
   for (auto& p : ctx->prof) { (void)hipEventDestroy(p.e0); (void)hipEventDestroy(p.e1); }
   for (hipEvent_t e : ctx->event_pool) (void)hipEventDestroy(e);
@@ -1490,7 +1490,7 @@ extern "C" gr_status gr_assign(gr_ctx* ctx, gr_array dst, gr_array value) {
   OutSpec spec;
   if (!resolve_view_rt(d, &base, &spec.base, spec.strides)) return fail(ctx, GR_ERR_UNSUPPORTED, "assign: destination is not (a view of) a materialised array");
   if (v->dtype != d->dtype) return fail(ctx, GR_ERR_DTYPE, "assign: element types differ");
-  if (d->dtype == GR_BF16) return fail(ctx, GR_ERR_DTYPE, "assign: bf16 arrays are operands of the attention and rotary calls only");
+  if (narrow(d->dtype)) return fail(ctx, GR_ERR_DTYPE, std::string("assign: ") + NARROW_ONLY);
   if (v->ndim != d->ndim) return fail(ctx, GR_ERR_SHAPE, "assign: shapes differ");
   for (int k = 0; k < d->ndim; ++k) {
     if (v->shape[k] != d->shape[k]) return fail(ctx, GR_ERR_SHAPE, "assign: shapes differ");

@@ -24,7 +24,7 @@ from typing import Optional, Sequence
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("GRUMPY_HIP_LIB", os.path.join(_HERE, "libgrumpy_hip.so"))
 
-GR_F32, GR_I32, GR_I64, GR_BF16 = 0, 1, 2, 3
+GR_F32, GR_I32, GR_I64, GR_BF16, GR_E4M3 = 0, 1, 2, 3, 4
 GR_NEG, GR_ABS, GR_EXP, GR_LOG, GR_SQRT, GR_SQUARE, GR_TANH, GR_ERF = range(8)
 GR_ADD, GR_SUB, GR_MUL, GR_DIV, GR_MAXIMUM, GR_MINIMUM, GR_POW_INT = range(16, 23)
 _UNARY = {"neg": 0, "abs": 1, "exp": 2, "log": 3, "sqrt": 4, "square": 5, "tanh": 6, "erf": 7}
@@ -42,6 +42,7 @@ SYMBOLS = [
     "gr_is_materialized", "gr_data_ptr", "gr_retain", "gr_release", "gr_plan_describe", "gr_plan_source",
     "gr_plan_compile", "gr_compile_wait", "gr_stats", "gr_profile_reset", "gr_profile_read", "gr_stream_copy", "gr_stream_read",
     "gr_attention", "gr_attention_grad", "gr_attention_step", "gr_rotary",
+    "gr_rms_norm", "gr_rms_norm_grad", "gr_quantize", "gr_dot_scaled",
 ]
 
 
@@ -112,6 +113,9 @@ def lib():
         "gr_attention": [P, PP(_Scores)] + [U64] * 6, "gr_attention_grad": [P, PP(_Scores)] + [U64] * 10,
         "gr_attention_step": [P, PP(_Scores)] + [U64] * 4,
         "gr_rotary": [P, U64, U64, I64, P, I, I, I, ctypes.c_double, U64],
+        "gr_rms_norm": [P, U64, U64, U64, ctypes.c_double, ctypes.c_double, U64, U64, U64],
+        "gr_rms_norm_grad": [P, U64, U64, U64, U64, ctypes.c_double, ctypes.c_double, U64, U64],
+        "gr_quantize": [P, U64, I, I, U64, U64], "gr_dot_scaled": [P] + [U64] * 5,
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -293,7 +297,8 @@ class Context:
             torch = _torch()
             if not isinstance(t, torch.Tensor):
                 raise TypeError("expected a torch.Tensor on the GPU")
-            _TORCH_DTYPES.update({torch.float32: GR_F32, torch.int32: GR_I32, torch.int64: GR_I64, torch.bfloat16: GR_BF16})
+            _TORCH_DTYPES.update({torch.float32: GR_F32, torch.int32: GR_I32, torch.int64: GR_I64, torch.bfloat16: GR_BF16,
+                                  torch.float8_e4m3fn: GR_E4M3})
             if t.dtype not in _TORCH_DTYPES:
                 raise GrError(3, f"unsupported dtype {t.dtype}")
             dt = _TORCH_DTYPES[t.dtype]
@@ -494,9 +499,9 @@ class _ArrayMethods:
         Section 2) and returns its value as a torch tensor on the context's device: a copy by default,
         with copy=False a tensor that shares the node's storage (and keeps this handle alive)."""
         torch = _torch()
-        # (the array interface has no bfloat16: those are handed over as 16-bit integers and seen as what they are)
+        # (the array interface has no bfloat16 and no e4m3: those are handed over as integers and seen as what they are)
         dt = {GR_F32: (torch.float32, "<f4", 4), GR_I32: (torch.int32, "<i4", 4), GR_I64: (torch.int64, "<i8", 8),
-              GR_BF16: (torch.bfloat16, "<i2", 2)}[self.dtype_code]
+              GR_BF16: (torch.bfloat16, "<i2", 2), GR_E4M3: (torch.float8_e4m3fn, "|i1", 1)}[self.dtype_code]
         shape = self.shape
         if 0 in shape:
             return torch.empty(shape, dtype=dt[0], device=f"cuda:{self.ctx.device}")
@@ -851,21 +856,31 @@ def _tensor(ctx: Context, a: "Array") -> int:
 
 
 def _result_array(ctx: Context, given, shape, dtype: int) -> "Array":
-    """The array that a call writes: the caller's, or a new one over memory from torch, which hands a stream the memory that work queued on
-    that stream was the last to use: it is taken for the stream of the context, whichever is torch's at the time."""
+    """The array that a call writes: the caller's, or a new one."""
     if given is not None:
         return given
     if dtype not in (GR_F32, GR_BF16):
         raise GrError(3, "operands must be f32 or bf16")
+    return _new_array(ctx, shape, dtype)
+
+
+def _new_array(ctx: Context, shape, dtype: int, axes=None) -> "Array":
+    """An array over memory from torch, which hands a stream the memory that work queued on
+    that stream was the last to use: it is taken for the stream of the context, whichever is torch's at the time.  axes: the order in which the
+    axes lie in memory."""
     if ctx.device < 0:
         raise GrError(11, "the context has no device for a new result")
     torch = _torch()
-    dtype = torch.float32 if dtype == GR_F32 else torch.bfloat16
+    dtype = {GR_F32: torch.float32, GR_BF16: torch.bfloat16, GR_E4M3: torch.float8_e4m3fn}[dtype]
+    if axes is not None:
+        shape = tuple(shape[i] for i in axes)
     if torch.cuda.current_stream(ctx.device).cuda_stream == ctx._stream:
         t = torch.empty(shape, device=f"cuda:{ctx.device}", dtype=dtype)
     else:
         with torch.cuda.stream(torch.cuda.ExternalStream(ctx._stream, ctx.device)):
             t = torch.empty(shape, device=f"cuda:{ctx.device}", dtype=dtype)
+    if axes is not None:
+        t = t.permute([axes.index(i) for i in range(len(axes))])
     a = ctx.array(t)
     a._view = True   # nobody else holds the tensor: the handle keeps it through materialize() and torch()
     return a
@@ -951,6 +966,106 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
     arr = isinstance(positions, Array)
     st = lib().gr_rotary(ctx._p, hx, _tensor(ctx, positions) if arr else 0, 0 if arr else _place(positions), frequencies, n,
                          builtins.bool(interleaved), builtins.bool(inverse), factor, _tensor(ctx, out))
+    if st:
+        ctx.check(st)
+    return out
+
+
+# ---- norms, 8-bit tensors with scales and their products (include/grumpy_hip_scaled.h) ------------------------------------
+
+def _float_code(a: "Array") -> int:
+    """The element type of a new result like `a`: f32 or bf16."""
+    dtype = a.dtype_code
+    if dtype not in (GR_F32, GR_BF16):
+        raise GrError(3, "operands must be f32 or bf16")
+    return dtype
+
+
+def _optional(ctx: Context, a) -> int:
+    return 0 if a is None else _tensor(ctx, a)
+
+
+def _new_scales(ctx: Context, rows, values: int) -> "Array":
+    """Scales of rows, those of neighbouring rows side by side: that is how a product reads them."""
+    n = len(rows)
+    return _new_array(ctx, tuple(rows) + ((values + 127) // 128,), GR_F32, axes=[n] + list(range(n)))
+
+
+def rms_norm(x: "Array", weight=None, residual=None, eps: float = 1e-6, offset: float = 0.0, out=None, total=None, scales=None, eight: bool = False):
+    """total = x + residual and out = total / sqrt(mean(total ** 2) + eps) * (offset + weight) over the last axis (gr_rms_norm); returns
+    (out, total, scales), x for total where there is no residual.  What is not given is new; total=False: not wanted, returned as None.  An e4m3 out, or
+    eight=True, is the result in 8 bits with scales of rows, as ``dot_scaled`` takes it; else scales is None."""
+    ctx = _context_of(x)
+    hx, hr, hw = _tensor(ctx, x), _optional(ctx, residual), _optional(ctx, weight)
+    if out is None or (total is None and residual is not None) or scales is None:
+        shape = x.shape
+        if not shape:
+            raise GrError(2, "rms_norm: x has no axes")
+    if out is None:
+        out = _new_array(ctx, shape, GR_E4M3 if eight else _float_code(x))
+    ho = _tensor(ctx, out)
+    if scales is None and (eight or out.dtype_code == GR_E4M3):
+        scales = _new_scales(ctx, shape[:-1], shape[-1])
+    if total is False:
+        total = None
+    elif total is None and residual is not None:
+        total = _new_array(ctx, shape, _float_code(x))
+    st = lib().gr_rms_norm(ctx._p, hx, hr, hw, eps, offset, _optional(ctx, total), ho, _optional(ctx, scales))
+    if st:
+        ctx.check(st)
+    return out, x if residual is None else total, scales
+
+
+def rms_norm_grad(dout: "Array", total: "Array", weight=None, dtotal=None, eps: float = 1e-6, offset: float = 0.0, dx=None, dweight=None):
+    """The gradients of x (and of residual alike) and of weight (gr_rms_norm_grad) for the gradients of out and, by other ways, of total; returns
+    (dx, dweight).  dweight=False, or no weight: not wanted, returned as None."""
+    ctx = _context_of(total)
+    ht, hd, hw, hm = _tensor(ctx, total), _tensor(ctx, dout), _optional(ctx, weight), _optional(ctx, dtotal)
+    if dx is None:
+        dx = _new_array(ctx, total.shape, _float_code(total))
+    if dweight is None and weight is not None:
+        dweight = _new_array(ctx, weight.shape, GR_F32)
+    elif dweight is False:
+        dweight = None
+    st = lib().gr_rms_norm_grad(ctx._p, hd, ht, hw, hm, eps, offset, _tensor(ctx, dx), _optional(ctx, dweight))
+    if st:
+        ctx.check(st)
+    return dx, dweight
+
+
+def quantize(x: "Array", blocks: bool = False, transposed: bool = False, out=None, scales=None):
+    """x (M, K) in 8 bits (gr_quantize); returns (out, scales).  128 neighbours of a row share a scale, or with blocks=True 128 x 128 values;
+    transposed=True: the same of x.T."""
+    ctx = _context_of(x)
+    hx = _tensor(ctx, x)
+    if out is None or scales is None:
+        shape = x.shape
+        if len(shape) != 2:
+            raise GrError(2, "quantize: x is (M, K)")
+        rows, cols = shape[::-1] if transposed else shape
+    if out is None:
+        out = _new_array(ctx, (rows, cols), GR_E4M3)
+    if scales is None:
+        scales = _new_scales(ctx, ((rows + 127) // 128 if blocks else rows,), cols)
+    st = lib().gr_quantize(ctx._p, hx, builtins.bool(blocks), builtins.bool(transposed), _tensor(ctx, out), _tensor(ctx, scales))
+    if st:
+        ctx.check(st)
+    return out, scales
+
+
+def dot_scaled(a: "Array", a_scales: "Array", b: "Array", b_scales: "Array", out=None, dtype: int = GR_BF16):
+    """a b.T (gr_dot_scaled) of the values that a (M, K) and b (N, K), e4m3, stand for; a_scales of rows, b_scales of rows or of blocks.  A new out is
+    of `dtype`, GR_BF16 or GR_F32."""
+    ctx = _context_of(a)
+    h = [_tensor(ctx, t) for t in (a, a_scales, b, b_scales)]
+    if out is None:
+        m, n = a.shape, b.shape
+        if len(m) != 2 or len(n) != 2:
+            raise GrError(2, "dot_scaled: a is (M, K) and b (N, K)")
+        if dtype not in (GR_F32, GR_BF16):
+            raise GrError(3, "out must be f32 or bf16")
+        out = _new_array(ctx, (m[0], n[0]), dtype)
+    st = lib().gr_dot_scaled(ctx._p, *h, _tensor(ctx, out))
     if st:
         ctx.check(st)
     return out
