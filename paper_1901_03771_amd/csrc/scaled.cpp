@@ -262,10 +262,7 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   TRY(c.take(out, "out", dt, {M, N}, true));
   TRY(c.neighbours({{a, "a"}, {b, "b"}, {out, "out"}}));
   Dot d;
-  d.mt = (int)blocks_of(M);
-  d.nt = (int)blocks_of(N);
-  const int64_t tiles = (int64_t)d.mt * d.nt;
-  if (tiles > GROUPS) return c.error(GR_ERR_UNSUPPORTED, "more results than a launch holds");
+  if (blocks_of(M) * blocks_of(N) > GROUPS) return c.error(GR_ERR_UNSUPPORTED, "more results than a launch holds");
   TRY(c.settle());
   if (M == 0 || N == 0) return GR_OK;
   d.a = (const uint8_t*)c.view(a).data;
@@ -284,14 +281,22 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   d.N = (int)N;
   d.K = (int)K;
   d.KB = (int)KB;
-  d.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, KB / 4));
+  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes.
+  auto direct = [&](const uint8_t* p, int64_t s) { return (uintptr_t)p % 16 == 0 && s % 16 == 0 && K % 16 == 0 && (s == 0 || (s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
+  int form = direct(d.a, M > 1 ? d.a_s : 0) && (M == 1 || d.a_s > 0) && direct(d.b, N > 1 ? d.b_s : 0) && (N == 1 || d.b_s > 0) ? DOT_DIRECT : DOT_STAGED;
+  if (form == DOT_DIRECT && M >= 256 && N >= 256 && ((M + 255) / 256) * ((N + 255) / 256) >= 192) form = DOT_LARGE;
+  const int64_t side = form == DOT_LARGE ? 256 : 128;
+  d.mt = (int)((M + side - 1) / side);
+  d.nt = (int)((N + side - 1) / side);
+  const int64_t tiles = (int64_t)d.mt * d.nt;
+  d.splits = form == DOT_LARGE ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, KB / 4));
   if (d.splits > 1) {
     char* ws;
     TRY(c.space(rounded((size_t)d.splits * M * N * 4), &ws));
     d.parts = (float*)ws;
   }
   const int type = Call::type_of(dt);
-  TRY(c.launch("gr_dot_scaled", [&] { return dot(d, DOT_STAGED, blocks, type, ctx->stream); }));
+  TRY(c.launch("gr_dot_scaled", [&] { return dot(d, form, blocks, type, ctx->stream); }));
   if (d.splits > 1) TRY(c.launch("gr_dot_scaled_join", [&] { return dot_join(d, type, ctx->stream); }));
   return GR_OK;
 }

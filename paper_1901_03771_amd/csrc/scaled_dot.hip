@@ -66,6 +66,9 @@ static __device__ __forceinline__ i32x8 operand(const GR_LDS char* tile, int r, 
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// Waits for this wave's loads and LDS accesses, then for everybody's.
+static __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <class T>
 static __device__ __forceinline__ void store4(T* row, int n, int N, f32x4 v) {
   if (n + 4 <= N) {
@@ -96,6 +99,36 @@ static __device__ __forceinline__ Place place_of(const Dot& d) {
   return p;
 }
 
+// A tile of rows in flight straight into LDS (buffer_load_dwordx4 .. lds: lane L of a wave fills the 16 bytes at L of its kilobyte, so the twist is in the lane's
+// address).  The buffer ends with the last valid row, and a place behind the end of a row is given an address behind it: both read zeros.
+template <int ROWS, int THREADS>
+struct Flight {
+  static constexpr int N = ROWS * 8 / THREADS, STEP = THREADS / 8;
+  static_assert(N * THREADS == ROWS * 8 && STEP % 16 == 0, "whole chunks for every thread, the same twist for all of them");
+  i32x4 rsrc;
+  uint32_t first, step;      // of the thread's first chunk, and from one to the next
+  int at;                    // of the chunk in the row
+  uint32_t lds0;
+  __device__ __forceinline__ Flight(const uint8_t* base, int64_t stride, int rows, int K, int tid, GR_LDS char* tile) {
+    const uint64_t b = (uint64_t)base;
+    const int r = tid / 8;
+    rsrc = i32x4{__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), __builtin_amdgcn_readfirstlane((rows - 1) * (int)stride + K), 0x00027000};
+    at = ((tid % 8) ^ twist(r)) * 16;
+    first = r * (uint32_t)stride + at;
+    step = STEP * (uint32_t)stride;
+    lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile + (tid & ~63) * 16);
+  }
+  __device__ __forceinline__ void go(int kb, int K, uint32_t stage) const {
+    const bool inside = kb * 128 + at < K;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint32_t off = inside ? first + kb * 128 + n * step : 0x80000000u;
+      // (the statement leaves the scalar condition code alone; wait states: M0, and a base that a vector instruction wrote)
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off), "s"(rsrc), "s"(lds0 + stage + n * THREADS * 16) : "memory", "m0");
+    }
+  }
+};
+
 // A tile of TM rows of a by TN rows of b, waves WM x WN.  Two stages of tiles in LDS: while one is multiplied, the next block's is under way, through
 // registers (any strides) or straight into LDS (DIRECT).
 template <int TM, int TN, int WM, int WN, bool DIRECT, bool BLOCKS, class OUT>
@@ -103,11 +136,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   constexpr int THREADS = WM * WN * 64, I = TN / WN / 16, J = TM / WM / 16, NB = TN / BLOCK;
   constexpr int CA = TM * 8 / THREADS, CB = TN * 8 / THREADS;               // chunks of a thread
   static_assert(CA * THREADS == TM * 8 && CB * THREADS == TN * 8, "whole chunks for every thread");
-  extern __shared__ __attribute__((aligned(1024))) char memory[];
-  GR_LDS char* const lds = (GR_LDS char*)memory;
   constexpr int STAGE = (TM + TN) * 128;
   // factors of a stage: of the rows of a, for each block of rows of b (BLOCKS) or apart from those of the rows of b
   constexpr int FACTORS = BLOCKS ? NB * TM : TM + TN;
+  __shared__ __attribute__((aligned(1024))) char memory[2 * (STAGE + FACTORS * 4)];
+  GR_LDS char* const lds = (GR_LDS char*)memory;
   GR_LDS float* const factors = (GR_LDS float*)(lds + 2 * STAGE);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 15, g = lane >> 4;
   const int wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
@@ -118,8 +151,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   const uint8_t* const b = d.b + (int64_t)n0 * d.b_s;
 
   i32x4 staged[DIRECT ? 1 : CA + CB];
+  const Flight<TM, THREADS> fa(a, d.a_s, rows_a, d.K, tid, lds);
+  const Flight<TN, THREADS> fb(b, d.b_s, rows_b, d.K, tid, lds + TM * 128);
   auto fetch = [&](int kb, int stage) {
-    if constexpr (!DIRECT) {
+    if constexpr (DIRECT) {
+      fa.go(kb, d.K, stage * STAGE);
+      fb.go(kb, d.K, stage * STAGE);
+    } else {
 #pragma unroll
       for (int c = 0; c < CA; ++c) {
         const int i = c * THREADS + tid, r = i / 8;
@@ -142,29 +180,20 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     }
   };
   // The factors of a block, a thread each.  (Rows behind the last have the last one's: their results go nowhere.)
-  constexpr int EACH = (FACTORS + THREADS - 1) / THREADS;
-  float factor[EACH];
+  static_assert(FACTORS <= THREADS && TM % 64 == 0, "a factor a thread, of the same operand across a wave");
+  const bool of_a = BLOCKS || tid < TM;
+  const float* const row_factor = of_a ? d.sa + (int64_t)(m0 + min(tid % TM, rows_a - 1)) * d.sa_m : d.sb + (int64_t)(n0 + min(tid - TM, rows_b - 1)) * d.sb_n;
+  const int64_t row_step = of_a ? d.sa_k : d.sb_k;
+  const float* const block_factor = d.sb + (int64_t)min(n0 / BLOCK + __builtin_amdgcn_readfirstlane(tid / TM), (d.N - 1) / BLOCK) * d.sb_n;
+  float factor = 0.0f;
   auto fetch_factors = [&](int kb) {
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int i = e * THREADS + tid;
-      if (FACTORS % THREADS != 0 && i >= FACTORS) continue;
-      if constexpr (BLOCKS) {
-        const int r = min(i % TM, rows_a - 1), nb = min((n0 / BLOCK) + i / TM, (d.N - 1) / BLOCK);
-        factor[e] = d.sa[(m0 + r) * d.sa_m + kb * d.sa_k] * d.sb[nb * d.sb_n + kb * d.sb_k];
-      } else {
-        const int r = i < TM ? min(i, rows_a - 1) : min(i - TM, rows_b - 1);
-        factor[e] = i < TM ? d.sa[(m0 + r) * d.sa_m + kb * d.sa_k] : d.sb[(n0 + r) * d.sb_n + kb * d.sb_k];
-      }
-    }
+    if (FACTORS < THREADS && tid >= FACTORS) return;
+    factor = row_factor[kb * row_step];
   };
-  auto settle_factors = [&](int stage) {
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int i = e * THREADS + tid;
-      if (FACTORS % THREADS != 0 && i >= FACTORS) continue;
-      factors[stage * FACTORS + i] = factor[e];
-    }
+  auto settle_factors = [&](int kb, int stage) {
+    if (FACTORS < THREADS && tid >= FACTORS) return;
+    if constexpr (BLOCKS) factor *= ((const __attribute__((address_space(4))) float*)block_factor)[kb * d.sb_k];
+    factors[stage * FACTORS + tid] = factor;
   };
 
   f32x4 acc[I][J];
@@ -174,47 +203,59 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   if (first < last) {
-    fetch(first, 0);
     fetch_factors(first);
+    fetch(first, 0);
     settle(0);
-    settle_factors(0);
+    settle_factors(first, 0);
   }
-  __syncthreads();
+  arrive();
   for (int kb = first; kb < last; ++kb) {
     const int stage = (kb - first) & 1;
-    const bool more = kb + 1 < last;
-    if (more) {
-      fetch(kb + 1, stage ^ 1);
-      fetch_factors(kb + 1);
-    }
+    // (behind the last block: another split's or zeros, which nothing takes)
+    fetch_factors(min(kb + 1, last - 1));
+    fetch(kb + 1, stage ^ 1);
     const GR_LDS char* const ta = lds + stage * STAGE;
     const GR_LDS char* const tb = ta + TM * 128;
     const GR_LDS float* const f = factors + stage * FACTORS;
-    Operand<sizeof(OUT) == 4> x[J], y;
+    // Columns 16 at a time: while the matrix cores have those of step i, the sums of step i - 1 are added and the operand of step i + 1 is read.
+    constexpr bool PROPER = sizeof(OUT) == 4;
+    Operand<PROPER> x[J];
+    i32x8 y[2];
+    f32x4 z[2][J], t[2];
     float s[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       x[j].set(operand(ta, wm + 16 * j + l, g));
       s[j] = f[(BLOCKS ? wn / BLOCK * TM : 0) + wm + 16 * j + l];
     }
+    y[0] = operand(tb, wn + l, g);
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-      y.set(operand(tb, wn + 16 * i + l, g));
-      f32x4 t = {1.0f, 1.0f, 1.0f, 1.0f};
-      if constexpr (!BLOCKS) t = *(const GR_LDS f32x4*)(f + TM + wn + 16 * i + 4 * g);
+    for (int i = 0; i <= I; ++i) {
+      if (i + 1 < I) y[(i + 1) & 1] = operand(tb, wn + 16 * (i + 1) + l, g);
+      if constexpr (!BLOCKS) if (i < I) t[i & 1] = *(const GR_LDS f32x4*)(f + TM + wn + 16 * i + 4 * g);
+      if (i < I) {
+        Operand<PROPER> o;
+        o.set(y[i & 1]);
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        f32x4 z = block_product(y, x[j]);
-        if constexpr (!BLOCKS) z *= t;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(z[e], s[j], acc[i][j][e]);
+        for (int j = 0; j < J; ++j) z[i & 1][j] = block_product(o, x[j]);
       }
+      if (i > 0) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = BLOCKS ? z[(i - 1) & 1][j][e] : z[(i - 1) & 1][j][e] * t[(i - 1) & 1][e];
+            acc[i - 1][j][e] = __builtin_fmaf(v, s[j], acc[i - 1][j][e]);
+          }
+        // (kept here: moved behind the loop's end, the sums would leave all products of the block in registers, and a branch between them and their use)
+#pragma unroll
+        for (int j = 0; j < J; ++j) asm volatile("" : "+v"(acc[i - 1][j]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (more) {
-      settle(stage ^ 1);
-      settle_factors(stage ^ 1);
-    }
-    __syncthreads();
+    settle(stage ^ 1);
+    settle_factors(min(kb + 1, last - 1), stage ^ 1);
+    arrive();
   }
 
 #pragma unroll
@@ -244,13 +285,14 @@ __global__ __launch_bounds__(256) void gr_dot_scaled_join_kernel(const Dot d) {
 
 template <int TM, int TN, int WM, int WN, bool DIRECT, bool BLOCKS, class OUT>
 static hipError_t launch(const Dot& d, hipStream_t stream) {
-  constexpr size_t lds = 2 * ((TM + TN) * 128 + (BLOCKS ? TN / BLOCK * TM : TM + TN) * 4);
-  gr_dot_scaled_kernel<TM, TN, WM, WN, DIRECT, BLOCKS, OUT><<<dim3((unsigned)(d.mt * d.nt * d.splits)), dim3(WM * WN * 64), lds, stream>>>(d);
+  gr_dot_scaled_kernel<TM, TN, WM, WN, DIRECT, BLOCKS, OUT><<<dim3((unsigned)(d.mt * d.nt * d.splits)), dim3(WM * WN * 64), 0, stream>>>(d);
   return hipGetLastError();
 }
 
 template <bool BLOCKS, class OUT>
 static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
+  if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
+  if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
   return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
 }
 
