@@ -284,7 +284,7 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes.
   auto direct = [&](const uint8_t* p, int64_t s) { return (uintptr_t)p % 16 == 0 && s % 16 == 0 && K % 16 == 0 && (s == 0 || (s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
   int form = direct(d.a, M > 1 ? d.a_s : 0) && (M == 1 || d.a_s > 0) && direct(d.b, N > 1 ? d.b_s : 0) && (N == 1 || d.b_s > 0) ? DOT_DIRECT : DOT_STAGED;
-  if (form == DOT_DIRECT && M >= 256 && N >= 256 && ((M + 255) / 256) * ((N + 255) / 256) >= 192) form = DOT_LARGE;
+  if (form == DOT_DIRECT && dt == GR_BF16 && M >= 256 && N >= 256 && ((M + 255) / 256) * ((N + 255) / 256) >= 192) form = DOT_LARGE;
   const int64_t side = form == DOT_LARGE ? 256 : 128;
   d.mt = (int)((M + side - 1) / side);
   d.nt = (int)((N + side - 1) / side);

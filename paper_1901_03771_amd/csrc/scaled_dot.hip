@@ -8,12 +8,15 @@
 // places below its leading one: sums of normal numbers are off by 1.5e-5 of themselves, at most by 7 x 2^-13 of the sum of their sizes.  A result rounded to bfloat16 does not show it (half a
 // step of it is 2^-8; 1.7e-3 from binary64 with and without).  For a float32 result the operands become bfloat16 on their way from LDS, which holds e4m3 exactly, and four products of 32 places
 // each are summed in float32 proper: 2^-24, at twice the cycles.
+#include <type_traits>
+
 #include "scaled_kernels.h"
 
 namespace gr {
 namespace scaled {
 
 #define GR_LDS __attribute__((address_space(3)))
+#define GR_INLINE __attribute__((always_inline))
 
 // 32 places of a row a lane, as the matrix cores take them: 8-bit, or bfloat16 where sums are to be float32 proper.
 template <bool PROPER> struct Operand;
@@ -100,32 +103,33 @@ static __device__ __forceinline__ Place place_of(const Dot& d) {
 }
 
 // A tile of rows in flight straight into LDS (buffer_load_dwordx4 .. lds: lane L of a wave fills the 16 bytes at L of its kilobyte, so the twist is in the lane's
-// address).  The buffer ends with the last valid row, and a place behind the end of a row is given an address behind it: both read zeros.
+// address).  Each of a thread's chunks has a buffer of its own, in scalar registers, so that one vector register holds its place in all of them; a buffer ends with the last
+// valid row, and a place behind the end of a row is given an address behind it: both read zeros.
 template <int ROWS, int THREADS>
 struct Flight {
   static constexpr int N = ROWS * 8 / THREADS, STEP = THREADS / 8;
   static_assert(N * THREADS == ROWS * 8 && STEP % 16 == 0, "whole chunks for every thread, the same twist for all of them");
-  i32x4 rsrc;
-  uint32_t first, step;      // of the thread's first chunk, and from one to the next
+  i32x4 rsrc[N];
+  uint32_t first;            // of the thread's first chunk
   int at;                    // of the chunk in the row
   uint32_t lds0;
   __device__ __forceinline__ Flight(const uint8_t* base, int64_t stride, int rows, int K, int tid, GR_LDS char* tile) {
-    const uint64_t b = (uint64_t)base;
     const int r = tid / 8;
-    rsrc = i32x4{__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff), __builtin_amdgcn_readfirstlane((rows - 1) * (int)stride + K), 0x00027000};
-    at = ((tid % 8) ^ twist(r)) * 16;
-    first = r * (uint32_t)stride + at;
-    step = STEP * (uint32_t)stride;
-    lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile + (tid & ~63) * 16);
-  }
-  __device__ __forceinline__ void go(int kb, int K, uint32_t stage) const {
-    const bool inside = kb * 128 + at < K;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const uint32_t off = inside ? first + kb * 128 + n * step : 0x80000000u;
-      // (the statement leaves the scalar condition code alone; wait states: M0, and a base that a vector instruction wrote)
-      asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off), "s"(rsrc), "s"(lds0 + stage + n * THREADS * 16) : "memory", "m0");
+      const uint64_t b = (uint64_t)base + n * STEP * stride;
+      const int left = rows - n * STEP;
+      rsrc[n] = i32x4{__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32) & 0xffff),
+                      __builtin_amdgcn_readfirstlane(left > 0 ? (left - 1) * (int)stride + K : 0), 0x00027000};
     }
+    at = ((tid % 8) ^ twist(r)) * 16;
+    first = r * (uint32_t)stride + at;
+    lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)tile + (tid & ~63) * 16);
+  }
+  __device__ __forceinline__ uint32_t place(int kb, int K) const { return kb * 128 + at < K ? first + kb * 128 : 0x80000000u; }
+  __device__ __forceinline__ void go(int n, uint32_t off, uint32_t stage) const {
+    // (the statement leaves the scalar condition code alone; wait states: M0)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off), "s"(rsrc[n]), "s"(lds0 + stage + n * THREADS * 16) : "memory", "m0");
   }
 };
 
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   static_assert(CA * THREADS == TM * 8 && CB * THREADS == TN * 8, "whole chunks for every thread");
   constexpr int STAGE = (TM + TN) * 128;
   // factors of a stage: of the rows of a, for each block of rows of b (BLOCKS) or apart from those of the rows of b
-  constexpr int FACTORS = BLOCKS ? NB * TM : TM + TN;
+  constexpr int USED = BLOCKS ? NB * TM : TM + TN, FACTORS = USED > THREADS ? USED : THREADS;
   __shared__ __attribute__((aligned(1024))) char memory[2 * (STAGE + FACTORS * 4)];
   GR_LDS char* const lds = (GR_LDS char*)memory;
   GR_LDS float* const factors = (GR_LDS float*)(lds + 2 * STAGE);
@@ -153,109 +157,164 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   i32x4 staged[DIRECT ? 1 : CA + CB];
   const Flight<TM, THREADS> fa(a, d.a_s, rows_a, d.K, tid, lds);
   const Flight<TN, THREADS> fb(b, d.b_s, rows_b, d.K, tid, lds + TM * 128);
-  auto fetch = [&](int kb, int stage) {
-    if constexpr (DIRECT) {
-      fa.go(kb, d.K, stage * STAGE);
-      fb.go(kb, d.K, stage * STAGE);
-    } else {
+  // Chunk c of a tile on its way into LDS.
+  auto send = [&](int c, int kb, int stage) GR_INLINE {
+    if (c < CA) fa.go(c, fa.place(kb, d.K), stage * STAGE);
+    else fb.go(c - CA, fb.place(kb, d.K), stage * STAGE);
+  };
+  auto fetch = [&](int kb) GR_INLINE {
 #pragma unroll
-      for (int c = 0; c < CA; ++c) {
-        const int i = c * THREADS + tid, r = i / 8;
-        staged[c] = r < rows_a ? bytes_at(a + r * d.a_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
-      }
+    for (int c = 0; c < CA; ++c) {
+      const int i = c * THREADS + tid, r = i / 8;
+      staged[c] = r < rows_a ? bytes_at(a + r * d.a_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
+    }
 #pragma unroll
-      for (int c = 0; c < CB; ++c) {
-        const int i = c * THREADS + tid, r = i / 8;
-        staged[CA + c] = r < rows_b ? bytes_at(b + r * d.b_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
-      }
+    for (int c = 0; c < CB; ++c) {
+      const int i = c * THREADS + tid, r = i / 8;
+      staged[CA + c] = r < rows_b ? bytes_at(b + r * d.b_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
     }
   };
-  auto settle = [&](int stage) {
-    if constexpr (!DIRECT) {
+  auto settle = [&](int stage) GR_INLINE {
 #pragma unroll
-      for (int c = 0; c < CA + CB; ++c) {
-        const int i = (c < CA ? c : c - CA) * THREADS + tid, r = i / 8;
-        *(GR_LDS i32x4*)(lds + stage * STAGE + (c < CA ? 0 : TM * 128) + r * 128 + ((i % 8 ^ twist(r)) << 4)) = staged[c];
-      }
+    for (int c = 0; c < CA + CB; ++c) {
+      const int i = (c < CA ? c : c - CA) * THREADS + tid, r = i / 8;
+      *(GR_LDS i32x4*)(lds + stage * STAGE + (c < CA ? 0 : TM * 128) + r * 128 + ((i % 8 ^ twist(r)) << 4)) = staged[c];
     }
   };
-  // The factors of a block, a thread each.  (Rows behind the last have the last one's: their results go nowhere.)
-  static_assert(FACTORS <= THREADS && TM % 64 == 0, "a factor a thread, of the same operand across a wave");
+  // The factors of a block, a thread each.  (Rows behind the last have the last one's: their results go nowhere.  Threads without a factor of their own write one that
+  // nothing reads: between a product and its use stands no branch, where the compiler has been seen to count too few wait states.)
+  static_assert(FACTORS == THREADS && TM % 64 == 0, "a factor a thread, of the same operand across a wave");
   const bool of_a = BLOCKS || tid < TM;
   const float* const row_factor = of_a ? d.sa + (int64_t)(m0 + min(tid % TM, rows_a - 1)) * d.sa_m : d.sb + (int64_t)(n0 + min(tid - TM, rows_b - 1)) * d.sb_n;
   const int64_t row_step = of_a ? d.sa_k : d.sb_k;
   const float* const block_factor = d.sb + (int64_t)min(n0 / BLOCK + __builtin_amdgcn_readfirstlane(tid / TM), (d.N - 1) / BLOCK) * d.sb_n;
   float factor = 0.0f;
-  auto fetch_factors = [&](int kb) {
-    if (FACTORS < THREADS && tid >= FACTORS) return;
-    factor = row_factor[kb * row_step];
-  };
-  auto settle_factors = [&](int kb, int stage) {
-    if (FACTORS < THREADS && tid >= FACTORS) return;
-    if constexpr (BLOCKS) factor *= ((const __attribute__((address_space(4))) float*)block_factor)[kb * d.sb_k];
+  auto fetch_factors = [&](int kb) GR_INLINE { factor = row_factor[min(kb, last - 1) * row_step]; };
+  auto settle_factors = [&](int kb, int stage) GR_INLINE {
+    if constexpr (BLOCKS) factor *= ((const __attribute__((address_space(4))) float*)block_factor)[min(kb, last - 1) * d.sb_k];
     factors[stage * FACTORS + tid] = factor;
   };
 
+  // Steps that operands of b are read ahead: LDS is nearly as busy as the matrix cores.  (With factors of their own for b's rows the registers hold one, of tiles of 256 x 256.)
+  constexpr int AHEAD = I == 8 && !BLOCKS ? 1 : 2, RING = 2 * AHEAD;
+  constexpr int EARLY = AHEAD + I / 8;   // steps over which a tile is sent for
+  constexpr bool PROPER = sizeof(OUT) == 4;
   f32x4 acc[I][J];
 #pragma unroll
   for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  if (first < last) {
-    fetch_factors(first);
-    fetch(first, 0);
-    settle(0);
-    settle_factors(first, 0);
-  }
-  arrive();
-  for (int kb = first; kb < last; ++kb) {
-    const int stage = (kb - first) & 1;
-    // (behind the last block: another split's or zeros, which nothing takes)
-    fetch_factors(min(kb + 1, last - 1));
-    fetch(kb + 1, stage ^ 1);
-    const GR_LDS char* const ta = lds + stage * STAGE;
-    const GR_LDS char* const tb = ta + TM * 128;
-    const GR_LDS float* const f = factors + stage * FACTORS;
-    // Columns 16 at a time: while the matrix cores have those of step i, the sums of step i - 1 are added and the operand of step i + 1 is read.
-    constexpr bool PROPER = sizeof(OUT) == 4;
+  // A block begins with the operands of a's rows in registers, and the first of b's; they are read while the last step of the block before it is multiplied, each once the
+  // product that had its registers is on its way.
+  static_assert(I % RING == 0 && EARLY <= I - AHEAD, "operands of b go round their registers, and a tile has time to come");
+  i32x8 raw[J], y[RING];
+  f32x4 t[BLOCKS ? 1 : RING];
+  float s[2][J];
+  auto read_a = [&](int j, auto parity) GR_INLINE {
+    constexpr int P = decltype(parity)::value;
+    raw[j] = operand(lds + P * STAGE, wm + 16 * j + l, g);
+    s[P][j] = factors[P * FACTORS + (BLOCKS ? wn / BLOCK * TM : 0) + wm + 16 * j + l];
+  };
+  auto read_b = [&](int i, auto parity) GR_INLINE {
+    constexpr int P = decltype(parity)::value;
+    y[i % RING] = operand(lds + P * STAGE + TM * 128, wn + 16 * i + l, g);
+    if constexpr (!BLOCKS) t[i % RING] = *(const GR_LDS f32x4*)(factors + P * FACTORS + TM + wn + 16 * i + 4 * g);
+  };
+  auto block = [&](int kb, auto parity) GR_INLINE {
+    constexpr int P = decltype(parity)::value;
+    constexpr std::integral_constant<int, P ^ 1> other;
     Operand<PROPER> x[J];
-    i32x8 y[2];
-    f32x4 z[2][J], t[2];
-    float s[J];
+    f32x4 z[J], before = {1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      x[j].set(operand(ta, wm + 16 * j + l, g));
-      s[j] = f[(BLOCKS ? wn / BLOCK * TM : 0) + wm + 16 * j + l];
+    for (int j = 0; j < J; ++j) x[j].set(raw[j]);
+    if constexpr (!DIRECT) {   // (has branches: before the first product)
+      settle(P ^ 1);
+      fetch(kb + 2);
     }
-    y[0] = operand(tb, wn + l, g);
+    // Columns 16 at a time: four sums of the step before are added, then the registers take the next product.
 #pragma unroll
     for (int i = 0; i <= I; ++i) {
-      if (i + 1 < I) y[(i + 1) & 1] = operand(tb, wn + 16 * (i + 1) + l, g);
-      if constexpr (!BLOCKS) if (i < I) t[i & 1] = *(const GR_LDS f32x4*)(f + TM + wn + 16 * i + 4 * g);
-      if (i < I) {
-        Operand<PROPER> o;
-        o.set(y[i & 1]);
-#pragma unroll
-        for (int j = 0; j < J; ++j) z[i & 1][j] = block_product(o, x[j]);
+      if (i == I - AHEAD) {
+        // All operands of this block have been read: everybody waits for the next one's tiles, and the one after it takes this one's place.
+        settle_factors(kb + 1, P ^ 1);
+        arrive();
+        fetch_factors(kb + 2);
       }
-      if (i > 0) {
+      Operand<PROPER> o;
+      if (i < I) o.set(y[i % RING]);
+      f32x4 last_t = {1.0f, 1.0f, 1.0f, 1.0f};
+      if constexpr (!BLOCKS) { last_t = before; before = t[i % RING]; }
+      if (i + AHEAD < I) read_b(i + AHEAD, parity);
+      else if (i < I) read_b(i + AHEAD - I, other);
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j) {
+        if (i > 0) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = BLOCKS ? z[(i - 1) & 1][j][e] : z[(i - 1) & 1][j][e] * t[(i - 1) & 1][e];
-            acc[i - 1][j][e] = __builtin_fmaf(v, s[j], acc[i - 1][j][e]);
+            float v = z[j][e];
+            if constexpr (!BLOCKS) v *= last_t[e];
+            acc[i - 1][j][e] = __builtin_fmaf(v, s[P][j], acc[i - 1][j][e]);
           }
-        // (kept here: moved behind the loop's end, the sums would leave all products of the block in registers, and a branch between them and their use)
+          // (kept here: moved behind a block's end, the sums would leave all its products in registers, and a branch between them and their use)
+          asm volatile("" : "+v"(acc[i - 1][j]));
+        }
+        if (i < I) z[j] = block_product(o, x[j]);
+        if constexpr (DIRECT) {
+          // A tile is sent for a few chunks at a time, from where its place is free: all at once would keep the waves from multiplying until they are under way.
+          // (behind the last block: another split's or zeros, which nothing takes)
+          constexpr int SLOTS = EARLY * J;
+          const int slot = i >= I ? SLOTS : i >= I - AHEAD ? (i - I + AHEAD) * J + j : i < EARLY - AHEAD ? (i + AHEAD) * J + j : SLOTS;
+          if (slot < SLOTS)
 #pragma unroll
-        for (int j = 0; j < J; ++j) asm volatile("" : "+v"(acc[i - 1][j]));
+            for (int c = slot * (CA + CB) / SLOTS; c < (slot + 1) * (CA + CB) / SLOTS; ++c) {
+              if (i >= I - AHEAD) send(c, kb + 2, P);
+              else send(c, kb + 1, P ^ 1);
+            }
+        }
+        if (i == I - 1) read_a(j, other);
+      }
+      if (i > 0 && i < I) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x2, BLOCKS ? 4 : 8, 0);   // vector instructions
+          __builtin_amdgcn_sched_group_barrier(0x8, PROPER ? 4 : 1, 0);   // products
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    settle(stage ^ 1);
-    settle_factors(min(kb + 1, last - 1), stage ^ 1);
+  };
+  if (first < last) {
+    fetch_factors(first);
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int c = 0; c < CA + CB; ++c) send(c, first, 0);
+    } else {
+      fetch(first);
+      settle(0);
+    }
+    settle_factors(first, 0);
     arrive();
+    fetch_factors(first + 1);
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int c = 0; c < AHEAD * J * (CA + CB) / (EARLY * J); ++c) send(c, first + 1, 1);
+    } else {
+      fetch(first + 1);
+    }
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read_b(i, even);
+#pragma unroll
+    for (int j = 0; j < J; ++j) read_a(j, even);
+    for (int kb = first;;) {
+      block(kb, even);
+      if (++kb >= last) break;
+      block(kb, odd);
+      if (++kb >= last) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (loads into LDS that nothing takes end before the workgroup does)
   }
 
 #pragma unroll
@@ -291,7 +350,7 @@ static hipError_t launch(const Dot& d, hipStream_t stream) {
 
 template <bool BLOCKS, class OUT>
 static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
-  if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
+  if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
   if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
   return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
 }
