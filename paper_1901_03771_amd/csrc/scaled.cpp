@@ -243,6 +243,43 @@ static gr_status quantize_call(gr_ctx* ctx, gr_array x, int blocks, int transpos
   return c.launch("gr_quantize", [&] { return quantize(a, Call::type_of(dt), blocks != 0, transposed != 0, ctx->stream); });
 }
 
+// The form of a product, its tiles, and how many splits of the blocks of K there are where tiles are few.
+static int choose(Dot* d, int out) {
+  const int64_t M = d->M, N = d->N, K = d->K, KB = d->KB;
+  auto tiles_of = [&](int64_t tm, int64_t tn) {
+    d->mt = (int)((M + tm - 1) / tm);
+    d->nt = (int)((N + tn - 1) / tn);
+    return (int64_t)d->mt * d->nt;
+  };
+  // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy; a split of fewer than 32 blocks is over before it would pay.  (16 rows by 4096 x 4096: 8.3 us,
+  // tiles of 64 x 128 13; 32 rows by 14336 x 4096: 18 and 19 us; 64 rows: 28 and 19)
+  if (M <= 32) {
+    d->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles_of(32, 32), KB / 32));
+    return ((uintptr_t)d->a | (uintptr_t)d->b | (uintptr_t)(M > 1 ? d->a_s : 0) | (uintptr_t)(N > 1 ? d->b_s : 0) | (uintptr_t)(K % BLOCK ? K : 0)) % 4 == 0 ? DOT_FEW : DOT_FEW_WORDS;
+  }
+  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 27 us, by 4096 x 4088 29,
+  // by 4096 x 4095 34).
+  auto direct = [&](const uint8_t* p, int64_t rows, int64_t s) { return (uintptr_t)p % 16 == 0 && (rows == 1 || (s % 16 == 0 && s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
+  const bool straight = K % 16 == 0 && direct(d->a, M, d->a_s) && direct(d->b, N, d->b_s);
+  d->splits = 1;
+  // Tiles of 256 x 256 where there are enough for three quarters of the compute units, and a bf16 result (8192^3: 455 us, tiles of 128 x 128 600).
+  if (straight && out == GR_BF16 && tiles_of(256, 256) >= 192) return DOT_LARGE;
+  // Tiles of 128 rows of b, and 64 of a if there are no more (64 rows by 4096 x 14336: 18.8 us, 19.5 with 128).  The splits that take least by what was measured: a block of a workgroup alone on
+  // its compute unit 0.62 us, with another one beside it 1.02; the join a launch, 3.5 us, and its parts written and read.
+  const bool low = straight && M <= 64;
+  const int64_t tiles = tiles_of(low ? 64 : 128, 128);
+  double least = 0.0;
+  for (int64_t s = 1; s <= 16 && s <= std::max<int64_t>(1, KB / 4); ++s) {
+    const int64_t groups = tiles * s, rounds = (groups + 511) / 512;
+    const double each = 0.62 + 0.4 * (double)std::max<int64_t>(0, std::min<int64_t>(groups, 512) - 256) / 256;
+    const double us = (double)((KB + s - 1) / s) * each * (double)rounds + (s > 1 ? 3.5 + (double)(s * M * N) * 8e-7 : 0.0);
+    if (s > 1 && us >= least) continue;
+    least = us;
+    d->splits = (int)s;
+  }
+  return straight ? (low ? DOT_LOW : DOT_DIRECT) : DOT_STAGED;
+}
+
 static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b, gr_array b_scales, gr_array out) {
   Call c{ctx, "dot_scaled"};
   const Node *x = lookup(ctx, a), *y = lookup(ctx, b), *s = lookup(ctx, b_scales), *o = lookup(ctx, out);
@@ -281,15 +318,7 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   d.N = (int)N;
   d.K = (int)K;
   d.KB = (int)KB;
-  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes.
-  auto direct = [&](const uint8_t* p, int64_t s) { return (uintptr_t)p % 16 == 0 && s % 16 == 0 && K % 16 == 0 && (s == 0 || (s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
-  int form = direct(d.a, M > 1 ? d.a_s : 0) && (M == 1 || d.a_s > 0) && direct(d.b, N > 1 ? d.b_s : 0) && (N == 1 || d.b_s > 0) ? DOT_DIRECT : DOT_STAGED;
-  if (form == DOT_DIRECT && dt == GR_BF16 && M >= 256 && N >= 256 && ((M + 255) / 256) * ((N + 255) / 256) >= 192) form = DOT_LARGE;
-  const int64_t side = form == DOT_LARGE ? 256 : 128;
-  d.mt = (int)((M + side - 1) / side);
-  d.nt = (int)((N + side - 1) / side);
-  const int64_t tiles = (int64_t)d.mt * d.nt;
-  d.splits = form == DOT_LARGE ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, KB / 4));
+  const int form = choose(&d, dt);
   if (d.splits > 1) {
     char* ws;
     TRY(c.space(rounded((size_t)d.splits * M * N * 4), &ws));

@@ -45,16 +45,42 @@ static __device__ __forceinline__ f32x4 block_product(const Operand<true>& a, co
   return z;
 }
 
-// 16 bytes k .. k + 15 of a row of K bytes at any address; zeros behind its end.
-static __device__ __forceinline__ i32x4 bytes_at(const uint8_t* row, int k, int K) {
+// 16 bytes k .. k + 15 of a row of K bytes at any address, zeros behind its end, in two steps without a branch between loads: what is loaded ends with the row, and is moved
+// to its place once it is needed.
+static __device__ __forceinline__ i32x4 bytes_until(const uint8_t* row, int k, int K) {
   typedef int anywhere __attribute__((ext_vector_type(4), aligned(1)));
+  if (K >= 16) return *(const anywhere*)(row + min(k, K - 16));
   i32x4 v = {0, 0, 0, 0};
-  if (k + 16 <= K) {
-    v = *(const anywhere*)(row + k);
-  } else if (k < K) {
 #pragma unroll
-    for (int e = 0; e < 15; ++e) if (k + e < K) v[e / 4] |= (int)row[k + e] << (8 * (e % 4));
-  }
+  for (int e = 0; e < 15; ++e) v[e / 4] |= (e < K ? (int)row[min(e, K - 1)] : 0) << (8 * (e % 4));
+  return v;
+}
+static __device__ __forceinline__ i32x4 in_place(i32x4 v, int k, int K) {
+  const int off = K >= 16 ? k - min(k, K - 16) : k;   // bytes that are too many in front
+  uint64_t lo = (uint32_t)v[0] | (uint64_t)(uint32_t)v[1] << 32, hi = (uint32_t)v[2] | (uint64_t)(uint32_t)v[3] << 32;
+  const int bits = 8 * (off & 7);
+  if (off >= 8) { lo = hi; hi = 0; }
+  lo = bits ? lo >> bits | hi << (64 - bits) : lo;
+  hi >>= bits;
+  if (off >= 16) lo = hi = 0;
+  return i32x4{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+}
+
+// The same of rows at odd addresses: whole words, each of which holds a byte of the row, and a fifth one where the bytes stand across five.  (Vector loads at addresses that are no
+// multiple of four bytes take this card 2.7 times as long: 4 rows by 4096, 4095 places, 20 us.)
+struct Words { i32x4 v; int more; };
+static __device__ __forceinline__ Words words_until(const uint8_t* row, int k, int K) {
+  if (K < 16) return {bytes_until(row, k, K), 0};
+  typedef int anywhere __attribute__((ext_vector_type(4), aligned(4)));
+  const uint8_t* const p = row + min(k, K - 16);
+  const int off = (int)(uintptr_t)p & 3;
+  return {*(const anywhere*)(p - off), *(const int*)(p - off + (off ? 16 : 12))};
+}
+static __device__ __forceinline__ i32x4 joined(const Words& w, const uint8_t* row, int k, int K) {
+  const uint32_t off = K < 16 ? 0 : (uint32_t)(uintptr_t)(row + min(k, K - 16)) & 3;
+  i32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = (int)__builtin_amdgcn_alignbyte((uint32_t)(e < 3 ? w.v[e + 1] : w.more), (uint32_t)w.v[e], off);
   return v;
 }
 
@@ -133,8 +159,8 @@ struct Flight {
   }
 };
 
-// A tile of TM rows of a by TN rows of b, waves WM x WN.  Two stages of tiles in LDS: while one is multiplied, the next block's is under way, through
-// registers (any strides) or straight into LDS (DIRECT).
+// A tile of TM rows of a by TN rows of b, waves WM x WN.  Two stages of a block each in LDS: while one is multiplied, the other is under way, through registers (any strides) or straight
+// into LDS (DIRECT).
 template <int TM, int TN, int WM, int WN, bool DIRECT, bool BLOCKS, class OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Dot d) {
   constexpr int THREADS = WM * WN * 64, I = TN / WN / 16, J = TM / WM / 16, NB = TN / BLOCK;
@@ -162,19 +188,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     if (c < CA) fa.go(c, fa.place(kb, d.K), stage * STAGE);
     else fb.go(c - CA, fb.place(kb, d.K), stage * STAGE);
   };
+  // (a row behind the last is read as the last: its results go nowhere)
   auto fetch = [&](int kb) GR_INLINE {
 #pragma unroll
-    for (int c = 0; c < CA; ++c) {
-      const int i = c * THREADS + tid, r = i / 8;
-      staged[c] = r < rows_a ? bytes_at(a + r * d.a_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
-    }
+    for (int c = 0; c < CA; ++c) staged[c] = bytes_until(a + min((c * THREADS + tid) / 8, rows_a - 1) * d.a_s, kb * 128 + tid % 8 * 16, d.K);
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-      const int i = c * THREADS + tid, r = i / 8;
-      staged[CA + c] = r < rows_b ? bytes_at(b + r * d.b_s, kb * 128 + i % 8 * 16, d.K) : i32x4{0, 0, 0, 0};
-    }
+    for (int c = 0; c < CB; ++c) staged[CA + c] = bytes_until(b + min((c * THREADS + tid) / 8, rows_b - 1) * d.b_s, kb * 128 + tid % 8 * 16, d.K);
   };
-  auto settle = [&](int stage) GR_INLINE {
+  auto settle = [&](int kb, int stage) GR_INLINE {
+    if (kb * 128 + 128 > d.K) {
+#pragma unroll
+      for (int c = 0; c < CA + CB; ++c) staged[c] = in_place(staged[c], kb * 128 + tid % 8 * 16, d.K);
+    }
 #pragma unroll
     for (int c = 0; c < CA + CB; ++c) {
       const int i = (c < CA ? c : c - CA) * THREADS + tid, r = i / 8;
@@ -229,7 +254,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 #pragma unroll
     for (int j = 0; j < J; ++j) x[j].set(raw[j]);
     if constexpr (!DIRECT) {   // (has branches: before the first product)
-      settle(P ^ 1);
+      settle(kb + 1, P ^ 1);
       fetch(kb + 2);
     }
     // Columns 16 at a time: four sums of the step before are added, then the registers take the next product.
@@ -291,7 +316,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
       for (int c = 0; c < CA + CB; ++c) send(c, first, 0);
     } else {
       fetch(first);
-      settle(0);
+      settle(first, 0);
     }
     settle_factors(first, 0);
     arrive();
@@ -330,6 +355,123 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   }
 }
 
+// Few rows of a (16 MT at most): b is what is read, at the rate of the memory.  A workgroup has 32 rows of b, its eight waves take blocks of 128 places in turn, U of them in
+// flight at once, straight from memory to the registers that the matrix cores read; the waves' sums are added in order.
+template <bool WORDS> struct Chunk;
+template <> struct Chunk<false> {
+  i32x4 v;
+  __device__ __forceinline__ void load(const uint8_t* row, int k, int K) { v = bytes_until(row, k, K); }
+  __device__ __forceinline__ i32x4 get(const uint8_t*, int, int) const { return v; }
+};
+template <> struct Chunk<true> {
+  Words w;
+  __device__ __forceinline__ void load(const uint8_t* row, int k, int K) { w = words_until(row, k, K); }
+  __device__ __forceinline__ i32x4 get(const uint8_t* row, int k, int K) const { return joined(w, row, k, K); }
+};
+
+template <int MT, bool WORDS, bool BLOCKS, class OUT>
+__global__ __launch_bounds__(512) void gr_dot_scaled_few_kernel(const Dot d) {
+  constexpr bool PROPER = sizeof(OUT) == 4;
+  constexpr int WAVES = 8, NT = 2, U = WORDS ? 2 : 4 / MT, PITCH = 16 * NT + 4;
+  __shared__ __attribute__((aligned(16))) float part[WAVES][16 * MT][PITCH];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4;
+  const int tile = blockIdx.x % d.nt, split = blockIdx.x / d.nt, n0 = tile * 16 * NT;
+  const int first = (int)((int64_t)d.KB * split / d.splits), last = (int)((int64_t)d.KB * (split + 1) / d.splits);
+  const uint8_t *a[MT], *b[NT];
+  const float* sa[MT];
+  const float* sb[NT][BLOCKS ? 1 : 4];
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int m = min(16 * j + l, d.M - 1);
+    a[j] = d.a + m * d.a_s;
+    sa[j] = d.sa + m * d.sa_m;
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    b[i] = d.b + min(n0 + 16 * i + l, d.N - 1) * d.b_s;
+    if constexpr (BLOCKS) {
+      sb[i][0] = d.sb + min(n0 + 16 * i, d.N - 1) / BLOCK * d.sb_n;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sb[i][e] = d.sb + min(n0 + 16 * i + 4 * g + e, d.N - 1) * d.sb_n;
+    }
+  }
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int kb0 = first + wave; kb0 < last; kb0 += WAVES * U) {
+    Chunk<WORDS> x[U][MT][2], y[U][NT][2];
+    float s[U][MT], t[U][NT][BLOCKS ? 1 : 4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kb = min(kb0 + u * WAVES, last - 1), k = kb * 128 + 16 * g;   // (behind the last block: the last again, which is left out of the sums)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        y[u][i][0].load(b[i], k, d.K);
+        y[u][i][1].load(b[i], k + 64, d.K);
+#pragma unroll
+        for (int e = 0; e < (BLOCKS ? 1 : 4); ++e) t[u][i][e] = sb[i][e][kb * d.sb_k];
+      }
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        x[u][j][0].load(a[j], k, d.K);
+        x[u][j][1].load(a[j], k + 64, d.K);
+        s[u][j] = sa[j][kb * d.sa_k];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kb = min(kb0 + u * WAVES, last - 1), k = kb * 128 + 16 * g;
+      const bool there = kb0 + u * WAVES < last;
+      i32x4 v[NT + MT][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) v[i][h] = y[u][i][h].get(b[i], k + 64 * h, d.K);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) v[NT + j][h] = x[u][j][h].get(a[j], k + 64 * h, d.K);
+      }
+      if (kb * 128 + 128 > d.K) {
+#pragma unroll
+        for (int i = 0; i < NT + MT; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) v[i][h] = in_place(v[i][h], k + 64 * h, d.K);
+      }
+      Operand<PROPER> p[NT], q[MT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) p[i].set(__builtin_shufflevector(v[i][0], v[i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int j = 0; j < MT; ++j) q[j].set(__builtin_shufflevector(v[NT + j][0], v[NT + j][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const f32x4 z = block_product(p[i], q[j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float sum = __builtin_fmaf(z[e], s[u][j] * t[u][i][BLOCKS ? 0 : e], acc[i][j][e]);
+            acc[i][j][e] = there ? sum : acc[i][j][e];
+          }
+          asm volatile("" : "+v"(acc[i][j]));   // (no branch between a product and its use)
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(f32x4*)&part[wave][16 * j + l][16 * i + 4 * g] = acc[i][j];
+  __syncthreads();
+  const int m = threadIdx.x / (4 * NT), n = threadIdx.x % (4 * NT) * 4;
+  if (m >= 16 * MT || m >= d.M) return;
+  f32x4 z = *(const f32x4*)&part[0][m][n];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) z += *(const f32x4*)&part[w][m][n];
+  if (d.splits > 1) store4<float>(d.parts + ((int64_t)split * d.M + m) * d.N, n0 + n, d.N, z);
+  else store4<OUT>((OUT*)d.out + m * d.out_s, n0 + n, d.N, z);
+}
+
 // The sum of the splits, in order.
 template <class OUT>
 __global__ __launch_bounds__(256) void gr_dot_scaled_join_kernel(const Dot d) {
@@ -338,7 +480,13 @@ __global__ __launch_bounds__(256) void gr_dot_scaled_join_kernel(const Dot d) {
   const int64_t m = i / n4;
   const int n = (int)(i - m * n4) * 4;
   f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < d.splits; ++s) z += get<float>(d.parts + (s * (int64_t)d.M + m) * d.N, n, d.N);
+  for (int s0 = 0; s0 < d.splits; s0 += 8) {   // (eight in flight)
+    f32x4 v[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) v[s] = s0 + s < d.splits ? get<float>(d.parts + ((s0 + s) * (int64_t)d.M + m) * d.N, n, d.N) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < 8; ++s) z += v[s];
+  }
   store4<OUT>((OUT*)d.out + m * d.out_s, n, d.N, z);
 }
 
@@ -348,9 +496,18 @@ static hipError_t launch(const Dot& d, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int MT, bool WORDS, bool BLOCKS, class OUT>
+static hipError_t launch_few(const Dot& d, hipStream_t stream) {
+  gr_dot_scaled_few_kernel<MT, WORDS, BLOCKS, OUT><<<dim3((unsigned)(d.nt * d.splits)), dim3(512), 0, stream>>>(d);
+  return hipGetLastError();
+}
+
 template <bool BLOCKS, class OUT>
 static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
+  if (form == DOT_FEW) return d.M <= 16 ? launch_few<1, false, BLOCKS, OUT>(d, stream) : launch_few<2, false, BLOCKS, OUT>(d, stream);
+  if (form == DOT_FEW_WORDS) return d.M <= 16 ? launch_few<1, true, BLOCKS, OUT>(d, stream) : launch_few<2, true, BLOCKS, OUT>(d, stream);
   if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
+  if (form == DOT_LOW) return launch<64, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
   if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
   return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
 }
