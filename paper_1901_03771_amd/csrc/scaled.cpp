@@ -264,20 +264,27 @@ static int choose(Dot* d, int out) {
   d->splits = 1;
   // Tiles of 256 x 256 where there are enough for three quarters of the compute units, and a bf16 result (8192^3: 455 us, tiles of 128 x 128 600).
   if (straight && out == GR_BF16 && tiles_of(256, 256) >= 192) return DOT_LARGE;
-  // Tiles of 128 rows of b, and 64 of a if there are no more (64 rows by 4096 x 14336: 18.8 us, 19.5 with 128).  The splits that take least by what was measured: a block of a workgroup alone on
-  // its compute unit 0.62 us, with another one beside it 1.02; the join a launch, 3.5 us, and its parts written and read.
-  const bool low = straight && M <= 64;
-  const int64_t tiles = tiles_of(low ? 64 : 128, 128);
+  // Tiles of 128 rows of b and 64 or 128 of a, and splits of K, whichever takes least by what was measured (us): a start, the blocks of a workgroup alone on its compute unit or with another one
+  // beside it, through registers twice as long, in float32 1.4 times; and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 23 with 256 tiles of 64 rows, 26 with 128
+  // of 128 rows, 23 with those in two splits; 384 x 4096 x 16384: 54 with 64 rows in two splits, 42 with 128 rows in four; 64 x 4096 x 14336: 70, 40, 25, 19, 19 with 1, 2, 4, 8, 12.)
+  const double slow = (straight ? 1.0 : 2.0) * (out == GR_F32 ? 1.4 : 1.0);
   double least = 0.0;
-  for (int64_t s = 1; s <= 16 && s <= std::max<int64_t>(1, KB / 4); ++s) {
-    const int64_t groups = tiles * s, rounds = (groups + 511) / 512;
-    const double each = 0.62 + 0.4 * (double)std::max<int64_t>(0, std::min<int64_t>(groups, 512) - 256) / 256;
-    const double us = (double)((KB + s - 1) / s) * each * (double)rounds + (s > 1 ? 3.5 + (double)(s * M * N) * 8e-7 : 0.0);
-    if (s > 1 && us >= least) continue;
-    least = us;
-    d->splits = (int)s;
+  int64_t rows = 0;
+  for (int64_t high : {64, 128}) {
+    if (high == 128 && (M <= 64 || (!straight && out == GR_F32))) break;   // (rows at odd addresses and float32 together leave registers for 64 only)
+    const int64_t tiles = tiles_of(high, 128);
+    for (int64_t s = 1; s <= 16 && s <= std::max<int64_t>(1, KB / 4); ++s) {
+      const int64_t groups = tiles * s;
+      const double beside = groups > 256 ? 0.4 + 0.6 * (double)(std::min<int64_t>(groups, 512) - 256) / 256 : 0.0, block = high == 64 ? 0.58 + 0.29 * beside : 0.65 + 0.54 * beside;
+      const double us = (high == 64 ? 3.0 : 5.0) + (double)((KB + s - 1) / s) * (double)((groups + 511) / 512) * block * slow + (s > 1 ? 5.5 + (double)(s * M * N) * 8e-7 : 0.0);
+      if (rows && us >= least) continue;
+      least = us;
+      rows = high;
+      d->splits = (int)s;
+    }
   }
-  return straight ? (low ? DOT_LOW : DOT_DIRECT) : DOT_STAGED;
+  tiles_of(rows, 128);
+  return straight ? (rows == 64 ? DOT_LOW : DOT_DIRECT) : rows == 64 ? DOT_STAGED_LOW : DOT_STAGED;
 }
 
 static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b, gr_array b_scales, gr_array out) {

@@ -70,7 +70,7 @@ struct Dot {
   int splits = 1;                                 // of the blocks of K
   int mt = 0, nt = 0;                             // tiles
 };
-enum { DOT_STAGED, DOT_DIRECT, DOT_LOW, DOT_LARGE, DOT_FEW, DOT_FEW_WORDS };
+enum { DOT_STAGED, DOT_DIRECT, DOT_LOW, DOT_STAGED_LOW, DOT_LARGE, DOT_FEW, DOT_FEW_WORDS };
 hipError_t dot(const Dot& d, int form, bool blocks, int out_type, hipStream_t stream);
 hipError_t dot_join(const Dot& d, int out_type, hipStream_t stream);
 

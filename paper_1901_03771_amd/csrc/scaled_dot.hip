@@ -509,7 +509,9 @@ static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
   if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
   if (form == DOT_LOW) return launch<64, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
   if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
-  return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
+  if (form == DOT_STAGED_LOW) return launch<64, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
+  if constexpr (sizeof(OUT) == 2) if (form == DOT_STAGED) return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
+  return hipErrorInvalidValue;
 }
 
 hipError_t dot(const Dot& d, int form, bool blocks, int out_type, hipStream_t stream) {
