@@ -14,7 +14,7 @@ static __device__ __forceinline__ T* row_at(const Rows& r, const Norm& a, int64_
   return (T*)r.p + h * r.s0 + j * r.s1 + k * r.s2;
 }
 
-// offset + weight of the thread's values; 1 where there is no weight
+// The weights of the thread's values, to which the offset is added where they are used: so the first row's loads need not wait for them.  1 where there are none.
 template <int TPR, int V, int N>
 static __device__ __forceinline__ void weights(const Norm& a, int t, float (&w)[V][N]) {
 #pragma unroll
@@ -25,17 +25,19 @@ static __device__ __forceinline__ void weights(const Norm& a, int t, float (&w)[
       for (int q = 0; q < N; q += 4) {
         const f32x4 v = get<float>(a.weight, d + q, a.D);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[j][q + e] = a.offset + v[e];
+        for (int e = 0; e < 4; ++e) w[j][q + e] = v[e];
       }
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const int64_t at = (d + e) * a.weight_s;
-        w[j][e] = d + e >= a.D ? 0.0f : a.weight ? a.offset + a.weight[at] : a.weight16 ? a.offset + (float)((const __bf16*)a.weight16)[at] : 1.0f;
+        w[j][e] = d + e >= a.D ? 0.0f : a.weight ? a.weight[at] : a.weight16 ? (float)((const __bf16*)a.weight16)[at] : 1.0f;
       }
     }
   }
 }
+// (a number that the compiler takes to be new in every turn of the loop)
+static __device__ __forceinline__ float anew(float x) { asm volatile("" : "+s"(x)); return x; }
 
 // The sums of a row over the TPR threads that share it, in all of them.  One barrier a row: `turn` alternates between two places in LDS.
 template <int TPR, int COUNT>
@@ -58,7 +60,7 @@ static __device__ __forceinline__ void row_sums(float (&s)[COUNT], int turn) {
   }
 }
 
-template <class T, bool EIGHT, int TPR, int V>
+template <class T, bool EIGHT, bool PAST, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(const Norm a) {
   constexpr int N = Vec<T>::N, THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -72,12 +74,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
     typename Vec<T>::type x[V];
     const T* const xr = row_at<const T>(a.x, a, row);
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = get<T>(xr, (j * TPR + t) * N, D);
+    for (int j = 0; j < V; ++j) x[j] = get<T, PAST>(xr, (j * TPR + t) * N, D);
     if (a.residual.p) {
       const T* const rr = row_at<const T>(a.residual, a, row);
       typename Vec<T>::type more[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) more[j] = get<T>(rr, (j * TPR + t) * N, D);
+      for (int j = 0; j < V; ++j) more[j] = get<T, PAST>(rr, (j * TPR + t) * N, D);
       // (rounded to the type before the norm: that is the stream as the next layer, and the gradient, find it)
 #pragma unroll
       for (int j = 0; j < V; ++j)
@@ -86,9 +88,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
       if (a.total.p) {
         T* const to = row_at<T>(a.total, a, row);
 #pragma unroll
-        for (int j = 0; j < V; ++j) put<T>(to, (j * TPR + t) * N, D, x[j]);
+        for (int j = 0; j < V; ++j) put<T, PAST>(to, (j * TPR + t) * N, D, x[j]);
       }
     }
+    const float offset = anew(a.offset);
     float s[1] = {0.0f};
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
         uint32_t top = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          y[e] = (float)x[j][e] * r * w[j][e];
+          y[e] = (float)x[j][e] * r * (offset + w[j][e]);
           const uint32_t b = d + e < D ? size_bits(y[e]) : 0;   // (r may be infinite or NaN: not behind the row's end)
           top = b > top ? b : top;
         }
@@ -122,7 +125,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
           anywhere v;
 #pragma unroll
           for (int e = 0; e < N / 4; ++e) v[e] = q[e];
-          *(anywhere*)(to + d) = v;
+          if constexpr (PAST) __builtin_nontemporal_store(v, (anywhere*)(to + d));
+          else *(anywhere*)(to + d) = v;
         } else {
 #pragma unroll
           for (int e = 0; e < N; ++e) if (d + e < D) to[d + e] = (uint8_t)(q[e / 4] >> (8 * (e % 4)));
@@ -135,14 +139,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
       for (int j = 0; j < V; ++j) {
         typename Vec<T>::type y;
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = (T)((float)x[j][e] * r * w[j][e]);
-        put<T>(to, (j * TPR + t) * N, D, y);
+        for (int e = 0; e < N; ++e) y[e] = (T)((float)x[j][e] * r * (offset + w[j][e]));
+        put<T, PAST>(to, (j * TPR + t) * N, D, y);
       }
     }
   }
 }
 
-template <class T, int TPR, int V>
+template <class T, bool PAST, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_grad_kernel(const Norm a) {
   constexpr int N = Vec<T>::N, THREADS = TPR < 256 ? 256 : TPR, PER = THREADS / TPR;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -162,14 +166,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_grad_kernel
     const T* const yr = row_at<const T>(a.dout, a, row);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      x[j] = get<T>(xr, (j * TPR + t) * N, D);
-      y[j] = get<T>(yr, (j * TPR + t) * N, D);
+      x[j] = get<T, PAST>(xr, (j * TPR + t) * N, D);
+      y[j] = get<T, PAST>(yr, (j * TPR + t) * N, D);
     }
     if (a.residual.p) {
       const T* const rr = row_at<const T>(a.residual, a, row);
 #pragma unroll
-      for (int j = 0; j < V; ++j) more[j] = get<T>(rr, (j * TPR + t) * N, D);
+      for (int j = 0; j < V; ++j) more[j] = get<T, PAST>(rr, (j * TPR + t) * N, D);
     }
+    const float offset = anew(a.offset);
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -177,7 +182,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_grad_kernel
       for (int e = 0; e < N; ++e) {
         const float v = (float)x[j][e];
         s[0] = __builtin_fmaf(v, v, s[0]);
-        s[1] = __builtin_fmaf((float)y[j][e] * w[j][e], v, s[1]);
+        s[1] = __builtin_fmaf((float)y[j][e] * (offset + w[j][e]), v, s[1]);
       }
     row_sums<TPR, 2>(s, turn);
     turn ^= 1;
@@ -189,12 +194,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_grad_kernel
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float v = (float)x[j][e], g = (float)y[j][e];
-        float z = r * __builtin_fmaf(-pull, v, g * w[j][e]);
+        float z = r * __builtin_fmaf(-pull, v, g * (offset + w[j][e]));
         if (a.residual.p) z += (float)more[j][e];
         dx[e] = (T)z;
         if (mine) dw[j][e] = __builtin_fmaf(g, v * r, dw[j][e]);
       }
-      put<T>(to, (j * TPR + t) * N, D, dx);
+      put<T, PAST>(to, (j * TPR + t) * N, D, dx);
     }
   }
   if (!a.parts) return;
@@ -220,13 +225,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_grad_kernel
   }
 }
 
-// dweight: the sums of all workgroups, in order; 32 columns a workgroup, eight threads for each
-__global__ __launch_bounds__(256) void gr_rms_norm_sum_kernel(const Norm a) {
-  __shared__ float side[8][32];
+// dweight: the sums of all workgroups, in order; 32 columns a workgroup, 32 threads for each.
+__global__ __launch_bounds__(1024) void gr_rms_norm_sum_kernel(const Norm a) {
+  __shared__ float side[32][32];
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5, d = blockIdx.x * 32 + c;
+  const int each = (a.groups + 31) / 32, to = min((g + 1) * each, a.groups);
   float z = 0.0f;
   if (d < a.D) {
-    const int each = (a.groups + 7) / 8, to = min((g + 1) * each, a.groups);
 #pragma unroll 8
     for (int p = g * each; p < to; ++p) z += a.parts[(int64_t)p * a.D + d];
   }
@@ -234,44 +239,59 @@ __global__ __launch_bounds__(256) void gr_rms_norm_sum_kernel(const Norm a) {
   __syncthreads();
   if (g == 0 && d < a.D) {
 #pragma unroll
-    for (int p = 1; p < 8; ++p) z += side[p][c];
+    for (int p = 1; p < 32; ++p) z += side[p][c];
     a.dweight[d * a.dweight_s] = z;
   }
 }
 
+// Tensors of 32 MiB and more go past the caches, which they have left by the time that anything reads them (16384 rows of 8192 bf16 values with a residual, to 8 bits: 177 us, 165 so; of 1024
+// values, to bf16: 27 and 25; 65536 rows of 128 values, 16 MiB: 7.6 and 8.1).
+static bool goes_past(const Norm& a, size_t size) { return a.rows * a.D * (int64_t)size >= (int64_t)32 << 20; }
+
 template <class T, bool EIGHT>
 static hipError_t norm_of(const Norm& a, Shape s, unsigned grid, hipStream_t stream) {
-#define CASE(THREADS, VECTORS) \
-  if (s.threads == THREADS && s.vectors == VECTORS) { gr_rms_norm_kernel<T, EIGHT, THREADS, VECTORS><<<dim3(grid), dim3(THREADS < 256 ? 256 : THREADS), 0, stream>>>(a); return hipGetLastError(); }
-  CASE(BLOCK / Vec<T>::N, 1) CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 2) CASE(256, 4) CASE(512, 4)
-  if constexpr (sizeof(T) == 4) { CASE(512, 8) CASE(1024, 8) }
-  else { CASE(1024, 4) }
+  const bool past = goes_past(a, sizeof(T));
+#define CASE(THREADS, VECTORS)                                                                                                               \
+  if (s.threads == THREADS && s.vectors == VECTORS) {                                                                                         \
+    constexpr int GROUP = THREADS < 256 ? 256 : THREADS;                                                                                      \
+    if (past && THREADS >= 64) gr_rms_norm_kernel<T, EIGHT, THREADS >= 64, THREADS, VECTORS><<<dim3(grid), dim3(GROUP), 0, stream>>>(a);      \
+    else gr_rms_norm_kernel<T, EIGHT, false, THREADS, VECTORS><<<dim3(grid), dim3(GROUP), 0, stream>>>(a);                                    \
+    return hipGetLastError();                                                                                                                 \
+  }
+  CASE(BLOCK / Vec<T>::N, 1) CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 2) CASE(512, 2) CASE(1024, 2) CASE(1024, 4)
+  if constexpr (sizeof(T) == 4) { CASE(1024, 8) }
 #undef CASE
   return hipErrorInvalidValue;
 }
 template <class T>
 static hipError_t grad_of(const Norm& a, Shape s, unsigned grid, hipStream_t stream) {
-#define CASE(THREADS, VECTORS) \
-  if (s.threads == THREADS && s.vectors == VECTORS) { gr_rms_norm_grad_kernel<T, THREADS, VECTORS><<<dim3(grid), dim3(THREADS < 256 ? 256 : THREADS), 0, stream>>>(a); return hipGetLastError(); }
-  CASE(BLOCK / Vec<T>::N, 1) CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 2) CASE(256, 4) CASE(512, 4)
-  if constexpr (sizeof(T) == 4) { CASE(512, 8) CASE(1024, 8) }
-  else { CASE(1024, 4) }
+  const bool past = goes_past(a, sizeof(T));
+#define CASE(THREADS, VECTORS)                                                                                                          \
+  if (s.threads == THREADS && s.vectors == VECTORS) {                                                                                    \
+    constexpr int GROUP = THREADS < 256 ? 256 : THREADS;                                                                                 \
+    if (past && THREADS >= 64) gr_rms_norm_grad_kernel<T, THREADS >= 64, THREADS, VECTORS><<<dim3(grid), dim3(GROUP), 0, stream>>>(a);   \
+    else gr_rms_norm_grad_kernel<T, false, THREADS, VECTORS><<<dim3(grid), dim3(GROUP), 0, stream>>>(a);                                 \
+    return hipGetLastError();                                                                                                            \
+  }
+  CASE(BLOCK / Vec<T>::N, 1) CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 2) CASE(256, 4) CASE(1024, 2) CASE(1024, 4)
+  if constexpr (sizeof(T) == 4) { CASE(1024, 8) }
 #undef CASE
   return hipErrorInvalidValue;
 }
 
-Shape norm_shape(int type, int D, int64_t rows) {
+// Short rows: as few threads as hold them, so that no barrier stands between a row's loads and its use (16384 rows of 2048 bf16 values: 45.6 us on 64 threads, 48 on 256).  Longer ones: few
+// registers a thread in the norm (8192 values: 512 threads 165 us, 256 with twice as many vectors 170); in the gradient, whose every thread keeps its part of dweight, as many vectors as 256
+// registers hold (8192 bf16 values, 4096 rows: 256 threads 55 us, 512 57; 5003 float32 values, 777 rows: 1024 threads 17, 512 22).
+Shape norm_shape(int type, int D, bool gradient) {
   const int n = type == BF16 ? 8 : 4, vectors = (D + n - 1) / n, narrow = BLOCK / n;
   if (vectors <= narrow) return {narrow, 1};
-  // (64 threads to 4 vectors each where rows are many: no barrier)
   if (vectors <= 64) return {64, 1};
   if (vectors <= 128) return {64, 2};
   if (vectors <= 256) return {64, 4};
   if (vectors <= 512) return {256, 2};
-  if (vectors <= 1024) return {256, 4};
-  if (vectors <= 2048) return {512, 4};
-  if (type == BF16) return {1024, 4};
-  return vectors <= 4096 ? Shape{512, 8} : Shape{1024, 8};
+  if (vectors <= 1024) return gradient ? Shape{256, 4} : Shape{512, 2};
+  if (vectors <= 2048) return {1024, 2};
+  return vectors <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
 }
 
 hipError_t norm(const Norm& a, int type, bool eight, Shape s, unsigned grid, hipStream_t stream) {
@@ -282,7 +302,7 @@ hipError_t norm_grad(const Norm& a, int type, Shape s, unsigned grid, hipStream_
   return type == BF16 ? grad_of<__bf16>(a, s, grid, stream) : grad_of<float>(a, s, grid, stream);
 }
 hipError_t norm_sum(const Norm& a, hipStream_t stream) {
-  gr_rms_norm_sum_kernel<<<dim3((a.D + 31) / 32), dim3(256), 0, stream>>>(a);
+  gr_rms_norm_sum_kernel<<<dim3((a.D + 31) / 32), dim3(1024), 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -41,7 +41,7 @@ struct Norm {
 // The threads that share a row, and the vectors of 16 bytes that each of them holds of it.
 struct Shape { int threads, vectors; };
 constexpr int MOST_VALUES = 32768;                // of a row
-Shape norm_shape(int type, int D, int64_t rows);
+Shape norm_shape(int type, int D, bool gradient);
 hipError_t norm(const Norm& a, int type, bool eight, Shape s, unsigned grid, hipStream_t stream);
 hipError_t norm_grad(const Norm& a, int type, Shape s, unsigned grid, hipStream_t stream);
 hipError_t norm_sum(const Norm& a, hipStream_t stream);

@@ -29,24 +29,26 @@ template <> struct Vec<__bf16> {
   typedef __bf16 anywhere __attribute__((ext_vector_type(8), aligned(2)));
 };
 
-// Values d .. d + N - 1 of a row of D; zeros behind its end.
-template <class T>
+// Values d .. d + N - 1 of a row of D; zeros behind its end.  PAST: leaves the caches alone.
+template <class T, bool PAST = false>
 static __device__ __forceinline__ typename Vec<T>::type get(const T* row, int d, int D) {
   constexpr int N = Vec<T>::N;
   typename Vec<T>::type v = (T)0.0f;
   if (d + N <= D) {
-    v = *(const typename Vec<T>::anywhere*)(row + d);
+    if constexpr (PAST) v = __builtin_nontemporal_load((const typename Vec<T>::anywhere*)(row + d));
+    else v = *(const typename Vec<T>::anywhere*)(row + d);
   } else if (d < D) {
 #pragma unroll
     for (int e = 0; e < N - 1; ++e) if (d + e < D) v[e] = row[d + e];
   }
   return v;
 }
-template <class T>
+template <class T, bool PAST = false>
 static __device__ __forceinline__ void put(T* row, int d, int D, typename Vec<T>::type v) {
   constexpr int N = Vec<T>::N;
   if (d + N <= D) {
-    *(typename Vec<T>::anywhere*)(row + d) = v;
+    if constexpr (PAST) __builtin_nontemporal_store((typename Vec<T>::anywhere)v, (typename Vec<T>::anywhere*)(row + d));
+    else *(typename Vec<T>::anywhere*)(row + d) = v;
   } else if (d < D) {
 #pragma unroll
     for (int e = 0; e < N - 1; ++e) if (d + e < D) row[d + e] = v[e];
