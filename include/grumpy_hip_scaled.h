@@ -13,8 +13,8 @@
  *     are leaves and views of leaves; no call but these computes with them (GR_ERR_DTYPE).
  *   - Scales (f32, any strides) belong to 128 neighbours along the last axis, the last ones of a row perhaps to fewer: of one row ("rows",
  *     shape (.., ceil(K / 128))), or of 128 rows together ("blocks", shape (ceil(M / 128), ceil(K / 128))).  A value stands for
- *     itself times its scale.  The scale is max|x| / 448, or 2^-126 where that is smaller; values are rounded to the nearest e4m3, ties to even,
- *     after a division by it that is right to 2^-22.  Where one of the values of a scale is infinite or NaN, the scale and all its values are NaN.
+ *     itself times its scale.  The scale is max|x| / 448, or 2^-126 where that is smaller; values are divided by it in f32 (right to a last place) and rounded to the
+ *     nearest e4m3, ties to even.  Where one of the values of a scale is infinite or NaN, the scale and all its values are NaN.
  *   - The values of a row (the last axis) of every tensor are neighbours, or GR_ERR_UNSUPPORTED; rows may lie anywhere.  The elements of a result do
  *     not overlap (GR_ERR_UNSUPPORTED), nor do two results or a result and an operand (GR_ERR_ALIAS), except where a call says so.
  *   - Temporary memory and captured graphs: as in grumpy_hip_attention.h, with whose calls these share it.

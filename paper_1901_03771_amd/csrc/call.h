@@ -55,17 +55,18 @@ struct Call {
     return v;
   }
 
-  // Do two views of rank 3 or 4 share no element?  Certain where their extents do not meet, and where they are parts of one packed array: the
-  // same steps between batches and rows, and within a row two stretches that do not meet.
+  // Do two views share no element?  Certain where their extents do not meet, and where they are parts of one packed array: the
+  // same steps between batches and rows (the first two axes, of two axes the first), and within a row two stretches that do not meet.
   bool apart(gr_array a, gr_array b) const {
     const StoredView x = view(a), y = view(b);
     if (!(x.lo < y.hi && y.lo < x.hi)) return true;
     const Node *m = lookup(ctx, a), *n = lookup(ctx, b);
-    if (m->ndim != 4 || n->ndim != 4 || m->dtype != n->dtype) return false;
+    if (m->ndim != n->ndim || m->ndim < 2 || m->ndim > 4 || m->dtype != n->dtype) return false;
+    const int outer = m->ndim == 2 ? 1 : 2;
     const int64_t size = (int64_t)itemsize(m->dtype);
     int64_t least = INT64_MAX;
-    int64_t steps[2], counts[2];
-    for (int d = 0; d < 2; ++d) {
+    int64_t steps[2] = {0, 0}, counts[2] = {1, 1};
+    for (int d = 0; d < outer; ++d) {
       if (m->shape[d] != n->shape[d]) return false;
       counts[d] = m->shape[d];
       steps[d] = 0;
@@ -80,7 +81,7 @@ struct Call {
     }
     auto reach = [&](const Node* t, const StoredView& v, int64_t* lo, int64_t* hi) {
       *lo = *hi = (v.data - std::min(x.data, y.data)) / size;
-      for (int d = 2; d < 4; ++d) (v.strides[d] < 0 ? *lo : *hi) += v.strides[d] * (t->shape[d] - 1);
+      for (int d = outer; d < t->ndim; ++d) (v.strides[d] < 0 ? *lo : *hi) += v.strides[d] * (t->shape[d] - 1);
     };
     int64_t alo, ahi, blo, bhi;
     reach(m, x, &alo, &ahi);

@@ -119,7 +119,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
         const bool some = top < 0x7f800000u;
         uint32_t q[N / 4];
 #pragma unroll
-        for (int e = 0; e < N; e += 4) q[e / 4] = some ? eight(y[e], y[e + 1], y[e + 2], y[e + 3], inverse) : NO_NUMBERS;
+        for (int e = 0; e < N; e += 4) q[e / 4] = some ? eight(y[e], y[e + 1], y[e + 2], y[e + 3], scale, inverse) : NO_NUMBERS;
         if (d + N <= D) {
           typedef uint32_t anywhere __attribute__((ext_vector_type(N / 4), aligned(1)));
           anywhere v;

@@ -18,6 +18,22 @@ ROW = (0.5 * (32 + 6 + 15) + 6) * 2.0 ** -24
 
 
 # ---------------------------------------------------------------- without a GPU --
+def test_parts_of_packed_rows_are_told_from_overlapping_ones(dry):  # noqa: F811
+    s = Specs(dry)
+    base, w = s.at, s((200,))
+    s.at += 1 << 20
+    part = lambda off, rows=6, step=700, cols=200: dry.from_device(base + 4 * off, gr.GR_F32, (rows, cols), (step, 1))  # noqa: E731
+    gr.rms_norm(part(0), w, part(200), out=part(400), total=part(200))
+    gr.rms_norm(part(0), w, out=part(500))
+    for off in (1, 199, 501, 700):                                          # into the columns, around the end of a row, a row further
+        refused("GR_ERR_ALIAS", gr.rms_norm, part(0), w, out=part(off))
+    refused("GR_ERR_ALIAS", gr.rms_norm, part(0), w, out=part(300, step=800))
+    wide = lambda off: dry.from_device(base + 4 * off, gr.GR_F32, (2, 6, 200), (4200, 700, 1))  # noqa: E731
+    gr.rms_norm(wide(0), w, out=wide(300))
+    refused("GR_ERR_ALIAS", gr.rms_norm, wide(0), w, out=wide(600))
+    refused("GR_ERR_ALIAS", gr.rms_norm, wide(0), w, out=wide(4200))
+
+
 @pytest.mark.parametrize("dtype", [gr.GR_F32, gr.GR_BF16])
 def test_calls_run_dry_and_count_their_launches(dry, dtype):  # noqa: F811
     s = Specs(dry)
@@ -517,3 +533,221 @@ def test_product_with_what_is_no_number(ctx):
     assert got[bad].isnan().all() and torch.equal(got[~bad], want[~bad])
     zero = gr.dot_scaled(*(ctx.array(t.cuda()) for t in (a[:, :0], sa[:, :0], b[:, :0], sb[:, :0])), dtype=gr.GR_F32).torch()
     assert bool((zero == 0).all()) and zero.shape == (m, n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(4100, 3100, 272), (8200, 1700, 144), (2050, 6200, 640), (3001, 4500, 261), (12289, 1300, 128)])
+@pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
+def test_large_products_of_whole_numbers(ctx, blocks, m, n, k):
+    """Tiles of 256 x 256, with rows of whole vectors and without, last tiles and last blocks of K that are not full."""
+    a, sa = whole(m + k, m, k, 1)
+    b, sb = whole(n + k, n, k, 128 if blocks else 1)
+    x, y = a.float() * plain.spread(sa, a.shape).float(), b.float() * plain.spread(sb, b.shape).float()
+    want = (x @ y.T)                                # (exact in float32 too: below 2^24 sixteenths)
+    for out in (BF16, F32):
+        to = Guarded((m, n), out)
+        gr.dot_scaled(*(ctx.array(t.cuda()) for t in (a, sa, b, sb)), out=ctx.array(to.t))
+        got = to.t.cpu()
+        assert torch.equal(got, want.to(out)), int((got != want.to(out)).sum())
+        assert to.untouched()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,D", [(BF16, 4200, 4100), (F32, 2100, 4100), (F32, 140000, 70), (BF16, 70000, 300), (BF16, 2100, 8192), (F32, 600, 16000), (BF16, 1100, 16400)])
+def test_large_norms(ctx, dtype, rows, D):
+    """Tensors that go past the caches, and more rows than workgroups."""
+    n = rows + D
+    x, res, more = (normal(n + i, rows, D, dtype=dtype) for i in range(3))
+    w = normal(n + 5, D, by=0.3)
+    y, total = plain.norm(x, res, w, 1e-6, 1.0)
+    gx, gres, gw = (ctx.array(t.cuda()) for t in (x, res, w))
+    out, sums, _ = gr.rms_norm(gx, gw, gres, offset=1.0)
+    assert torch.equal(sums.torch().cpu(), total)
+    assert ((out.torch().cpu().double() - y).abs() <= (ROW + HALF[dtype]) * y.abs()).all()
+    q, _, s = gr.rms_norm(gx, gw, gres, offset=1.0, eight=True, total=False)
+    s = s.torch().cpu()
+    v = y / plain.spread(s, y.shape)
+    assert ((q.torch().float().cpu() - v).abs() <= plain.half_step(v.clamp(-448, 448)) + (ROW + 2.0 ** -22) * v.abs() + (v.abs() - 448).clamp(min=0)).all()
+    dx, dw, size, terms = plain.norm_grad(more, total, w, x, 1e-6, 1.0)
+    gdx, gdw = gr.rms_norm_grad(ctx.array(more.cuda()), sums, gw, dtotal=gx, offset=1.0)
+    assert ((gdx.torch().cpu().double() - dx).abs() <= 4 * ROW * size + HALF[dtype] * dx.abs()).all()
+    # (rows of a workgroup one after another, then of the workgroups: fewer than all rows)
+    assert ((gdw.torch().cpu().double() - dw).abs() <= (ROW + (rows + 4) * 2.0 ** -24) * terms).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("blocks,transposed", [(False, False), (True, False), (False, True), (True, True)], ids=["rows", "blocks", "columns", "blocks_transposed"])
+@pytest.mark.parametrize("dtype,m,k", [(BF16, 8300, 4100), (F32, 4099, 4100)])
+def test_large_quantize(ctx, dtype, m, k, blocks, transposed):
+    x = normal(m, m, k, dtype=dtype)
+    q, s = gr.quantize(ctx.array(x.cuda()), blocks=blocks, transposed=transposed)
+    exact = (x.T if transposed else x).contiguous()
+    high = 128 if blocks else 1
+    wide = torch.nn.functional.pad(exact.float(), (0, -exact.shape[1] % 128, 0, -exact.shape[0] % high)).abs()
+    top = wide.view(wide.shape[0] // high, high, wide.shape[1] // 128, 128).amax((1, 3))
+    assert torch.equal(s.torch().cpu(), top / 448.0)
+    v = exact.double() / plain.spread(s.torch().cpu(), exact.shape)
+    assert ((q.torch().float().cpu() - v).abs() <= plain.half_step(v.clamp(-448, 448)) + 2.0 ** -22 * v.abs() + (v.abs() - 448).clamp(min=0)).all()
+
+
+@pytest.mark.gpu
+def test_rows_far_apart(ctx):
+    """Offsets beyond 2^31 and 2^32 bytes and elements, in operands and results."""
+    step = (1 << 30) + 48
+    flat = torch.empty(5 * step, dtype=torch.bfloat16, device="cuda")        # 10 GiB
+    x = torch.as_strided(flat, (5, 520), (step, 1))
+    vals = normal(4, 5, 520, dtype=BF16)
+    x.copy_(vals.cuda())
+    w = normal(5, 520)
+    y, _ = plain.norm(vals, None, w, 1e-6, 0.0)
+    out = torch.as_strided(flat, (5, 520), (step, 1), 4096)
+    gr.rms_norm(ctx.array(x), ctx.array(w.cuda()), out=ctx.array(out))
+    assert ((out.cpu().double() - y).abs() <= (ROW + HALF[BF16]) * y.abs()).all()
+    dx, dw, size, terms = plain.norm_grad(vals, vals, w, None, 1e-6, 0.0)
+    _, gw = gr.rms_norm_grad(ctx.array(x), ctx.array(x), ctx.array(w.cuda()), dx=ctx.array(out))
+    assert ((out.cpu().double() - dx).abs() <= 4 * ROW * size + HALF[BF16] * dx.abs()).all()
+    assert ((gw.torch().cpu().double() - dw).abs() <= (ROW + 9 * 2.0 ** -24) * terms).all()
+    bytes_ = torch.empty(10 * step, dtype=torch.uint8, device="cuda").view(E4M3)
+    q = torch.as_strided(bytes_, (5, 520), (2 * step, 1), 16384)
+    for blocks in (False, True):
+        q2, s2 = gr.quantize(ctx.array(x), blocks=blocks, out=ctx.array(q))
+        want, ws = gr.quantize(ctx.array(vals.cuda()), blocks=blocks)
+        assert torch.equal(q2.torch().float(), want.torch().float()) and torch.equal(s2.torch(), ws.torch())
+    # a product of rows 2 GiB apart: few rows, and 40 of them 256 MiB apart, aligned and not
+    b, sb = whole(1, 300, 520, 128)
+    for rows, apart, off in ((5, 2 * step, 16384), (40, 1 << 28, 0), (40, (1 << 28) + 3, 1), (3, 2 * step + 5, 7)):
+        a, sa = whole(rows, rows, 520, 1)
+        far = torch.as_strided(bytes_, (rows, 520), (apart, 1), off)
+        far.copy_(a.cuda())
+        got = gr.dot_scaled(ctx.array(far), ctx.array(sa.cuda()), ctx.array(b.cuda()), ctx.array(sb.cuda()), dtype=gr.GR_F32).torch().cpu()
+        assert torch.equal(got.double(), plain.product(a, sa, b, sb)[0])
+        wide = torch.as_strided(flat.view(torch.float32), (rows, 300), (apart // 4 // 4 * 4, 1), 1 << 20)
+        gr.dot_scaled(ctx.array(a.cuda()), ctx.array(sa.cuda()), ctx.array(b.cuda()), ctx.array(sb.cuda()), out=ctx.array(wide))
+        assert torch.equal(wide.cpu(), got)
+        back = gr.dot_scaled(ctx.array(b.cuda()), ctx.array(spread_rows(sb, 300).cuda()), ctx.array(far), ctx.array(sa.cuda()), dtype=gr.GR_F32).torch().cpu()
+        assert torch.equal(back, got.T)
+
+
+def spread_rows(blocks, rows):
+    return blocks.repeat_interleave(128, 0)[:rows].contiguous()
+
+
+@pytest.mark.gpu
+def test_lazy_operands_and_pending_readers(ctx):
+    """Operands that are expressions or views of expressions are evaluated first; what was recorded on a result's memory keeps what it was recorded with."""
+    x, w = normal(1, 40, 256), normal(2, 256)
+    gx, gw = ctx.array(x.cuda()), ctx.array(w.cuda())
+    y, _ = plain.norm((x * 2 + 1)[:, 128:], None, (w * w)[:128], 1e-6, 0.0)
+    out = gr.rms_norm((gx * 2 + 1)[:, 128:], (gw * gw)[:128])[0].torch().cpu()
+    assert ((out.double() - y).abs() <= (ROW + HALF[F32]) * y.abs()).all()
+    t = torch.ones(40, 256, device="cuda")
+    at = ctx.array(t)
+    reader = at + 1.0
+    gr.rms_norm(gx, gw, out=at)
+    assert bool((reader.torch() == 2.0).all()) and not bool((t == 1.0).all())
+    q, s = gr.quantize(gx * 3.0)
+    want = gr.quantize(ctx.array((x * 3.0).cuda()))
+    assert torch.equal(q.torch().float(), want[0].torch().float()) and torch.equal(s.torch(), want[1].torch())
+    # (a product's scales may be lazy too: here twice as large)
+    a, sa = gr.quantize(gx)
+    b, sb = gr.quantize(ctx.array(normal(3, 30, 256).cuda()), blocks=True)
+    once, twice = gr.dot_scaled(a, sa, b, sb, dtype=gr.GR_F32), gr.dot_scaled(a, sa * 2.0, b, sb, dtype=gr.GR_F32)
+    assert torch.equal(twice.torch(), once.torch() * 2)
+    total = (gr.dot_scaled(a, sa, b, sb, dtype=gr.GR_F32) * 2.0).sum()                       # and results go on as lazy arrays
+    assert abs(float(total.numpy()) - 2 * float(once.torch().double().sum())) <= 1e-5 * float(once.torch().double().abs().sum())
+
+
+@pytest.mark.gpu
+def test_captured_calls_replay(ctx):
+    """Calls with temporary memory and without in a graph, replayed with other contents and eager calls between; a capture that would have to allocate is refused."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = gr.Context(stream=stream.cuda_stream)
+        A = c.array
+        rows, D, N = 96, 2048, 512
+        x, res, dy = (torch.empty(rows, D, device="cuda", dtype=BF16) for _ in range(3))
+        w = normal(1, D).cuda()
+        b, sb = (t.torch() for t in gr.quantize(A(normal(2, N, D).cuda()), blocks=True))
+        total, dx = torch.empty_like(x), torch.empty_like(x)
+        q, s, dw = torch.empty(rows, D, device="cuda", dtype=E4M3), torch.empty(rows, D // 128, device="cuda"), torch.empty(D, device="cuda")
+        y, qt, st = torch.empty(rows, N, device="cuda", dtype=BF16), torch.empty(D, rows, device="cuda", dtype=E4M3), torch.empty(D, 1, device="cuda")
+
+        def fill(seed):
+            for i, t in enumerate((x, res, dy)):
+                t.copy_(normal(seed + i, rows, D, dtype=BF16))
+
+        def step():
+            gr.rms_norm(A(x), A(w), A(res), out=A(q), total=A(total), scales=A(s))
+            gr.dot_scaled(A(q), A(s), A(b), A(sb), out=A(y))
+            gr.rms_norm_grad(A(dy), A(total), A(w), dx=A(dx), dweight=A(dw))
+            gr.quantize(A(dx), transposed=True, out=A(qt), scales=A(st))
+
+        def results():
+            return [t.float().clone() for t in (total, q, s, y, dx, dw, qt, st)]
+
+        fill(10)
+        step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for seed in (20, 30, 40):
+            fill(seed)
+            step()
+            want = results()
+            for t in (total, q, s, y, dx, dw, qt, st):
+                t.view(torch.uint8).zero_()
+            graph.replay()
+            stream.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(results(), want)), seed
+            # an eager call that needs more temporary memory leaves the graph's where it is
+            gr.rms_norm_grad(A(torch.zeros(seed * 40, 4096, device="cuda")), A(torch.ones(seed * 40, 4096, device="cuda")), A(torch.ones(4096, device="cuda")))
+        del graph
+        fresh = gr.Context(stream=stream.cuda_stream)
+        F = fresh.array
+        graph = torch.cuda.CUDAGraph()
+        codes = []
+        with torch.cuda.graph(graph, stream=stream):
+            torch.zeros(1, device="cuda").add_(1)
+            for call in (lambda: gr.rms_norm_grad(F(dy), F(total), F(w), dx=F(dx), dweight=F(dw)), lambda: gr.dot_scaled(F(q), F(s), F(b), F(sb), out=F(y))):
+                try:
+                    call()
+                    codes.append("none")
+                except gr.GrError as e:
+                    codes.append(e.code)
+        assert codes == ["GR_ERR_OOM", "GR_ERR_OOM"]
+        stream.synchronize()
+        fresh.close()
+        c.close()
+
+
+@pytest.mark.gpu
+def test_calls_on_a_stream_that_is_not_torchs(ctx):
+    """The context's stream carries the work, and new results are taken for it."""
+    stream = torch.cuda.Stream()
+    c = gr.Context(stream=stream.cuda_stream)
+    x, w = normal(7, 300, 1024, dtype=BF16), normal(8, 1024)
+    gx, gw = x.cuda(), w.cuda()
+    torch.cuda.synchronize()
+    y, _ = plain.norm(x, None, w, 1e-6, 0.0)
+    for _ in range(5):
+        q, _, s = gr.rms_norm(c.array(gx), c.array(gw), eight=True)
+        p = gr.dot_scaled(q, s, q, s, dtype=gr.GR_F32)
+        c.sync()
+        check_eight(q.torch().float().cpu(), s.torch().cpu(), y, off=ROW + 2.0 ** -22)
+        want, size = plain.product(q.torch().cpu(), s.torch().cpu(), q.torch().cpu(), s.torch().cpu())
+        assert ((p.torch().cpu().double() - want).abs() <= (127 * 2.0 ** -23 + 12 * 2.0 ** -24) * size).all()
+    c.close()
+
+
+@pytest.mark.gpu
+def test_results_are_the_same_every_time(ctx):
+    x, w, dy = normal(1, 3000, 1024, dtype=BF16).cuda(), normal(2, 1024).cuda(), normal(3, 3000, 1024, dtype=BF16).cuda()
+    b, sb = gr.quantize(ctx.array(normal(4, 700, 1024).cuda()))
+    first = None
+    for _ in range(4):
+        q, _, s = gr.rms_norm(ctx.array(x), ctx.array(w), eight=True)
+        dx, dw = gr.rms_norm_grad(ctx.array(dy), ctx.array(x), ctx.array(w))
+        got = [t.torch().float() for t in (q, s, dx, dw, gr.dot_scaled(q, s, b, sb), gr.dot_scaled(q, s, b, sb, dtype=gr.GR_F32), gr.dot_scaled(q[:40], s[:40], b, sb))]
+        first = first or got
+        assert all(torch.equal(u, v) for u, v in zip(first, got))
