@@ -5,8 +5,15 @@ gradient on packed documents, weights updated in place, and generation of single
 
 trains the layer for a few steps to repeat each document's tokens two places later and then generates with it; it
 prints the loss per step and how far generated rows are from those of a whole forward pass.  float32 throughout: the
-projections are the lazy arrays' own products."""
+projections are the lazy arrays' own products.
+
+    python -m paper_1901_03771_amd.attention_layer --norm --eight
+
+the same with a norm in front of the projections, whose gain is trained too, and with the projections of training and of
+generation as products of 8-bit tensors (attention and the weights that are updated stay in float32)."""
 from __future__ import annotations
+
+import sys
 
 import torch
 
@@ -14,46 +21,88 @@ from . import lazy as gr
 
 
 class AttentionLayer:
-    """y = attention(rotary(x Wq), rotary(x Wk), x Wv) Wo; x (B, N, width), `heads` heads of `values` values on `shared` heads of k and v."""
+    """y = attention(rotary(x Wq), rotary(x Wk), x Wv) Wo; x (B, N, width), `heads` heads of `values` values on `shared` heads of k and v.
+    norm: x / sqrt(mean(x ** 2)) * gain in its place.  eight: products of 8-bit tensors with scales, forward and backward."""
 
-    def __init__(self, ctx: gr.Context, width: int, heads: int, shared: int, values: int, cap: float = 0.0, seed: int = 0):
+    def __init__(self, ctx: gr.Context, width: int, heads: int, shared: int, values: int, cap: float = 0.0, seed: int = 0, norm: bool = False, eight: bool = False):
         self.ctx, self.width, self.heads, self.shared, self.values, self.cap = ctx, width, heads, shared, values, cap
+        self.norm, self.eight = norm, eight
         g = torch.Generator().manual_seed(seed)
         device = f"cuda:{ctx.device}"
         self.weights = {name: (torch.randn(rows, cols, generator=g) * rows ** -0.5).to(device) for name, rows, cols in
                         (("q", width, heads * values), ("k", width, shared * values), ("v", width, shared * values), ("o", heads * values, width))}
+        if norm:
+            self.weights["gain"] = torch.ones(width, device=device)
         self._w = {name: ctx.array(t) for name, t in self.weights.items()}
         self.frequencies = gr.rotary_frequencies(values)
+        self._eight = {}   # of each weight, as the products of the forward pass and of the gradients take it
+
+    def _weight8(self, name: str, transposed: bool):
+        """The weight in 8 bits, in blocks: (columns, rows) for products with it, or as it lies for those with its transpose.  Laid out once until it is changed."""
+        if (name, transposed) not in self._eight:
+            self._eight[name, transposed] = gr.quantize(self._w[name], blocks=True, transposed=transposed)
+        return self._eight[name, transposed]
+
+    def _product(self, x, name: str):
+        """x W; with eight, x may come as (values, scales) already."""
+        if not self.eight:
+            return gr.dot(x, self._w[name])
+        q, s = x if isinstance(x, tuple) else gr.quantize(x)
+        return gr.dot_scaled(q, s, *self._weight8(name, True), dtype=gr.GR_F32)
+
+    def _product_back(self, dy, name: str):
+        """dy W'."""
+        if not self.eight:
+            return gr.dot(dy, self._w[name].T)
+        return gr.dot_scaled(*gr.quantize(dy), *self._weight8(name, False), dtype=gr.GR_F32)
+
+    def _weight_gradient(self, x, dy):
+        """x' dy: with eight, sums over tokens of both sides' columns in 8 bits."""
+        if not self.eight:
+            return gr.dot(x.T, dy)
+        return gr.dot_scaled(*gr.quantize(x, transposed=True), *gr.quantize(dy, transposed=True), dtype=gr.GR_F32)
+
+    def _normed(self, lx):
+        """What the projections take of the rows lx; with eight, (values, scales), which all of them share."""
+        if not self.norm:
+            return gr.quantize(lx) if self.eight else lx
+        h, _, scales = gr.rms_norm(lx, self._w["gain"], eight=self.eight)
+        return (h, scales) if self.eight else h
 
     def _projected(self, x, name: str, shape):
-        return gr.reshape(gr.dot(x, self._w[name]), shape)
+        return gr.reshape(self._product(x, name), shape)
 
     def forward(self, x, positions, documents):
         """Returns y (B * N, width), unevaluated, and what the gradient needs."""
         B, N, _ = x.shape
         lx = self.ctx.array(x.view(B * N, self.width))
-        q = gr.rotary(self._projected(lx, "q", (B, N, self.heads, self.values)), self.frequencies, positions)
-        k = gr.rotary(self._projected(lx, "k", (B, N, self.shared, self.values)), self.frequencies, positions)
-        v = self._projected(lx, "v", (B, N, self.shared, self.values)).materialize()
+        h = self._normed(lx)
+        q = gr.rotary(self._projected(h, "q", (B, N, self.heads, self.values)), self.frequencies, positions)
+        k = gr.rotary(self._projected(h, "k", (B, N, self.shared, self.values)), self.frequencies, positions)
+        v = self._projected(h, "v", (B, N, self.shared, self.values)).materialize()
         scores = self.ctx.scores(cap=self.cap, causal=True, documents=documents)
         out, lse = gr.attention(q, k, v, scores)
-        y = gr.dot(gr.reshape(out, (B * N, self.heads * self.values)), self._w["o"])
-        return y, (lx, positions, scores, q, k, v, out, lse)
+        y = self._product(gr.reshape(out, (B * N, self.heads * self.values)), "o")
+        return y, (lx, h, positions, scores, q, k, v, out, lse)
 
     def gradients(self, dy, kept):
         """The weights' gradients, unevaluated, for the gradient `dy` (B * N, width) of y."""
-        lx, positions, scores, q, k, v, out, lse = kept
+        lx, h, positions, scores, q, k, v, out, lse = kept
         B, N = q.shape[:2]
         flat = gr.reshape(out, (B * N, self.heads * self.values)).materialize()
-        dout = gr.reshape(gr.dot(dy, self._w["o"].T), (B, N, self.heads, self.values))
+        dout = gr.reshape(self._product_back(dy, "o"), (B, N, self.heads, self.values))
         dq, dk, dv = gr.attention_grad(dout, q, k, v, scores, out, lse)
         for d in (dq, dk):
             gr.rotary(d, self.frequencies, positions, inverse=True, out=d)   # back through the turn, in place
         rows = B * N
-        return {"o": gr.dot(flat.T, dy),
-                "q": gr.dot(lx.T, gr.reshape(dq, (rows, self.heads * self.values)).materialize()),
-                "k": gr.dot(lx.T, gr.reshape(dk, (rows, self.shared * self.values)).materialize()),
-                "v": gr.dot(lx.T, gr.reshape(dv, (rows, self.shared * self.values)).materialize())}
+        d = {name: gr.reshape(g, (rows, heads * self.values)).materialize() for name, g, heads in (("q", dq, self.heads), ("k", dk, self.shared), ("v", dv, self.shared))}
+        if self.eight:   # (by rows is not how a sum over tokens takes them)
+            h = gr.rms_norm(lx, self._w["gain"])[0] if self.norm else lx
+        grads = {"o": self._weight_gradient(flat, dy), **{name: self._weight_gradient(h, g) for name, g in d.items()}}
+        if self.norm:
+            dh = (self._product_back(d["q"], "q") + self._product_back(d["k"], "k")) + self._product_back(d["v"], "v")
+            grads["gain"] = gr.rms_norm_grad(dh, lx, self._w["gain"])[1]
+        return grads
 
     def train_step(self, x, target, positions, documents, rate: float) -> float:
         """One step of gradient descent on the mean square of y - target; returns it."""
@@ -65,25 +114,27 @@ class AttentionLayer:
         for g in grads.values():
             g.materialize()
         for name, g in grads.items():
-            self._w[name][:, :] = self._w[name] - g * rate
+            w = self._w[name]
+            w[tuple([slice(None)] * w.ndim)] = w - g * rate
+        self._eight.clear()
         return float(loss.numpy()) / (rows * self.width)
 
     def step(self, x, cache_k, cache_v, lengths):
         """The next token x (B, width) of each sequence: its k and v go into row lengths[b] of the caches (B, M, shared, values), lengths (i32)
         grows by one, and y (B, width) comes back as a tensor."""
         B = x.shape[0]
-        lx = self.ctx.array(x)
+        h = self._normed(self.ctx.array(x))
         positions = self.ctx.array(lengths.view(B, 1))
-        q = gr.rotary(self._projected(lx, "q", (B, 1, self.heads, self.values)), self.frequencies, positions)
-        k = gr.rotary(self._projected(lx, "k", (B, 1, self.shared, self.values)), self.frequencies, positions)
-        v = self._projected(lx, "v", (B, 1, self.shared, self.values))
+        q = gr.rotary(self._projected(h, "q", (B, 1, self.heads, self.values)), self.frequencies, positions)
+        k = gr.rotary(self._projected(h, "k", (B, 1, self.shared, self.values)), self.frequencies, positions)
+        v = self._projected(h, "v", (B, 1, self.shared, self.values))
         each, at = torch.arange(B, device=x.device), lengths.long()
         cache_k[each, at] = k.torch(copy=False)[:, 0]
         cache_v[each, at] = v.torch(copy=False)[:, 0]
         lengths += 1
         out = gr.attention_step(self.ctx.array(q.torch(copy=False)[:, 0]), self.ctx.array(cache_k), self.ctx.array(cache_v),
                                 self.ctx.scores(cap=self.cap, lengths=self.ctx.array(lengths)))
-        return gr.dot(gr.reshape(out, (B, self.heads * self.values)), self._w["o"]).torch()
+        return self._product(gr.reshape(out, (B, self.heads * self.values)), "o").torch()
 
 
 def packed_documents(batch: int, rows: int, device, seed: int = 0):
@@ -96,9 +147,9 @@ def packed_documents(batch: int, rows: int, device, seed: int = 0):
     return ids.to(device), (torch.arange(rows) - start).to(torch.int32).to(device)
 
 
-def main():
+def main(arguments=()):
     ctx = gr.Context()
-    layer = AttentionLayer(ctx, width=64, heads=4, shared=2, values=32, cap=30.0)
+    layer = AttentionLayer(ctx, width=64, heads=4, shared=2, values=32, cap=30.0, norm="--norm" in arguments, eight="--eight" in arguments)
     device = f"cuda:{ctx.device}"
     ids, places = packed_documents(2, 256, device)
     g = torch.Generator().manual_seed(1)
@@ -118,4 +169,4 @@ def main():
 
 
 if __name__ == "__main__":
-    main()
+    main(sys.argv[1:])

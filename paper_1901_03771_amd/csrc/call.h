@@ -21,10 +21,19 @@
 
 namespace gr {
 
+// The operands or results of a call, by handle and name: none has more.  (Nothing is allocated for them: a call of small tensors is bound by the host.)
+struct Named {
+  std::pair<gr_array, const char*> list[16];
+  int n = 0;
+  void push_back(const std::pair<gr_array, const char*>& a) { if (n == 16) throw std::bad_alloc(); list[n++] = a; }
+  const std::pair<gr_array, const char*>* begin() const { return list; }
+  const std::pair<gr_array, const char*>* end() const { return list + n; }
+};
+
 struct Call {
   gr_ctx* ctx;
   const char* name;
-  std::vector<std::pair<gr_array, const char*>> inputs, results;
+  Named inputs, results;
 
   gr_status error(gr_status s, const std::string& what) const { return fail(ctx, s, std::string(name) + ": " + what); }
 

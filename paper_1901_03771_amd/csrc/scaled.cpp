@@ -57,35 +57,34 @@ struct Call : gr::Call {
 // The rows of tensors of one shape, axes that can be walked as one taken together.
 struct Walk {
   Call& c;
-  std::vector<std::pair<gr_array, Rows*>> tensors;
-  void add(gr_array a, Rows* r) { if (a) tensors.push_back({a, r}); }
+  gr_array arrays[5];
+  Rows* rows[5];
+  int count = 0;
+  explicit Walk(Call& call) : c(call) {}
+  void add(gr_array a, Rows* r) { if (a) { arrays[count] = a; rows[count++] = r; } }
   void fill(Norm* n) {
-    const Node* x = lookup(c.ctx, tensors[0].first);
-    std::vector<int> axes;
-    for (int d = 0; d + 1 < x->ndim; ++d) if (x->shape[d] > 1) axes.push_back(d);
-    std::vector<int64_t> extents;
-    std::vector<std::vector<int64_t>> steps(tensors.size());
-    for (int d : axes) {
-      bool joined = !extents.empty();
-      for (size_t t = 0; t < tensors.size() && joined; ++t) joined = steps[t].back() == c.step(tensors[t].first, d) * x->shape[d];
-      if (joined) extents.back() *= x->shape[d];
-      else extents.push_back(x->shape[d]);
-      for (size_t t = 0; t < tensors.size(); ++t) {
-        const int64_t s = c.step(tensors[t].first, d);
-        if (joined) steps[t].back() = s;
-        else steps[t].push_back(s);
-      }
+    const Node* x = lookup(c.ctx, arrays[0]);
+    int64_t extents[3] = {1, 1, 1}, steps[5][3] = {};
+    StoredView views[5];
+    for (int t = 0; t < count; ++t) {
+      views[t] = c.view(arrays[t]);
+      rows[t]->p = views[t].data;
     }
-    const size_t k = extents.size();
+    int k = 0;
+    for (int d = 0; d + 1 < x->ndim; ++d) {
+      if (x->shape[d] <= 1) continue;
+      bool joined = k > 0;
+      for (int t = 0; t < count && joined; ++t) joined = steps[t][k - 1] == views[t].strides[d] * x->shape[d];
+      if (joined) extents[k - 1] *= x->shape[d];
+      else extents[k++] = x->shape[d];
+      for (int t = 0; t < count; ++t) steps[t][k - 1] = views[t].strides[d];
+    }
     n->n1 = k >= 2 ? (int)extents[k - 2] : 1;
     n->n2 = k >= 2 ? (int)extents[k - 1] : 1;
-    for (size_t t = 0; t < tensors.size(); ++t) {
-      Rows* r = tensors[t].second;
-      r->p = c.view(tensors[t].first).data;
-      const std::vector<int64_t>& s = steps[t];
-      r->s0 = k == 1 ? s[0] : k == 3 ? s[0] : 0;
-      r->s1 = k >= 2 ? s[k - 2] : 0;
-      r->s2 = k >= 2 ? s[k - 1] : 0;
+    for (int t = 0; t < count; ++t) {
+      rows[t]->s0 = k == 1 || k == 3 ? steps[t][0] : 0;
+      rows[t]->s1 = k >= 2 ? steps[t][k - 2] : 0;
+      rows[t]->s2 = k >= 2 ? steps[t][k - 1] : 0;
     }
   }
 };
@@ -152,7 +151,7 @@ static gr_status rms_norm(gr_ctx* ctx, gr_array x, gr_array residual, gr_array w
   Norm a;
   a.rows = r.rows;
   a.D = (int)r.D;
-  Walk w{c};
+  Walk w(c);
   w.add(x, &a.x);
   w.add(residual, &a.residual);
   w.add(total, &a.total);
@@ -190,7 +189,7 @@ static gr_status rms_norm_grad(gr_ctx* ctx, gr_array dout, gr_array total, gr_ar
   Norm a;
   a.rows = r.rows;
   a.D = (int)r.D;
-  Walk w{c};
+  Walk w(c);
   w.add(total, &a.x);
   w.add(dout, &a.dout);
   w.add(dtotal, &a.residual);

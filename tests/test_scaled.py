@@ -751,3 +751,118 @@ def test_results_are_the_same_every_time(ctx):
         got = [t.torch().float() for t in (q, s, dx, dw, gr.dot_scaled(q, s, b, sb), gr.dot_scaled(q, s, b, sb, dtype=gr.GR_F32), gr.dot_scaled(q[:40], s[:40], b, sb))]
         first = first or got
         assert all(torch.equal(u, v) for u, v in zip(first, got))
+
+
+class EightProduct(torch.autograd.Function):
+    """x W and its gradients in binary64, of the values that the 8-bit tensors of a layer stand for."""
+
+    @staticmethod
+    def rounded(x, blocks=False):
+        s = plain.scales_of(x, blocks).float()
+        each = plain.spread(s, x.shape)
+        return (x.float() / each.float()).clamp(-448, 448).to(E4M3).double() * each
+
+    @staticmethod
+    def forward(ctx, x, w):
+        ctx.save_for_backward(x, w)
+        return EightProduct.rounded(x) @ EightProduct.rounded(w.T, True).T
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w = ctx.saved_tensors
+        return EightProduct.rounded(dy) @ EightProduct.rounded(w, True).T, EightProduct.rounded(x.T) @ EightProduct.rounded(dy.T).T
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm,eight", [(True, False), (True, True), (False, True)], ids=["norm", "norm_eight", "eight"])
+def test_layer_with_norm_and_eight_bits(norm, eight):
+    """The layer's training step and its generation against the same in binary64 with automatic differentiation, 8-bit roundings included."""
+    from paper_1901_03771_amd import attention_layer as al
+    c = gr.Context()
+    layer = al.AttentionLayer(c, width=144, heads=4, shared=2, values=24, cap=8.0, seed=4, norm=norm, eight=eight)
+    g = torch.Generator().manual_seed(6)
+    x, target = torch.randn(2, 70, 144, generator=g).cuda(), torch.randn(2, 70, 144, generator=g).cuda()
+    if norm:
+        layer.weights["gain"].copy_(1 + 0.2 * torch.randn(144, generator=g))
+    w = {n: t.cpu().double().requires_grad_() for n, t in layer.weights.items()}
+    times = EightProduct.apply if eight else torch.matmul
+
+    def turned(t):
+        a = torch.arange(70).double()[:, None, None] * torch.tensor(list(layer.frequencies), dtype=torch.float64)
+        lo, hi = t[..., :12], t[..., 12:]
+        return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+
+    h = x.cpu().double().view(140, 144)
+    if norm:
+        h = h / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6) * w["gain"]
+    q, k, v = turned(times(h, w["q"]).view(2, 70, 4, 24)), turned(times(h, w["k"]).view(2, 70, 2, 24)), times(h, w["v"]).view(2, 70, 2, 24)
+    k, v = k.repeat_interleave(2, 2), v.repeat_interleave(2, 2)
+    s = 8.0 * torch.tanh(torch.einsum("bihd,bjhd->bhij", q, k) * 24 ** -0.5 / 8.0)
+    p = torch.softmax(s.masked_fill(torch.ones(70, 70, dtype=torch.bool).triu(1), -math.inf), -1)
+    y = times(torch.einsum("bhij,bjhd->bihd", p, v).reshape(140, 96), w["o"])
+    loss = ((y - target.cpu().double().view(140, 144)) ** 2).mean()
+    loss.backward()
+    before = {n: t.cpu().double() for n, t in layer.weights.items()}
+    got = layer.train_step(x, target, 0, None, rate=1.0)
+    # float32: a handful of products and sums of up to 144 values one after another, as for the layer without norm, and the norm's own error.
+    bar = 6 * (140 + 144) * 2.0 ** -24 * 16
+    if eight:
+        # Two computations that agree to `bar` before a rounding to 8 bits fall to different sides of a middle where a value is that near to one: of the steps between numbers, 2^-4 of a value
+        # at least, a share of 2 bar / 2^-4; there they differ by 2^-3 of the value, in norm by 2^-3 sqrt(share) of all.  Four roundings in a row, their gradients as many.
+        bar = 8 * 2.0 ** -3 * math.sqrt(2 * bar / 2.0 ** -4)
+    assert abs(got - loss.item()) <= bar * loss.item()
+    for n, t in layer.weights.items():
+        step = before[n] - t.cpu().double()
+        assert (step - w[n].grad).norm() <= bar * w[n].grad.norm() + 2.0 ** -24 * before[n].norm(), n
+    one = x[:, :20].contiguous()
+    whole = layer.forward(one, 0, None)[0].torch().view(2, 20, 144)
+    cache = [torch.full((2, 30, 2, 24), math.nan, device="cuda") for _ in range(2)]
+    lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for i in range(20):
+        y1 = layer.step(one[:, i].contiguous(), *cache, lengths)
+        assert (y1 - whole[:, i]).norm() <= bar * whole[:, i].norm(), i
+    c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("arguments", [["--norm"], ["--norm", "--eight"]])
+def test_layer_command_runs(arguments, capsys):
+    from paper_1901_03771_amd import attention_layer as al
+    al.main(arguments)
+    assert "step 7: mean square" in capsys.readouterr().out
+
+
+@pytest.mark.gpu
+def test_a_step_of_a_layer_in_eight_bits(ctx):
+    """The calls as they follow one another in training: norm, product, both gradients of the product, the norm's gradient; each against binary64 of what the one before it gave."""
+    rows, D, N = 300, 520, 260
+    x, res, dy = normal(1, rows, D, dtype=BF16), normal(2, rows, D, dtype=BF16, by=2.0), normal(3, rows, N, dtype=BF16)
+    w, gain = normal(4, N, D, by=D ** -0.5), 1 + normal(5, D, by=0.2)
+    A = lambda t: ctx.array(t.cuda())  # noqa: E731
+    h8, stream, hs = gr.rms_norm(A(x), A(gain), A(res), eight=True)
+    y64, total = plain.norm(x, res, gain, 1e-6, 0.0)
+    assert torch.equal(stream.torch().cpu(), total)
+    check_eight(h8.torch().float().cpu(), hs.torch().cpu(), y64, off=ROW + 2.0 ** -22)
+    w8, ws = gr.quantize(A(w), blocks=True)
+    out = gr.dot_scaled(h8, hs, w8, ws)
+    want, size = plain.product(h8.torch().cpu(), hs.torch().cpu(), w8.torch().cpu(), ws.torch().cpu())
+    room = 127 * 2.0 ** -23 + 16 * 2.0 ** -24
+    assert ((out.torch().cpu().double() - want).abs() <= (room + 7 * 2.0 ** -13) * size + HALF[BF16] * want.abs()).all()
+    # dx = dy W: the same blocks, transposed
+    wt, wts = gr.quantize(A(w), blocks=True, transposed=True)
+    assert torch.equal(wt.torch().float(), w8.torch().float().T) and torch.equal(wts.torch(), ws.torch().T)
+    d8, ds = gr.quantize(A(dy))
+    dh = gr.dot_scaled(d8, ds, wt, wts)
+    want, size = plain.product(d8.torch().cpu(), ds.torch().cpu(), wt.torch().cpu(), wts.torch().cpu())
+    assert ((dh.torch().cpu().double() - want).abs() <= (room + 7 * 2.0 ** -13) * size + HALF[BF16] * want.abs()).all()
+    # dW = dy' h: sums over tokens
+    h = gr.rms_norm(stream, A(gain))[0]
+    dt, dts = gr.quantize(A(dy), transposed=True)
+    ht, hts = gr.quantize(h, transposed=True)
+    dw = gr.dot_scaled(dt, dts, ht, hts, dtype=gr.GR_F32)
+    want, size = plain.product(dt.torch().cpu(), dts.torch().cpu(), ht.torch().cpu(), hts.torch().cpu())
+    assert ((dw.torch().cpu().double() - want).abs() <= room * size).all()
+    dx, dgain = gr.rms_norm_grad(dh, stream, A(gain), dtotal=A(dy[:, :1].expand(rows, D).contiguous()))
+    want, wgain, size, terms = plain.norm_grad(dh.torch().cpu(), total, gain, dy[:, :1].expand(rows, D), 1e-6, 0.0)
+    assert ((dx.torch().cpu().double() - want).abs() <= 4 * ROW * size + HALF[BF16] * want.abs()).all()
+    assert ((dgain.torch().cpu().double() - wgain).abs() <= (ROW + (rows + 4) * 2.0 ** -24) * terms).all()
