@@ -32,7 +32,8 @@ extern "C" {
 /* total = x + residual, rounded to its type (residual = 0: total is x, and no result; total = 0: not wanted);
  * r = 1 / sqrt(mean(total^2) + eps) over the last axis;  out = total r (offset + weight).
  * x, residual, total: f32 or bf16, one type, 1 to 4 axes, up to 32768 values in a row.  out: of that type, or GR_E4M3 with `scales` of rows.
- * weight: f32 or x's type, (D); 0 = a factor of 1 (offset must be 0).  eps: 1e-12 .. 1.  Squares are summed in f32: a row whose sum passes its range has out 0.
+ * weight: f32 or x's type, (D); 0 = a factor of 1 (offset must be 0).  eps: 1e-12 .. 1.  Squares are summed in f32: a row whose sum passes its range (values of 10^18 and more) has out 0, and a
+ * gradient that may be NaN.
  * total and out may each be x or residual themselves (the same view). */
 gr_status gr_rms_norm(gr_ctx* ctx, gr_array x, gr_array residual, gr_array weight, double eps, double offset, gr_array total, gr_array out, gr_array scales);
 

@@ -13,7 +13,7 @@ namespace gr {
 namespace scaled {
 
 constexpr int64_t LIMIT = int64_t(1) << 30;      // extents that kernels hold in 32 bits
-constexpr int64_t GROUPS = int64_t(1) << 22;     // workgroups of a launch: 1024 threads each do not reach 2^32
+constexpr int64_t GROUPS = int64_t(1) << 22;     // workgroups of a launch: 512 threads of each do not reach 2^32
 
 struct Call : gr::Call {
   static int type_of(int dtype) { return dtype == GR_F32 ? F32 : dtype == GR_BF16 ? BF16 : E4M3; }
@@ -221,7 +221,7 @@ static gr_status quantize_call(gr_ctx* ctx, gr_array x, int blocks, int transpos
   if ((blocks != 0 && blocks != 1) || (transposed != 0 && transposed != 1)) return c.error(GR_ERR_ARG, "blocks and transposed must be 0 or 1");
   const int64_t M = n->shape[0], K = n->shape[1], R = transposed ? K : M, C = transposed ? M : K;
   const int dt = n->dtype;
-  if (M * blocks_of(K) > GROUPS * 128 || ((blocks || transposed) && blocks_of(M) * blocks_of(K) > GROUPS)) return c.error(GR_ERR_UNSUPPORTED, "more values than a launch holds");
+  if (M * blocks_of(K) > GROUPS * 64 || ((blocks || transposed) && blocks_of(M) * blocks_of(K) > GROUPS)) return c.error(GR_ERR_UNSUPPORTED, "more values than a launch holds");
   TRY(c.take(x, "x", dt, {M, K}, false));
   TRY(c.take(out, "out", GR_E4M3, {R, C}, true));
   TRY(c.take(scales, "scales", GR_F32, {blocks ? blocks_of(R) : R, blocks_of(C)}, true));
@@ -306,7 +306,7 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   TRY(c.take(out, "out", dt, {M, N}, true));
   TRY(c.neighbours({{a, "a"}, {b, "b"}, {out, "out"}}));
   Dot d;
-  if (blocks_of(M) * blocks_of(N) > GROUPS) return c.error(GR_ERR_UNSUPPORTED, "more results than a launch holds");
+  if (blocks_of(M) * blocks_of(N) > GROUPS || N > GROUPS * 32) return c.error(GR_ERR_UNSUPPORTED, "more results than a launch holds");   // (32 columns a workgroup at least)
   TRY(c.settle());
   if (M == 0 || N == 0) return GR_OK;
   d.a = (const uint8_t*)c.view(a).data;

@@ -163,6 +163,7 @@ def test_calls_beyond_a_launch_are_refused(dry):  # noqa: F811
     m = 1 << 20
     refused("GR_ERR_UNSUPPORTED", gr.dot_scaled, big((m, 1)), big((m, 1), gr.GR_F32), big((m, 1)), big((m, 1), gr.GR_F32), out=big((m, m), gr.GR_F32))
     refused("GR_ERR_UNSUPPORTED", gr.dot_scaled, big((m << 11, 1)), big((m << 11, 1), gr.GR_F32), big((1, 1)), big((1, 1), gr.GR_F32), out=big((m << 11, 1), gr.GR_F32))
+    refused("GR_ERR_UNSUPPORTED", gr.dot_scaled, big((1, 1)), big((1, 1), gr.GR_F32), big((1 << 28, 1)), big((1 << 28, 1), gr.GR_F32), out=big((1, 1 << 28), gr.GR_F32))
     refused("GR_ERR_UNSUPPORTED", gr.quantize, big((1 << 30, 1), gr.GR_F32), out=big((1 << 30, 1)), scales=big((1 << 30, 1), gr.GR_F32))
     refused("GR_ERR_UNSUPPORTED", gr.rms_norm, big((1 << 31, 1), gr.GR_F32), out=big((1 << 31, 1), gr.GR_F32))
     assert dry.stats()["kernel_launches"] == n
