@@ -67,7 +67,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void gr_rms_norm_kernel(cons
   float w[V][N];
   weights<TPR, V, N>(a, t, w);
   int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * PER; row0 < a.rows; row0 += (int64_t)gridDim.x * PER) {
+  // Workgroups go round the eight XCDs in turn, each with an L2 of its own: eight neighbouring rows go to one XCD, so that the scales of a block, which may lie side by side, are written
+  // to memory together.
+  unsigned place = blockIdx.x;
+  if (EIGHT && gridDim.x % 64 == 0) place = place / 64 * 64 + place % 8 * 8 + place / 8 % 8;
+  for (int64_t row0 = (int64_t)place * PER; row0 < a.rows; row0 += (int64_t)gridDim.x * PER) {
     const int64_t row = row0 + sub < a.rows ? row0 + sub : a.rows - 1;
     const bool mine = row0 + sub < a.rows;
     const int D = mine ? a.D : 0;             // (a row behind the last is neither read nor written)

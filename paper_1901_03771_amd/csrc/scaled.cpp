@@ -221,7 +221,8 @@ static gr_status quantize_call(gr_ctx* ctx, gr_array x, int blocks, int transpos
   if ((blocks != 0 && blocks != 1) || (transposed != 0 && transposed != 1)) return c.error(GR_ERR_ARG, "blocks and transposed must be 0 or 1");
   const int64_t M = n->shape[0], K = n->shape[1], R = transposed ? K : M, C = transposed ? M : K;
   const int dt = n->dtype;
-  if (M * blocks_of(K) > GROUPS * 64 || ((blocks || transposed) && blocks_of(M) * blocks_of(K) > GROUPS)) return c.error(GR_ERR_UNSUPPORTED, "more values than a launch holds");
+  // (the fewest rows that a workgroup has are 8, and a tile is 128 x 128)
+  if ((blocks || transposed ? blocks_of(M) : (M + 7) / 8) * blocks_of(K) > GROUPS * (blocks || transposed ? 1 : 2)) return c.error(GR_ERR_UNSUPPORTED, "more values than a launch holds");
   TRY(c.take(x, "x", dt, {M, K}, false));
   TRY(c.take(out, "out", GR_E4M3, {R, C}, true));
   TRY(c.take(scales, "scales", GR_F32, {blocks ? blocks_of(R) : R, blocks_of(C)}, true));
