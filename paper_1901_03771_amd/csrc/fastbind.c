@@ -13,7 +13,7 @@
 #include <Python.h>
 #include <structmember.h>
 
-#include "../../include/grumpy_hip.h"
+#include "../../include/grumpy_hip_scaled.h"
 
 /* Where a Context keeps the address of its gr_ctx (attribute _cell): 0 once closed.  Every array holds its context's, so that a
  * recorded operation and a dropped handle reach the library without looking up an attribute. */
@@ -53,6 +53,10 @@ static __typeof__(&gr_release) p_release;
 static __typeof__(&gr_reduce) p_reduce;
 static __typeof__(&gr_ndim) p_ndim;
 static __typeof__(&gr_shape) p_shape;
+static __typeof__(&gr_rms_norm) p_rms_norm;
+static __typeof__(&gr_rms_norm_grad) p_rms_norm_grad;
+static __typeof__(&gr_quantize) p_quantize;
+static __typeof__(&gr_dot_scaled) p_dot_scaled;
 
 static PyObject* hook_binary;   /* (op, a, b) -> Array, for operands this file does not marshal */
 static PyObject* hook_getitem;  /* (a, key) -> Array */
@@ -566,6 +570,65 @@ static PyObject* mod_binary(PyObject* m, PyObject* const* args, Py_ssize_t nargs
   return do_binary(op, args[1], args[2]);
 }
 
+/* The calls of grumpy_hip_scaled.h on arrays of one open context: a call of small tensors is over before its arguments are marshalled twice.  Each returns the
+ * status, or None for anything that this file does not marshal, which the binding then looks at (and refuses, if it is wrong). */
+static int handles(PyObject* const* args, Py_ssize_t n, unsigned optional, gr_ctx** ctx, gr_array* h) {
+  CellObject* cell = NULL;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (args[i] == Py_None && (optional >> i & 1)) { h[i] = 0; continue; }
+    if (!IS_ARRAY(args[i])) return 0;
+    ArrayObject* a = (ArrayObject*)args[i];
+    if (!a->cell || (cell && a->cell != cell)) return 0;
+    cell = a->cell;
+    h[i] = a->h;
+  }
+  if (!cell || !cell->address) return 0;
+  *ctx = (gr_ctx*)(uintptr_t)cell->address;
+  return 1;
+}
+
+static int numbers(PyObject* const* args, Py_ssize_t n, double* v) {
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!PyFloat_Check(args[i])) return 0;
+    v[i] = PyFloat_AS_DOUBLE(args[i]);
+  }
+  return 1;
+}
+
+static PyObject* mod_rms_norm(PyObject* m, PyObject* const* args, Py_ssize_t nargs) {
+  gr_ctx* ctx;
+  gr_array h[6];
+  double v[2];
+  if (nargs != 8) { PyErr_SetString(PyExc_TypeError, "rms_norm(x, residual, weight, total, out, scales, eps, offset)"); return NULL; }
+  if (!handles(args, 6, 0x2e, &ctx, h) || !numbers(args + 6, 2, v)) Py_RETURN_NONE;
+  return PyLong_FromLong(p_rms_norm(ctx, h[0], h[1], h[2], v[0], v[1], h[3], h[4], h[5]));
+}
+
+static PyObject* mod_rms_norm_grad(PyObject* m, PyObject* const* args, Py_ssize_t nargs) {
+  gr_ctx* ctx;
+  gr_array h[6];
+  double v[2];
+  if (nargs != 8) { PyErr_SetString(PyExc_TypeError, "rms_norm_grad(dout, total, weight, dtotal, dx, dweight, eps, offset)"); return NULL; }
+  if (!handles(args, 6, 0x2c, &ctx, h) || !numbers(args + 6, 2, v)) Py_RETURN_NONE;
+  return PyLong_FromLong(p_rms_norm_grad(ctx, h[0], h[1], h[2], h[3], v[0], v[1], h[4], h[5]));
+}
+
+static PyObject* mod_quantize(PyObject* m, PyObject* const* args, Py_ssize_t nargs) {
+  gr_ctx* ctx;
+  gr_array h[3];
+  if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "quantize(x, out, scales, blocks, transposed)"); return NULL; }
+  if (!handles(args, 3, 0, &ctx, h) || !PyBool_Check(args[3]) || !PyBool_Check(args[4])) Py_RETURN_NONE;
+  return PyLong_FromLong(p_quantize(ctx, h[0], args[3] == Py_True, args[4] == Py_True, h[1], h[2]));
+}
+
+static PyObject* mod_dot_scaled(PyObject* m, PyObject* const* args, Py_ssize_t nargs) {
+  gr_ctx* ctx;
+  gr_array h[5];
+  if (nargs != 5) { PyErr_SetString(PyExc_TypeError, "dot_scaled(a, a_scales, b, b_scales, out)"); return NULL; }
+  if (!handles(args, 5, 0, &ctx, h)) Py_RETURN_NONE;
+  return PyLong_FromLong(p_dot_scaled(ctx, h[0], h[1], h[2], h[3], h[4]));
+}
+
 static int take_address(PyObject* d, const char* name, void** out) {
   PyObject* v = PyDict_GetItemString(d, name);
   if (!v) { PyErr_Format(PyExc_KeyError, "bind: address of %s is missing", name); return 0; }
@@ -585,7 +648,9 @@ static PyObject* mod_bind(PyObject* m, PyObject* d) {
       !take_address(d, "gr_materialize_into", (void**)&p_materialize_into) ||
       !take_address(d, "gr_materialize_into_static", (void**)&p_materialize_into_static) ||
       !take_address(d, "gr_is_materialized", (void**)&p_is_materialized) ||
-      !take_address(d, "gr_program_run", (void**)&p_program_run))
+      !take_address(d, "gr_program_run", (void**)&p_program_run) ||
+      !take_address(d, "gr_rms_norm", (void**)&p_rms_norm) || !take_address(d, "gr_rms_norm_grad", (void**)&p_rms_norm_grad) ||
+      !take_address(d, "gr_quantize", (void**)&p_quantize) || !take_address(d, "gr_dot_scaled", (void**)&p_dot_scaled))
     return NULL;
   Py_RETURN_NONE;
 }
@@ -608,6 +673,10 @@ static PyMethodDef module_methods[] = {
     {"leaf", (PyCFunction)(void (*)(void))mod_leaf, METH_FASTCALL, "leaf(type, ctx, address, dtype, shape, strides, owner): gr_array_from_device, None if not marshalled here"},
     {"wrap", (PyCFunction)(void (*)(void))mod_wrap, METH_FASTCALL, "wrap(type, ctx, tensor, codes): leaf of a tensor on the GPU, None if not marshalled here"},
     {"program_run", (PyCFunction)(void (*)(void))mod_program_run, METH_FASTCALL, "program_run(program, input addresses, output address) -> status: gr_program_run"},
+    {"rms_norm", (PyCFunction)(void (*)(void))mod_rms_norm, METH_FASTCALL, "rms_norm(x, residual, weight, total, out, scales, eps, offset) -> status: gr_rms_norm, None if not marshalled here"},
+    {"rms_norm_grad", (PyCFunction)(void (*)(void))mod_rms_norm_grad, METH_FASTCALL, "rms_norm_grad(dout, total, weight, dtotal, dx, dweight, eps, offset) -> status: gr_rms_norm_grad, likewise"},
+    {"quantize", (PyCFunction)(void (*)(void))mod_quantize, METH_FASTCALL, "quantize(x, out, scales, blocks, transposed) -> status: gr_quantize, likewise"},
+    {"dot_scaled", (PyCFunction)(void (*)(void))mod_dot_scaled, METH_FASTCALL, "dot_scaled(a, a_scales, b, b_scales, out) -> status: gr_dot_scaled, likewise"},
     {"bind", mod_bind, METH_O, "bind({name: address}): entry points of the loaded library"},
     {"set_hooks", mod_set_hooks, METH_VARARGS, "set_hooks(binary, getitem, setitem, pow, reduce): Python fallbacks"},
     {NULL, NULL, 0, NULL}};

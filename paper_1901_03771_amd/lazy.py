@@ -577,7 +577,8 @@ def _bind_fast_paths(L):
         return
     names = ["gr_array_from_device", "gr_unary", "gr_binary", "gr_binary_scalar", "gr_slice", "gr_transpose", "gr_dot", "gr_assign",
              "gr_materialize", "gr_release", "gr_reduce", "gr_ndim", "gr_shape", "gr_materialize_into",
-             "gr_materialize_into_static", "gr_is_materialized", "gr_program_run"]
+             "gr_materialize_into_static", "gr_is_materialized", "gr_program_run", "gr_rms_norm", "gr_rms_norm_grad", "gr_quantize",
+             "gr_dot_scaled"]
     _fastbind.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names})
     _fastbind.set_hooks(_binary_slow, slice_, _setitem_slow, _pow_slow, _reduce_slow)
 
@@ -972,6 +973,8 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
 
 
 # ---- norms, 8-bit tensors with scales and their products (include/grumpy_hip_scaled.h) ------------------------------------
+# Calls whose results are all given go through the C type first: it takes what is ordinary, and whatever it does not take, or the library refuses (before anything
+# runs), goes the longer way, which raises what there is to raise.
 
 def _float_code(a: "Array") -> int:
     """The element type of a new result like `a`: f32 or bf16."""
@@ -995,6 +998,11 @@ def rms_norm(x: "Array", weight=None, residual=None, eps: float = 1e-6, offset: 
     """total = x + residual and out = total / sqrt(mean(total ** 2) + eps) * (offset + weight) over the last axis (gr_rms_norm); returns
     (out, total, scales), x for total where there is no residual.  What is not given is new; total=False: not wanted, returned as None.  An e4m3 out, or
     eight=True, is the result in 8 bits with scales of rows, as ``dot_scaled`` takes it; else scales is None."""
+    if _fastbind is not None and out is not None and (scales is not None or not eight) and (residual is None or total is not None):
+        st = _fastbind.rms_norm(x, residual, weight, None if total is False else total, out, scales, eps, offset)
+        if st == 0:
+            return out, x if residual is None else None if total is False else total, scales
+        # (what is wrong, or an 8-bit result whose scales are to be new: neither has run)
     ctx = _context_of(x)
     hx, hr, hw = _tensor(ctx, x), _optional(ctx, residual), _optional(ctx, weight)
     if out is None or (total is None and residual is not None) or scales is None:
@@ -1019,6 +1027,10 @@ def rms_norm(x: "Array", weight=None, residual=None, eps: float = 1e-6, offset: 
 def rms_norm_grad(dout: "Array", total: "Array", weight=None, dtotal=None, eps: float = 1e-6, offset: float = 0.0, dx=None, dweight=None):
     """The gradients of x (and of residual alike) and of weight (gr_rms_norm_grad) for the gradients of out and, by other ways, of total; returns
     (dx, dweight).  dweight=False, or no weight: not wanted, returned as None."""
+    if _fastbind is not None and dx is not None and (weight is None or dweight is not None):
+        st = _fastbind.rms_norm_grad(dout, total, weight, dtotal, dx, None if dweight is False else dweight, eps, offset)
+        if st == 0:
+            return dx, None if dweight is False else dweight
     ctx = _context_of(total)
     ht, hd, hw, hm = _tensor(ctx, total), _tensor(ctx, dout), _optional(ctx, weight), _optional(ctx, dtotal)
     if dx is None:
@@ -1036,6 +1048,8 @@ def rms_norm_grad(dout: "Array", total: "Array", weight=None, dtotal=None, eps: 
 def quantize(x: "Array", blocks: bool = False, transposed: bool = False, out=None, scales=None):
     """x (M, K) in 8 bits (gr_quantize); returns (out, scales).  128 neighbours of a row share a scale, or with blocks=True 128 x 128 values;
     transposed=True: the same of x.T."""
+    if _fastbind is not None and out is not None and scales is not None and _fastbind.quantize(x, out, scales, blocks, transposed) == 0:
+        return out, scales
     ctx = _context_of(x)
     hx = _tensor(ctx, x)
     if out is None or scales is None:
@@ -1056,6 +1070,8 @@ def quantize(x: "Array", blocks: bool = False, transposed: bool = False, out=Non
 def dot_scaled(a: "Array", a_scales: "Array", b: "Array", b_scales: "Array", out=None, dtype: int = GR_BF16):
     """a b.T (gr_dot_scaled) of the values that a (M, K) and b (N, K), e4m3, stand for; a_scales of rows, b_scales of rows or of blocks.  A new out is
     of `dtype`, GR_BF16 or GR_F32."""
+    if _fastbind is not None and out is not None and _fastbind.dot_scaled(a, a_scales, b, b_scales, out) == 0:
+        return out
     ctx = _context_of(a)
     h = [_tensor(ctx, t) for t in (a, a_scales, b, b_scales)]
     if out is None:

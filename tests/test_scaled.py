@@ -223,6 +223,41 @@ def test_what_python_is_given_wrong_is_said_so(dry):  # noqa: F811
         refused("GR_ERR_NODEVICE", call)                                  # no memory for new results
 
 
+def test_both_routes_of_the_binding(dry, monkeypatch):  # noqa: F811
+    """The C type's route and the longer one make the same launches and refuse the same calls."""
+    s = Specs(dry)
+    x, res, out, total, w = (s((6, 200)) for _ in range(5))
+    w, q, sc, dw = s((200,)), s((6, 200), gr.GR_E4M3), s((6, 2)), s((200,))
+    b, sb, y = s((70, 200), gr.GR_E4M3), s((70, 2)), s((6, 70))
+    calls = [(lambda: gr.rms_norm(x, w, res, out=out, total=total), None), (lambda: gr.rms_norm(x, w, res, out=out, total=False), None), (lambda: gr.rms_norm(x, out=q, scales=sc), None),
+             (lambda: gr.rms_norm(x, w, out=out, eps=1), None), (lambda: gr.rms_norm(x, w, out=out, eps=0.0), "GR_ERR_ARG"), (lambda: gr.rms_norm(x, w, out=q), "GR_ERR_NODEVICE"),
+             (lambda: gr.rms_norm(x, w, res, out=out), "GR_ERR_NODEVICE"), (lambda: gr.rms_norm_grad(x, res, w, dx=out, dweight=dw), None),
+             (lambda: gr.rms_norm_grad(x, res, w, dx=out, dweight=False), None), (lambda: gr.rms_norm_grad(x, res, w, dx=out, dweight=sc), "GR_ERR_SHAPE"),
+             (lambda: gr.quantize(x, out=q, scales=sc), None), (lambda: gr.quantize(x, blocks=1, out=q, scales=s((1, 2))), None), (lambda: gr.quantize(x, blocks=True, out=q, scales=sc), "GR_ERR_SHAPE"),
+             (lambda: gr.dot_scaled(q, sc, b, sb, out=y), None), (lambda: gr.dot_scaled(q, sc, b, sc, out=y), "GR_ERR_SHAPE")]
+    seen = []
+    for fast in (gr._fastbind, None):
+        monkeypatch.setattr(gr, "_fastbind", fast)
+        got = []
+        for call, code in calls:
+            n = dry.stats()["kernel_launches"]
+            if code:
+                refused(code, call)
+            else:
+                call()
+            got.append(dry.stats()["kernel_launches"] - n)
+        seen.append(got)
+    assert seen[0] == seen[1] and all((n > 0) == (code is None) for n, (_, code) in zip(seen[0], calls))
+    monkeypatch.undo()
+    other = gr.Context(device=-1)
+    o = Specs(other)((6, 200))
+    with pytest.raises(ValueError):
+        gr.rms_norm(x, out=o)
+    other.close()
+    with pytest.raises((RuntimeError, gr.GrError)):
+        gr.rms_norm(o, out=o)                                             # a context that is closed
+
+
 def test_reference_gradient_against_differences():
     g = torch.Generator().manual_seed(5)
     x, dout, dtotal = (torch.randn(4, 7, generator=g, dtype=torch.float64) for _ in range(3))
