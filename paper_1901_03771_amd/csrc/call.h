@@ -206,10 +206,21 @@ inline bool resolved(gr_ctx* ctx, gr_array a) {
 
 inline size_t rounded(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// The context's device is the current one while a call runs, whichever the caller's is.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(int device) {
+    if (device < 0) return;
+    if (hipGetDevice(&before) != hipSuccess || before == device || hipSetDevice(device) != hipSuccess) before = -1;
+  }
+  ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
 // No exception leaves the C ABI.
 template <class F>
 gr_status guarded(gr_ctx* ctx, F&& f) {
   if (!ctx) return GR_ERR_ARG;
+  const OnDevice on(ctx->device);
   try {
     return f();
   } catch (const std::bad_alloc&) {

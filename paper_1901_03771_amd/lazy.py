@@ -973,8 +973,8 @@ def rotary(x: "Array", frequencies, positions=0, interleaved: bool = False, inve
 
 
 # ---- norms, 8-bit tensors with scales and their products (include/grumpy_hip_scaled.h) ------------------------------------
-# Calls whose results are all given go through the C type first: it takes what is ordinary, and whatever it does not take, or the library refuses (before anything
-# runs), goes the longer way, which raises what there is to raise.
+# Calls whose results are all given go through the C type first: it takes what is ordinary, and whatever it does not take goes the longer way, which raises what there is
+# to raise.
 
 def _float_code(a: "Array") -> int:
     """The element type of a new result like `a`: f32 or bf16."""
@@ -1002,7 +1002,7 @@ def rms_norm(x: "Array", weight=None, residual=None, eps: float = 1e-6, offset: 
         st = _fastbind.rms_norm(x, residual, weight, None if total is False else total, out, scales, eps, offset)
         if st == 0:
             return out, x if residual is None else None if total is False else total, scales
-        # (what is wrong, or an 8-bit result whose scales are to be new: neither has run)
+        # (what is wrong, or an 8-bit result whose scales are to be new: neither has run, the call is a single launch)
     ctx = _context_of(x)
     hx, hr, hw = _tensor(ctx, x), _optional(ctx, residual), _optional(ctx, weight)
     if out is None or (total is None and residual is not None) or scales is None:
@@ -1029,7 +1029,9 @@ def rms_norm_grad(dout: "Array", total: "Array", weight=None, dtotal=None, eps: 
     (dx, dweight).  dweight=False, or no weight: not wanted, returned as None."""
     if _fastbind is not None and dx is not None and (weight is None or dweight is not None):
         st = _fastbind.rms_norm_grad(dout, total, weight, dtotal, dx, None if dweight is False else dweight, eps, offset)
-        if st == 0:
+        if st is not None:
+            if st:
+                _context_of(total).check(st)
             return dx, None if dweight is False else dweight
     ctx = _context_of(total)
     ht, hd, hw, hm = _tensor(ctx, total), _tensor(ctx, dout), _optional(ctx, weight), _optional(ctx, dtotal)
@@ -1048,8 +1050,12 @@ def rms_norm_grad(dout: "Array", total: "Array", weight=None, dtotal=None, eps: 
 def quantize(x: "Array", blocks: bool = False, transposed: bool = False, out=None, scales=None):
     """x (M, K) in 8 bits (gr_quantize); returns (out, scales).  128 neighbours of a row share a scale, or with blocks=True 128 x 128 values;
     transposed=True: the same of x.T."""
-    if _fastbind is not None and out is not None and scales is not None and _fastbind.quantize(x, out, scales, blocks, transposed) == 0:
-        return out, scales
+    if _fastbind is not None and out is not None and scales is not None:
+        st = _fastbind.quantize(x, out, scales, blocks, transposed)
+        if st is not None:
+            if st:
+                _context_of(x).check(st)
+            return out, scales
     ctx = _context_of(x)
     hx = _tensor(ctx, x)
     if out is None or scales is None:
@@ -1070,8 +1076,12 @@ def quantize(x: "Array", blocks: bool = False, transposed: bool = False, out=Non
 def dot_scaled(a: "Array", a_scales: "Array", b: "Array", b_scales: "Array", out=None, dtype: int = GR_BF16):
     """a b.T (gr_dot_scaled) of the values that a (M, K) and b (N, K), e4m3, stand for; a_scales of rows, b_scales of rows or of blocks.  A new out is
     of `dtype`, GR_BF16 or GR_F32."""
-    if _fastbind is not None and out is not None and _fastbind.dot_scaled(a, a_scales, b, b_scales, out) == 0:
-        return out
+    if _fastbind is not None and out is not None:
+        st = _fastbind.dot_scaled(a, a_scales, b, b_scales, out)
+        if st is not None:
+            if st:
+                _context_of(a).check(st)
+            return out
     ctx = _context_of(a)
     h = [_tensor(ctx, t) for t in (a, a_scales, b, b_scales)]
     if out is None:
