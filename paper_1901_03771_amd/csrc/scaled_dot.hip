@@ -8,6 +8,9 @@
 // places below its leading one: sums of normal numbers are off by 1.5e-5 of themselves, at most by 7 x 2^-13 of the sum of their sizes.  A result rounded to bfloat16 does not show it (half a
 // step of it is 2^-8; 1.7e-3 from binary64 with and without).  For a float32 result the operands become bfloat16 on their way from LDS, which holds e4m3 exactly, and four products of 32 places
 // each are summed in float32 proper: 2^-24, at twice the cycles.
+//
+// Large products are bound by the card's power (8192^3: 445 to 465 us, 2.4 PFLOP/s, the matrix cores busy 62 % of the cycles at 1.8 GHz; of zeros 344 us), those into float32 by vector
+// instructions beside the products (4096 x 6144 x 16384 with factors of rows: 750 us, 1.1 PFLOP/s, vector units 69 %, matrix cores 53 %), few rows by reading b.
 #include <type_traits>
 
 #include "scaled_kernels.h"
@@ -159,19 +162,20 @@ struct Flight {
   }
 };
 
-// A tile of TM rows of a by TN rows of b, waves WM x WN.  Two stages of a block each in LDS: while one is multiplied, the other is under way, through registers (any strides) or straight
-// into LDS (DIRECT).
-template <int TM, int TN, int WM, int WN, bool DIRECT, bool BLOCKS, class OUT>
+// A tile of TM rows of a by TN rows of b, waves WM x WN.  Stages of a block each in LDS: while one is multiplied, the others are under way, through registers (any strides) or straight
+// into LDS (DIRECT).  Two of them, or three for tiles of 64 rows, which have few products to hide a load behind (512 x 4096 x 4096: 15.7 us, with two 23, with four, whose LDS leaves a compute unit
+// one workgroup, 18.7; of 128 x 128, 26 with two and 28 with three).
+template <int TM, int TN, int WM, int WN, bool DIRECT, int STAGES, bool BLOCKS, class OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Dot d) {
   constexpr int THREADS = WM * WN * 64, I = TN / WN / 16, J = TM / WM / 16, NB = TN / BLOCK;
   constexpr int CA = TM * 8 / THREADS, CB = TN * 8 / THREADS;               // chunks of a thread
   static_assert(CA * THREADS == TM * 8 && CB * THREADS == TN * 8, "whole chunks for every thread");
   constexpr int STAGE = (TM + TN) * 128;
-  // factors of a stage: of the rows of a, for each block of rows of b (BLOCKS) or apart from those of the rows of b
-  constexpr int USED = BLOCKS ? NB * TM : TM + TN, FACTORS = USED > THREADS ? USED : THREADS;
-  __shared__ __attribute__((aligned(1024))) char memory[2 * (STAGE + FACTORS * 4)];
+  // factors of a stage: of the rows of a, for each block of rows of b (BLOCKS, two stages) or apart from those of b
+  constexpr int USED = !BLOCKS ? TM + TN : STAGES > 2 ? TM + NB : NB * TM, FACTORS = USED > THREADS ? USED : THREADS;
+  __shared__ __attribute__((aligned(1024))) char memory[STAGES * (STAGE + FACTORS * 4)];
   GR_LDS char* const lds = (GR_LDS char*)memory;
-  GR_LDS float* const factors = (GR_LDS float*)(lds + 2 * STAGE);
+  GR_LDS float* const factors = (GR_LDS float*)(lds + STAGES * STAGE);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 15, g = lane >> 4;
   const int wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
   const Place p = place_of(d);
@@ -209,8 +213,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   // The factors of a block, a thread each.  (Rows behind the last have the last one's: their results go nowhere.  Threads without a factor of their own write one that
   // nothing reads: between a product and its use stands no branch, where the compiler has been seen to count too few wait states.)
   static_assert(FACTORS == THREADS && TM % 64 == 0, "a factor a thread, of the same operand across a wave");
-  const bool of_a = BLOCKS || tid < TM;
-  const float* const row_factor = of_a ? d.sa + (int64_t)(m0 + min(tid % TM, rows_a - 1)) * d.sa_m : d.sb + (int64_t)(n0 + min(tid - TM, rows_b - 1)) * d.sb_n;
+  constexpr bool DEEP = STAGES > 2;
+  static_assert(STAGES == 2 || (STAGES == 3 && DIRECT), "tiles that pass through registers have two stages");
+  const bool of_a = (BLOCKS && !DEEP) || tid < TM;
+  const int64_t of_b = BLOCKS ? min(n0 / BLOCK + tid - TM, (d.N - 1) / BLOCK) : n0 + min(tid - TM, rows_b - 1);
+  const float* const row_factor = of_a ? d.sa + (int64_t)(m0 + min(tid % TM, rows_a - 1)) * d.sa_m : d.sb + of_b * d.sb_n;
   const int64_t row_step = of_a ? d.sa_k : d.sb_k;
   const float* const block_factor = d.sb + (int64_t)min(n0 / BLOCK + __builtin_amdgcn_readfirstlane(tid / TM), (d.N - 1) / BLOCK) * d.sb_n;
   float factor = 0.0f;
@@ -219,8 +226,17 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     if constexpr (BLOCKS) factor *= ((const __attribute__((address_space(4))) float*)block_factor)[min(kb, last - 1) * d.sb_k];
     factors[stage * FACTORS + tid] = factor;
   };
+  // Three stages: factors go straight into LDS like the tiles, those of a's rows and those of b apart, and a wait leaves the tile after the next under way.
+  const uint32_t factors0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(factors + (tid & ~63)));
+  auto send_factors = [&](int kb, int stage) GR_INLINE {
+    const float* const from = row_factor + min(kb, last - 1) * row_step;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tglobal_load_lds_dword %0, off" : : "v"(from), "s"(factors0 + stage * FACTORS * 4) : "memory", "m0");
+  };
+  constexpr int UNDER_WAY = (STAGES - 2) * (CA + CB + 1);   // loads of the tile after the next, and of its factors
+  auto arrive_but_one = [&]() GR_INLINE { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(UNDER_WAY) : "memory"); };
 
-  // Steps that operands of b are read ahead: LDS is nearly as busy as the matrix cores.  (With factors of their own for b's rows the registers hold one, of tiles of 256 x 256.)
+  // Steps that operands of b are read ahead: a read from LDS takes longer than one step's products (8192^3: 465 us with one, 445 with two).  (With factors of their own for b's rows the
+  // registers hold one, of tiles of 256 x 256.)
   constexpr int AHEAD = I == 8 && !BLOCKS ? 1 : 2, RING = 2 * AHEAD;
   constexpr int EARLY = AHEAD + I / 8;   // steps over which a tile is sent for
   constexpr bool PROPER = sizeof(OUT) == 4;
@@ -235,11 +251,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   static_assert(I % RING == 0 && EARLY <= I - AHEAD, "operands of b go round their registers, and a tile has time to come");
   i32x8 raw[J], y[RING];
   f32x4 t[BLOCKS ? 1 : RING];
-  float s[2][J];
+  float s[STAGES][J];
   auto read_a = [&](int j, auto parity) GR_INLINE {
     constexpr int P = decltype(parity)::value;
     raw[j] = operand(lds + P * STAGE, wm + 16 * j + l, g);
-    s[P][j] = factors[P * FACTORS + (BLOCKS ? wn / BLOCK * TM : 0) + wm + 16 * j + l];
+    s[P][j] = factors[P * FACTORS + (BLOCKS && !DEEP ? wn / BLOCK * TM : 0) + wm + 16 * j + l];
+    if constexpr (BLOCKS && DEEP) s[P][j] *= factors[P * FACTORS + TM + wn / BLOCK];
   };
   auto read_b = [&](int i, auto parity) GR_INLINE {
     constexpr int P = decltype(parity)::value;
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   };
   auto block = [&](int kb, auto parity) GR_INLINE {
     constexpr int P = decltype(parity)::value;
-    constexpr std::integral_constant<int, P ^ 1> other;
+    constexpr std::integral_constant<int, (P + 1) % STAGES> other;
     Operand<PROPER> x[J];
     f32x4 z[J], before = {1.0f, 1.0f, 1.0f, 1.0f};
 #pragma unroll
@@ -262,9 +279,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     for (int i = 0; i <= I; ++i) {
       if (i == I - AHEAD) {
         // All operands of this block have been read: everybody waits for the next one's tiles, and the one after it takes this one's place.
-        settle_factors(kb + 1, P ^ 1);
-        arrive();
-        fetch_factors(kb + 2);
+        if constexpr (DEEP) {
+          arrive_but_one();
+          send_factors(kb + STAGES, P);
+        } else {
+          settle_factors(kb + 1, P ^ 1);
+          arrive();
+          fetch_factors(kb + 2);
+        }
       }
       Operand<PROPER> o;
       if (i < I) o.set(y[i % RING]);
@@ -293,8 +315,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
           if (slot < SLOTS)
 #pragma unroll
             for (int c = slot * (CA + CB) / SLOTS; c < (slot + 1) * (CA + CB) / SLOTS; ++c) {
-              if (i >= I - AHEAD) send(c, kb + 2, P);
-              else send(c, kb + 1, P ^ 1);
+              if (i >= I - AHEAD) send(c, kb + STAGES, P);
+              else send(c, kb + STAGES - 1, (P + STAGES - 1) % STAGES);
             }
         }
         if (i == I - 1) read_a(j, other);
@@ -310,25 +332,36 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     }
   };
   if (first < last) {
-    fetch_factors(first);
-    if constexpr (DIRECT) {
+    constexpr int SENT = AHEAD * J * (CA + CB) / (EARLY * J);   // of a tile before its first block begins
+    if constexpr (DEEP) {
 #pragma unroll
-      for (int c = 0; c < CA + CB; ++c) send(c, first, 0);
+      for (int t = 0; t < STAGES - 1; ++t) {
+        send_factors(first + t, t);
+#pragma unroll
+        for (int c = 0; c < CA + CB; ++c) send(c, first + t, t);
+      }
+      arrive_but_one();
+      send_factors(first + STAGES - 1, STAGES - 1);
     } else {
-      fetch(first);
-      settle(first, 0);
+      fetch_factors(first);
+      if constexpr (DIRECT) {
+#pragma unroll
+        for (int c = 0; c < CA + CB; ++c) send(c, first, 0);
+      } else {
+        fetch(first);
+        settle(first, 0);
+      }
+      settle_factors(first, 0);
+      arrive();
+      fetch_factors(first + 1);
     }
-    settle_factors(first, 0);
-    arrive();
-    fetch_factors(first + 1);
     if constexpr (DIRECT) {
 #pragma unroll
-      for (int c = 0; c < AHEAD * J * (CA + CB) / (EARLY * J); ++c) send(c, first + 1, 1);
+      for (int c = 0; c < SENT; ++c) send(c, first + STAGES - 1, STAGES - 1);
     } else {
       fetch(first + 1);
     }
     constexpr std::integral_constant<int, 0> even;
-    constexpr std::integral_constant<int, 1> odd;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read_b(i, even);
 #pragma unroll
@@ -336,8 +369,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     for (int kb = first;;) {
       block(kb, even);
       if (++kb >= last) break;
-      block(kb, odd);
+      block(kb, std::integral_constant<int, 1>());
       if (++kb >= last) break;
+      if constexpr (DEEP) {
+        block(kb, std::integral_constant<int, 2>());
+        if (++kb >= last) break;
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (loads into LDS that nothing takes end before the workgroup does)
   }
@@ -356,7 +393,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 }
 
 // Few rows of a (16 MT at most): b is what is read, at the rate of the memory.  A workgroup has 32 rows of b, its eight waves take blocks of 128 places in turn, U of them in
-// flight at once, straight from memory to the registers that the matrix cores read; the waves' sums are added in order.
+// flight at once, straight from memory to the registers that the matrix cores read; the waves' sums are added in order.  (4 rows by 14336 x 4096: 14 us, 4.2 TB/s.)
 template <bool WORDS> struct Chunk;
 template <> struct Chunk<false> {
   i32x4 v;
@@ -490,9 +527,9 @@ __global__ __launch_bounds__(256) void gr_dot_scaled_join_kernel(const Dot d) {
   store4<OUT>((OUT*)d.out + m * d.out_s, n, d.N, z);
 }
 
-template <int TM, int TN, int WM, int WN, bool DIRECT, bool BLOCKS, class OUT>
+template <int TM, int TN, int WM, int WN, bool DIRECT, int STAGES, bool BLOCKS, class OUT>
 static hipError_t launch(const Dot& d, hipStream_t stream) {
-  gr_dot_scaled_kernel<TM, TN, WM, WN, DIRECT, BLOCKS, OUT><<<dim3((unsigned)(d.mt * d.nt * d.splits)), dim3(WM * WN * 64), 0, stream>>>(d);
+  gr_dot_scaled_kernel<TM, TN, WM, WN, DIRECT, STAGES, BLOCKS, OUT><<<dim3((unsigned)(d.mt * d.nt * d.splits)), dim3(WM * WN * 64), 0, stream>>>(d);
   return hipGetLastError();
 }
 
@@ -506,11 +543,11 @@ template <bool BLOCKS, class OUT>
 static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
   if (form == DOT_FEW) return d.M <= 16 ? launch_few<1, false, BLOCKS, OUT>(d, stream) : launch_few<2, false, BLOCKS, OUT>(d, stream);
   if (form == DOT_FEW_WORDS) return d.M <= 16 ? launch_few<1, true, BLOCKS, OUT>(d, stream) : launch_few<2, true, BLOCKS, OUT>(d, stream);
-  if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, BLOCKS, OUT>(d, stream);
-  if (form == DOT_LOW) return launch<64, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
-  if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, BLOCKS, OUT>(d, stream);
-  if (form == DOT_STAGED_LOW) return launch<64, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
-  if constexpr (sizeof(OUT) == 2) if (form == DOT_STAGED) return launch<128, 128, 2, 2, false, BLOCKS, OUT>(d, stream);
+  if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, 2, BLOCKS, OUT>(d, stream);
+  if (form == DOT_LOW) return launch<64, 128, 2, 2, true, 3, BLOCKS, OUT>(d, stream);
+  if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, 2, BLOCKS, OUT>(d, stream);
+  if (form == DOT_STAGED_LOW) return launch<64, 128, 2, 2, false, 2, BLOCKS, OUT>(d, stream);
+  if constexpr (sizeof(OUT) == 2) if (form == DOT_STAGED) return launch<128, 128, 2, 2, false, 2, BLOCKS, OUT>(d, stream);
   return hipErrorInvalidValue;
 }
 

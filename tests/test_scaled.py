@@ -537,6 +537,25 @@ def test_product_of_whole_numbers(ctx, out, blocks, m, n, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out", [F32, BF16], ids=NAMES.get)
+@pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
+@pytest.mark.parametrize("k", [16, 128, 144, 256, 272, 384, 400, 512, 640, 784, 896, 1168])
+def test_product_of_few_blocks(ctx, out, blocks, k):
+    """Tiles that are sent for ahead of their use, where there are fewer blocks than are under way, as many, and some more; NaN behind rows and operands."""
+    m, n = 70, 133
+    a, sa = whole(k, m, k, 1)
+    b, sb = whole(k + 1, n, k, 128 if blocks else 1)
+    want = plain.product(a, sa, b, sb)[0].to(out)
+    wide = [torch.full((t.shape[0] + 64, k + 48), 0x7f, dtype=torch.uint8, device="cuda").view(E4M3) for t in (a, b)]
+    scales = [torch.full((t.shape[0] + 64, t.shape[1] + 4), float("nan"), device="cuda") for t in (sa, sb)]
+    for w, t in zip(wide + scales, (a, b, sa, sb)):
+        w[:t.shape[0], :t.shape[1]] = t.cuda()
+    to = Guarded((m, n), out)
+    gr.dot_scaled(*(ctx.array(w[:t.shape[0], :t.shape[1]]) for w, t in zip((wide[0], scales[0], wide[1], scales[1]), (a, sa, b, sb))), out=ctx.array(to.t))
+    assert torch.equal(to.t.cpu(), want) and to.untouched()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 def test_product(ctx, blocks, m, n, k):
@@ -707,6 +726,9 @@ def test_captured_calls_replay(ctx):
         total, dx = torch.empty_like(x), torch.empty_like(x)
         q, s, dw = torch.empty(rows, D, device="cuda", dtype=E4M3), torch.empty(rows, D // 128, device="cuda"), torch.empty(D, device="cuda")
         y, qt, st = torch.empty(rows, N, device="cuda", dtype=BF16), torch.empty(D, rows, device="cuda", dtype=E4M3), torch.empty(D, 1, device="cuda")
+        # (a product of many blocks and few tiles is split, and its parts are temporary memory)
+        (p, sp), (v, sv) = ([t.torch() for t in gr.quantize(A(normal(3 + i, n, 16384).cuda()), blocks=i == 1)] for i, n in enumerate((rows, N)))
+        z = torch.empty(rows, N, device="cuda")
 
         def fill(seed):
             for i, t in enumerate((x, res, dy)):
@@ -715,11 +737,12 @@ def test_captured_calls_replay(ctx):
         def step():
             gr.rms_norm(A(x), A(w), A(res), out=A(q), total=A(total), scales=A(s))
             gr.dot_scaled(A(q), A(s), A(b), A(sb), out=A(y))
+            gr.dot_scaled(A(p), A(sp), A(v), A(sv), out=A(z))
             gr.rms_norm_grad(A(dy), A(total), A(w), dx=A(dx), dweight=A(dw))
             gr.quantize(A(dx), transposed=True, out=A(qt), scales=A(st))
 
         def results():
-            return [t.float().clone() for t in (total, q, s, y, dx, dw, qt, st)]
+            return [t.float().clone() for t in (total, q, s, y, z, dx, dw, qt, st)]
 
         fill(10)
         step()
@@ -731,7 +754,7 @@ def test_captured_calls_replay(ctx):
             fill(seed)
             step()
             want = results()
-            for t in (total, q, s, y, dx, dw, qt, st):
+            for t in (total, q, s, y, z, dx, dw, qt, st):
                 t.view(torch.uint8).zero_()
             graph.replay()
             stream.synchronize()
@@ -745,7 +768,7 @@ def test_captured_calls_replay(ctx):
         codes = []
         with torch.cuda.graph(graph, stream=stream):
             torch.zeros(1, device="cuda").add_(1)
-            for call in (lambda: gr.rms_norm_grad(F(dy), F(total), F(w), dx=F(dx), dweight=F(dw)), lambda: gr.dot_scaled(F(q), F(s), F(b), F(sb), out=F(y))):
+            for call in (lambda: gr.rms_norm_grad(F(dy), F(total), F(w), dx=F(dx), dweight=F(dw)), lambda: gr.dot_scaled(F(p), F(sp), F(v), F(sv), out=F(z))):
                 try:
                     call()
                     codes.append("none")
