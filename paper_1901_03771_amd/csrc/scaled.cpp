@@ -252,8 +252,8 @@ static int choose(Dot* d, int out) {
     d->nt = (int)((N + tn - 1) / tn);
     return (int64_t)d->mt * d->nt;
   };
-  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 27 us, by 4096 x 4088 29,
-  // by 4096 x 4095 34).
+  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 18.5 us, by 4096 x 4088 25,
+  // by 4096 x 4095 29).
   auto direct = [&](const uint8_t* p, int64_t rows, int64_t s) { return (uintptr_t)p % 16 == 0 && (rows == 1 || (s % 16 == 0 && s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
   const bool straight = K % 16 == 0 && direct(d->a, M, d->a_s) && direct(d->b, N, d->b_s);
   // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy; a split of fewer than 32 blocks is over before it would pay.  (16 rows by 4096 x 4096: 8.3 us, tiles of
@@ -265,11 +265,12 @@ static int choose(Dot* d, int out) {
   // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (one workgroup a compute unit; straight, bf16 results), whichever takes least by what was measured (us): a
   // start, the blocks of a workgroup alone and what its neighbours add, rounds of them, and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 16 with 256 tiles of 64
   // rows, 26 with 128 of 128 rows, 23 with those in two splits; 1024 x 8192 x 4096: 51 and 42; 64 x 4096 x 14336: 39, 25, 17, 17 with 1, 2, 4, 8; 192 x 4096 x 14336: 41, 27, 25, 28 with 1, 2, 5,
-  // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77.)
+  // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77; through registers,
+  // 512 x 4096 x 4095: 28 and 39, 1024 x 4096 x 4095: 46 and 40.)
   const bool proper = out == GR_F32;
   struct Form { int which; int64_t high, wide; double start, alone, more; };
-  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : 0.34, proper ? 0.45 : 0.33} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.62 : 1.16, proper ? 0.81 : 0.58};
-  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : 0.65, proper ? 0.72 : 0.54} : Form{DOT_STAGED, 128, 128, 5.0, 1.30, 1.08};
+  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : 0.34, proper ? 0.45 : 0.33} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.00 : 0.70, 0.62};
+  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : 0.65, proper ? 0.72 : 0.54} : Form{DOT_STAGED, 128, 128, 5.0, 1.05, 0.77};
   const Form large = {DOT_LARGE, 256, 256, 6.0, 0.60, 1.15};
   const Form* best = nullptr;
   double least = 0.0;

@@ -50,9 +50,10 @@ static __device__ __forceinline__ f32x4 block_product(const Operand<true>& a, co
 
 // 16 bytes k .. k + 15 of a row of K bytes at any address, zeros behind its end, in two steps without a branch between loads: what is loaded ends with the row, and is moved
 // to its place once it is needed.
+template <bool LONG = false>
 static __device__ __forceinline__ i32x4 bytes_until(const uint8_t* row, int k, int K) {
   typedef int anywhere __attribute__((ext_vector_type(4), aligned(1)));
-  if (K >= 16) return *(const anywhere*)(row + min(k, K - 16));
+  if (LONG || K >= 16) return *(const __attribute__((address_space(1))) anywhere*)(uintptr_t)(row + min(k, K - 16));
   i32x4 v = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < 15; ++e) v[e / 4] |= (e < K ? (int)row[min(e, K - 1)] : 0) << (8 * (e % 4));
@@ -114,6 +115,9 @@ static __device__ __forceinline__ void store4(T* row, int n, int N, f32x4 v) {
     for (int e = 0; e < 3; ++e) if (n + e < N) row[n + e] = (T)v[e];
   }
 }
+
+// The same where only LDS is waited for: what is under way to registers stays so.
+static __device__ __forceinline__ void arrive_in_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Which tile and which split a workgroup takes.  Workgroups go round the eight XCDs in turn, each with an L2 of its own: an XCD takes neighbouring
 // tiles, eight rows of them at a time.
@@ -184,7 +188,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   const uint8_t* const a = d.a + (int64_t)m0 * d.a_s;
   const uint8_t* const b = d.b + (int64_t)n0 * d.b_s;
 
-  i32x4 staged[DIRECT ? 1 : CA + CB];
+  // blocks on their way through registers at once: as many as there are registers for (512 x 4096 x 4095: 29 us with two, 37 with one)
+  constexpr int SETS = TM == 64 ? 2 : 1;
+  i32x4 staged[SETS][DIRECT ? 1 : CA + CB];
   const Flight<TM, THREADS> fa(a, d.a_s, rows_a, d.K, tid, lds);
   const Flight<TN, THREADS> fb(b, d.b_s, rows_b, d.K, tid, lds + TM * 128);
   // Chunk c of a tile on its way into LDS.
@@ -192,22 +198,30 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
     if (c < CA) fa.go(c, fa.place(kb, d.K), stage * STAGE);
     else fb.go(c - CA, fb.place(kb, d.K), stage * STAGE);
   };
-  // (a row behind the last is read as the last: its results go nowhere)
-  auto fetch = [&](int kb) GR_INLINE {
+  // (a row behind the last is read as the last: its results go nowhere; a block behind the last as the last, which nothing takes.  MORE: of more than one, so that rows have 16 bytes, or none
+  // of them is taken and it reads the kernel's arguments: no branch makes the loads before it wait.)
+  const uint8_t* const some = (const uint8_t*)__builtin_amdgcn_kernarg_segment_ptr();
+  auto fetch = [&](int kb, int set, auto more) GR_INLINE {
+    constexpr bool MORE = decltype(more)::value;
+    if (MORE) kb = min(kb, last - 1);
+    const bool there = !MORE || d.K >= 16;
+    const uint8_t *const from_a = there ? a : some, *const from_b = there ? b : some;
+    const int64_t step_a = there ? d.a_s : 0, step_b = there ? d.b_s : 0;
+    const int K = there ? d.K : 16;
 #pragma unroll
-    for (int c = 0; c < CA; ++c) staged[c] = bytes_until(a + min((c * THREADS + tid) / 8, rows_a - 1) * d.a_s, kb * 128 + tid % 8 * 16, d.K);
+    for (int c = 0; c < CA; ++c) staged[set][c] = bytes_until<MORE>(from_a + min((c * THREADS + tid) / 8, rows_a - 1) * step_a, kb * 128 + tid % 8 * 16, K);
 #pragma unroll
-    for (int c = 0; c < CB; ++c) staged[CA + c] = bytes_until(b + min((c * THREADS + tid) / 8, rows_b - 1) * d.b_s, kb * 128 + tid % 8 * 16, d.K);
+    for (int c = 0; c < CB; ++c) staged[set][CA + c] = bytes_until<MORE>(from_b + min((c * THREADS + tid) / 8, rows_b - 1) * step_b, kb * 128 + tid % 8 * 16, K);
   };
-  auto settle = [&](int kb, int stage) GR_INLINE {
+  auto settle = [&](int kb, int stage, int set) GR_INLINE {
     if (kb * 128 + 128 > d.K) {
 #pragma unroll
-      for (int c = 0; c < CA + CB; ++c) staged[c] = in_place(staged[c], kb * 128 + tid % 8 * 16, d.K);
+      for (int c = 0; c < CA + CB; ++c) staged[set][c] = in_place(staged[set][c], kb * 128 + tid % 8 * 16, d.K);
     }
 #pragma unroll
     for (int c = 0; c < CA + CB; ++c) {
       const int i = (c < CA ? c : c - CA) * THREADS + tid, r = i / 8;
-      *(GR_LDS i32x4*)(lds + stage * STAGE + (c < CA ? 0 : TM * 128) + r * 128 + ((i % 8 ^ twist(r)) << 4)) = staged[c];
+      *(GR_LDS i32x4*)(lds + stage * STAGE + (c < CA ? 0 : TM * 128) + r * 128 + ((i % 8 ^ twist(r)) << 4)) = staged[set][c];
     }
   };
   // The factors of a block, a thread each.  (Rows behind the last have the last one's: their results go nowhere.  Threads without a factor of their own write one that
@@ -271,8 +285,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 #pragma unroll
     for (int j = 0; j < J; ++j) x[j].set(raw[j]);
     if constexpr (!DIRECT) {   // (has branches: before the first product)
-      settle(kb + 1, P ^ 1);
-      fetch(kb + 2);
+      settle(kb + 1, P ^ 1, (P ^ 1) % SETS);
+      fetch(kb + 1 + SETS, (P ^ 1) % SETS, std::true_type());
     }
     // Columns 16 at a time: four sums of the step before are added, then the registers take the next product.
 #pragma unroll
@@ -284,7 +298,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
           send_factors(kb + STAGES, P);
         } else {
           settle_factors(kb + 1, P ^ 1);
-          arrive();
+          if constexpr (DIRECT) arrive();
+          else arrive_in_lds();
           fetch_factors(kb + 2);
         }
       }
@@ -348,28 +363,39 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 #pragma unroll
         for (int c = 0; c < CA + CB; ++c) send(c, first, 0);
       } else {
-        fetch(first);
-        settle(first, 0);
+        fetch(first, 0, std::false_type());
+        settle(first, 0, 0);
       }
       settle_factors(first, 0);
       arrive();
+      if constexpr (!DIRECT) {
+#pragma unroll
+        for (int t = 1; t <= SETS; ++t) fetch(first + t, t % SETS, std::true_type());
+      }
       fetch_factors(first + 1);
     }
     if constexpr (DIRECT) {
 #pragma unroll
       for (int c = 0; c < SENT; ++c) send(c, first + STAGES - 1, STAGES - 1);
-    } else {
-      fetch(first + 1);
     }
     constexpr std::integral_constant<int, 0> even;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read_b(i, even);
 #pragma unroll
     for (int j = 0; j < J; ++j) read_a(j, even);
-    for (int kb = first;;) {
+    constexpr std::integral_constant<int, 1> odd;
+    if constexpr (SETS > 1 && !DIRECT) {
+      // (one way out of the loop: with two, the compiler waits for the later set of loads, too)
+      int kb = first;
+      for (; kb + 1 < last; kb += 2) {
+        block(kb, even);
+        block(kb + 1, odd);
+      }
+      if (kb < last) block(kb, even);
+    } else for (int kb = first;;) {
       block(kb, even);
       if (++kb >= last) break;
-      block(kb, std::integral_constant<int, 1>());
+      block(kb, odd);
       if (++kb >= last) break;
       if constexpr (DEEP) {
         block(kb, std::integral_constant<int, 2>());
