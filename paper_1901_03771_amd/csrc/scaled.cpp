@@ -256,10 +256,18 @@ static int choose(Dot* d, int out) {
   // by 4096 x 4095 29).
   auto direct = [&](const uint8_t* p, int64_t rows, int64_t s) { return (uintptr_t)p % 16 == 0 && (rows == 1 || (s % 16 == 0 && s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
   const bool straight = K % 16 == 0 && direct(d->a, M, d->a_s) && direct(d->b, N, d->b_s);
-  // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy; a split of fewer than 32 blocks is over before it would pay.  (16 rows by 4096 x 4096: 8.3 us, tiles of
-  // 64 x 128 9.6; by 4096 x 14336 17.8 and 14.1; 32 rows by 4096 x 14336: 20.8 and 15.0, by 4096 x 4088, through registers, 8.5 and 13.3)
+  // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy.  Rounds of 16 blocks, and a join of splits, take what was measured (us).  (4 rows by 4096 x 4096: 7.5 with one, 8.8
+  // with two splits; by 4096 x 14336 18.7 and 15.0; by 1024 x 8192 10.9, 10.1, 8.4 with 1, 2, 4.  16 rows by 4096 x 4096 8.4, tiles of 64 x 128 9.6; 32 rows by 4096 x 14336: 20.8 and 15.0, by
+  // 4096 x 4088, through registers, 8.5 and 13.3.)
   if (M <= (straight ? 16 : 32)) {
-    d->splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles_of(32, 32), KB / 32));
+    const int64_t most = std::max<int64_t>(1, 256 / tiles_of(32, 32));
+    double least = 0.0;
+    for (int64_t s = 1; s <= most && s <= std::max<int64_t>(1, KB); ++s) {
+      const double us = 1.7 * (double)((KB + 16 * s - 1) / (16 * s)) + (s > 1 ? 2.0 + 0.6 * (double)((s + 7) / 8) : 0.0);
+      if (s > 1 && us >= least) continue;
+      least = us;
+      d->splits = (int)s;
+    }
     return ((uintptr_t)d->a | (uintptr_t)d->b | (uintptr_t)(M > 1 ? d->a_s : 0) | (uintptr_t)(N > 1 ? d->b_s : 0) | (uintptr_t)(K % BLOCK ? K : 0)) % 4 == 0 ? DOT_FEW : DOT_FEW_WORDS;
   }
   // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (one workgroup a compute unit; straight, bf16 results), whichever takes least by what was measured (us): a

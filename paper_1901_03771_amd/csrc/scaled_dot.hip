@@ -419,7 +419,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 }
 
 // Few rows of a (16 MT at most): b is what is read, at the rate of the memory.  A workgroup has 32 rows of b, its eight waves take blocks of 128 places in turn, U of them in
-// flight at once, straight from memory to the registers that the matrix cores read; the waves' sums are added in order.  (4 rows by 14336 x 4096: 14 us, 4.2 TB/s.)
+// flight at once, straight from memory to the registers that the matrix cores read; the waves' sums are added in order.  (4 rows by 14336 x 4096: 13.3 us, 4.4 TB/s; with U = 4, whose registers leave
+// a compute unit one workgroup, 14.3, and by 16384 x 2048 14.1, 8.1 so.)
 template <bool WORDS> struct Chunk;
 template <> struct Chunk<false> {
   i32x4 v;
@@ -435,7 +436,7 @@ template <> struct Chunk<true> {
 template <int MT, bool WORDS, bool BLOCKS, class OUT>
 __global__ __launch_bounds__(512) void gr_dot_scaled_few_kernel(const Dot d) {
   constexpr bool PROPER = sizeof(OUT) == 4;
-  constexpr int WAVES = 8, NT = 2, U = WORDS ? 2 : 4 / MT, PITCH = 16 * NT + 4;
+  constexpr int WAVES = 8, NT = 2, U = 2, PITCH = 16 * NT + 4;
   __shared__ __attribute__((aligned(16))) float part[WAVES][16 * MT][PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 15, g = lane >> 4;
   const int tile = blockIdx.x % d.nt, split = blockIdx.x / d.nt, n0 = tile * 16 * NT;
