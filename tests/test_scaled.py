@@ -508,7 +508,8 @@ def whole(seed, rows, k, high):
 
 
 PRODUCTS = [(1, 1, 1), (1, 128, 128), (1, 300, 1000), (2, 64, 4096), (3, 129, 257), (16, 256, 512), (17, 130, 640), (33, 513, 300), (64, 1024, 1024), (65, 200, 2048), (100, 100, 100),
-            (128, 128, 128), (129, 127, 384), (192, 384, 5120), (255, 257, 1003), (300, 1100, 260), (513, 300, 144), (1000, 777, 400), (256, 2048, 256), (1, 1, 8192), (4, 16, 16384)]
+            (128, 128, 128), (129, 127, 384), (192, 384, 5120), (255, 257, 1003), (300, 1100, 260), (513, 300, 144), (1000, 777, 400), (256, 2048, 256), (1, 1, 8192), (4, 16, 16384),
+            (3, 40, 40000), (32, 33, 12288), (40, 64, 40000)]
 
 
 @pytest.mark.gpu
@@ -516,7 +517,7 @@ PRODUCTS = [(1, 1, 1), (1, 128, 128), (1, 300, 1000), (2, 64, 4096), (3, 129, 25
 @pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 def test_product_of_whole_numbers(ctx, out, blocks, m, n, k):
-    """Every product and sum is exact: results are equal to the last bit, wherever the places, tiles and splits are.  Sums stay below 4 x 4 x 16384 of quarters and more: 2^24 sixteenths."""
+    """Every product and sum is exact: results are equal to the last bit, wherever the places, tiles and splits are.  Sums stay below 4 x 4 x 40000, in sixteenths below 2^24."""
     a, sa = whole(m + k, m, k, 1)
     b, sb = whole(n + k, n, k, 128 if blocks else 1)
     want = plain.product(a, sa, b, sb)[0].to(out)
