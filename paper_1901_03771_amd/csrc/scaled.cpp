@@ -245,7 +245,7 @@ static gr_status quantize_call(gr_ctx* ctx, gr_array x, int blocks, int transpos
 }
 
 // The form of a product, its tiles, and how many splits of the blocks of K there are where tiles are few.
-static int choose(Dot* d, int out) {
+static int choose(Dot* d, int out, bool blocks) {
   const int64_t M = d->M, N = d->N, K = d->K, KB = d->KB;
   auto tiles_of = [&](int64_t tm, int64_t tn) {
     d->mt = (int)((M + tm - 1) / tm);
@@ -262,7 +262,7 @@ static int choose(Dot* d, int out) {
   if (M <= (straight ? 16 : 32)) {
     const int64_t most = std::max<int64_t>(1, 256 / tiles_of(32, 32));
     double least = 0.0;
-    for (int64_t s = 1; s <= most && s <= std::max<int64_t>(1, KB); ++s) {
+    for (int64_t s = 1; s == 1 || (s <= most && 16 * (s - 1) < KB); ++s) {   // (until a round is all)
       const double us = 1.7 * (double)((KB + 16 * s - 1) / (16 * s)) + (s > 1 ? 2.0 + 0.6 * (double)((s + 7) / 8) : 0.0);
       if (s > 1 && us >= least) continue;
       least = us;
@@ -273,13 +273,13 @@ static int choose(Dot* d, int out) {
   // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (one workgroup a compute unit; straight, bf16 results), whichever takes least by what was measured (us): a
   // start, the blocks of a workgroup alone and what its neighbours add, rounds of them, and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 16 with 256 tiles of 64
   // rows, 26 with 128 of 128 rows, 23 with those in two splits; 1024 x 8192 x 4096: 51 and 42; 64 x 4096 x 14336: 39, 25, 17, 17 with 1, 2, 4, 8; 192 x 4096 x 14336: 41, 27, 25, 28 with 1, 2, 5,
-  // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77; through registers,
-  // 512 x 4096 x 4095: 28 and 39, 1024 x 4096 x 4095: 46 and 40.)
+  // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77; with
+  // scales of b's rows 8192^3 674 and 625 with the larger two, 4096 x 6144 x 16384, 384 of the largest, 488 and 586; through registers, 512 x 4096 x 4095: 28 and 39, 1024 x 4096 x 4095: 46 and 40.)
   const bool proper = out == GR_F32;
   struct Form { int which; int64_t high, wide; double start, alone, more; };
-  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : 0.34, proper ? 0.45 : 0.33} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.00 : 0.70, 0.62};
-  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : 0.65, proper ? 0.72 : 0.54} : Form{DOT_STAGED, 128, 128, 5.0, 1.05, 0.77};
-  const Form large = {DOT_LARGE, 256, 256, 6.0, 0.60, 1.15};
+  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : blocks ? 0.34 : 0.42, proper ? 0.45 : blocks ? 0.35 : 0.37} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.00 : 0.70, 0.62};
+  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : blocks ? 0.65 : 0.72, proper ? 0.72 : blocks ? 0.54 : 0.57} : Form{DOT_STAGED, 128, 128, 5.0, 1.05, 0.77};
+  const Form large = {DOT_LARGE, 256, 256, 6.0, blocks ? 0.60 : 1.20, blocks ? 1.15 : 1.20};
   const Form* best = nullptr;
   double least = 0.0;
   for (const Form* f : {&low, &middle, &large}) {
@@ -340,7 +340,7 @@ static gr_status dot_call(gr_ctx* ctx, gr_array a, gr_array a_scales, gr_array b
   d.N = (int)N;
   d.K = (int)K;
   d.KB = (int)KB;
-  const int form = choose(&d, dt);
+  const int form = choose(&d, dt, blocks);
   if (d.splits > 1) {
     char* ws;
     TRY(c.space(rounded((size_t)d.splits * M * N * 4), &ws));
