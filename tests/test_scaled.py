@@ -540,7 +540,7 @@ def test_product_of_whole_numbers(ctx, out, blocks, m, n, k):
 @pytest.mark.gpu
 @pytest.mark.parametrize("out", [F32, BF16], ids=NAMES.get)
 @pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
-@pytest.mark.parametrize("k", [16, 128, 144, 256, 272, 384, 400, 512, 640, 784, 896, 1168])
+@pytest.mark.parametrize("k", [1, 7, 15, 16, 17, 128, 130, 144, 256, 257, 272, 383, 384, 400, 511, 512, 640, 701, 784, 896, 1168])
 def test_product_of_few_blocks(ctx, out, blocks, k):
     """Tiles that are sent for ahead of their use, where there are fewer blocks than are under way, as many, and some more; NaN behind rows and operands."""
     m, n = 70, 133
