@@ -592,10 +592,11 @@ def test_product_with_what_is_no_number(ctx):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m,n,k", [(4100, 3100, 272), (8200, 1700, 144), (2050, 6200, 640), (3001, 4500, 261), (12289, 1300, 128)])
+@pytest.mark.parametrize("m,n,k", [(4100, 3100, 272), (8200, 1700, 144), (2050, 6200, 640), (3001, 4500, 261), (12289, 1300, 128), (4090, 4070, 1040), (4090, 4070, 272),
+                                   (2040, 4000, 1552), (384, 2048, 16384), (1500, 3000, 2061)])
 @pytest.mark.parametrize("blocks", [True, False], ids=["blocks", "rows"])
 def test_large_products_of_whole_numbers(ctx, blocks, m, n, k):
-    """Tiles of 256 x 256, with rows of whole vectors and without, last tiles and last blocks of K that are not full."""
+    """Tiles of every size, with rows of whole vectors and without, splits, last tiles and last blocks of K that are not full."""
     a, sa = whole(m + k, m, k, 1)
     b, sb = whole(n + k, n, k, 128 if blocks else 1)
     x, y = a.float() * plain.spread(sa, a.shape).float(), b.float() * plain.spread(sb, b.shape).float()
