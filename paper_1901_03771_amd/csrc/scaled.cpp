@@ -252,8 +252,8 @@ static int choose(Dot* d, int out, bool blocks) {
     d->nt = (int)((N + tn - 1) / tn);
     return (int64_t)d->mt * d->nt;
   };
-  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 18.5 us, by 4096 x 4088 25,
-  // by 4096 x 4095 29).
+  // Straight into LDS where rows are of whole vectors, do not overlap, and those of a tile lie within 2^31 bytes; else through registers (512 rows by 4096 x 4080: 18.5 us, by 4096 x 4088 and
+  // 4096 x 4095 25).
   auto direct = [&](const uint8_t* p, int64_t rows, int64_t s) { return (uintptr_t)p % 16 == 0 && (rows == 1 || (s % 16 == 0 && s >= K && s <= (int64_t(1) << 22))) && K <= (int64_t(1) << 22); };
   const bool straight = K % 16 == 0 && direct(d->a, M, d->a_s) && direct(d->b, N, d->b_s);
   // Few rows: bound by the memory that b is read from, which 256 workgroups keep busy.  Rounds of 16 blocks, and a join of splits, take what was measured (us).  (4 rows by 4096 x 4096: 7.5 with one, 8.8
@@ -270,27 +270,29 @@ static int choose(Dot* d, int out, bool blocks) {
     }
     return ((uintptr_t)d->a | (uintptr_t)d->b | (uintptr_t)(M > 1 ? d->a_s : 0) | (uintptr_t)(N > 1 ? d->b_s : 0) | (uintptr_t)(K % BLOCK ? K : 0)) % 4 == 0 ? DOT_FEW : DOT_FEW_WORDS;
   }
-  // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (one workgroup a compute unit; straight, bf16 results), whichever takes least by what was measured (us): a
-  // start, the blocks of a workgroup alone and what its neighbours add, rounds of them, and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 16 with 256 tiles of 64
+  // Else tiles of 128 rows of b and 64 or 128 of a, with splits of K, or of 256 x 256 (straight, bf16 results), whichever takes least by what was measured (us): a
+  // start, the blocks of a workgroup alone and what its neighbours add, rounds of one or two workgroups a compute unit, and the join of splits: a launch, its parts written and read.  (512 x 4096 x 4096: 16 with 256 tiles of 64
   // rows, 26 with 128 of 128 rows, 23 with those in two splits; 1024 x 8192 x 4096: 51 and 42; 64 x 4096 x 14336: 39, 25, 17, 17 with 1, 2, 4, 8; 192 x 4096 x 14336: 41, 27, 25, 28 with 1, 2, 5,
   // 8; 8192^3: 746, 602 and 451 with the three tiles; 2304 x 8192 x 4096, 288 of the largest: 105, 97, 106; 64 x 65536 x 4096: 68, 69, 77; with
-  // scales of b's rows 8192^3 674 and 625 with the larger two, 4096 x 6144 x 16384, 384 of the largest, 488 and 586; through registers, 512 x 4096 x 4095: 28 and 39, 1024 x 4096 x 4095: 46 and 40.)
+  // scales of b's rows 8192^3 674 and 625 with the larger two, 4096 x 6144 x 16384, 384 of the largest, 488 and 586; through registers, 512 x 4096 x 4095: 25 and 33, 1024 x 4096 x 4095: 44 and 33.)
   const bool proper = out == GR_F32;
-  struct Form { int which; int64_t high, wide; double start, alone, more; };
-  const Form low = straight ? Form{DOT_LOW, 64, 128, 3.0, proper ? 0.70 : blocks ? 0.34 : 0.42, proper ? 0.45 : blocks ? 0.35 : 0.37} : Form{DOT_STAGED_LOW, 64, 128, 3.0, proper ? 1.00 : 0.70, 0.62};
-  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 5.0, proper ? 1.13 : blocks ? 0.65 : 0.72, proper ? 0.72 : blocks ? 0.54 : 0.57} : Form{DOT_STAGED, 128, 128, 5.0, 1.05, 0.77};
-  const Form large = {DOT_LARGE, 256, 256, 6.0, blocks ? 0.60 : 1.20, blocks ? 1.15 : 1.20};
+  struct Form { int which; int64_t high, wide, slots; double start, alone, more; };
+  const Form low = straight ? Form{DOT_LOW, 64, 128, 512, 3.0, proper ? 0.70 : blocks ? 0.34 : 0.42, proper ? 0.45 : blocks ? 0.35 : 0.37}
+                            : Form{DOT_STAGED_LOW, 64, 128, 512, 3.0, proper ? 0.87 : 0.66, proper ? 0.95 : 0.66};
+  const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 512, 5.0, proper ? 1.13 : blocks ? 0.65 : 0.72, proper ? 0.72 : blocks ? 0.54 : 0.57}
+                               : Form{DOT_STAGED, 128, 128, 256, 5.0, proper ? 1.00 : 0.70, proper ? 0.30 : 0.19};
+  const Form large = {DOT_LARGE, 256, 256, 256, 6.0, blocks ? 0.60 : 1.20, blocks ? 1.15 : 1.20};
   const Form* best = nullptr;
   double least = 0.0;
   for (const Form* f : {&low, &middle, &large}) {
-    if (f == &middle && (M <= 64 || (!straight && proper))) continue;   // (rows at odd addresses and float32 together leave registers for 64 only)
+    if (f == &middle && M <= 64) continue;
     if (f == &large && (M <= 128 || !straight || proper)) continue;
     const int64_t tiles = tiles_of(f->high, f->wide);
     for (int64_t s = 1; s == 1 || (f != &large && s <= 16 && s <= KB / 4); ++s) {
-      const int64_t groups = tiles * s, slots = f == &large ? 256 : 512, over = groups % slots;
-      double beside = std::min(1.0, (double)groups / slots), rounds = 1.0;
-      if (f != &large) beside = groups > 256 ? 1.2 * beside - 0.2 : 0.0;
-      if (groups > slots) rounds = (double)(groups / slots) + (over == 0 ? 0.0 : f == &large ? 1.0 : 0.5 + 0.5 * (double)over / slots);
+      const int64_t groups = tiles * s, over = groups % f->slots;
+      double beside = std::min(1.0, (double)groups / f->slots), rounds = 1.0;
+      if (f->slots == 512) beside = groups > 256 ? 1.2 * beside - 0.2 : 0.0;
+      if (groups > f->slots) rounds = (double)(groups / f->slots) + (over == 0 ? 0.0 : f->slots == 256 ? 1.0 : 0.5 + 0.5 * (double)over / f->slots);
       const double us = f->start + (double)((KB + s - 1) / s) * rounds * (f->alone + f->more * beside) + (s > 1 ? 5.5 + (double)(s * M * N) * 8e-7 : 0.0);
       if (best && us >= least) continue;
       least = us;

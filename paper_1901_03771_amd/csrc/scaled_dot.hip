@@ -168,7 +168,9 @@ struct Flight {
 
 // A tile of TM rows of a by TN rows of b, waves WM x WN.  Stages of a block each in LDS: while one is multiplied, the others are under way, through registers (any strides) or straight
 // into LDS (DIRECT).  Two of them, or three for tiles of 64 rows, which have few products to hide a load behind (512 x 4096 x 4096: 15.7 us, with two 23, with four, whose LDS leaves a compute unit
-// one workgroup, 18.7; of 128 x 128, 26 with two and 28 with three).
+// one workgroup, 18.7; of 128 x 128, 26 with two and 28 with three).  Four waves, or eight through registers, where a
+// SIMD's second wave works while one moves bytes into place (777 x 1291 x 1003 in float32: 11.7 us, with four 13.6; 1024 x 4096 x 4095 33 and 40, but 4000 x 6000 x 3001 146 and 135; straight into
+// LDS, 192 x 4096 x 14336: 25.7 and 24.9).
 template <int TM, int TN, int WM, int WN, bool DIRECT, int STAGES, bool BLOCKS, class OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Dot d) {
   constexpr int THREADS = WM * WN * 64, I = TN / WN / 16, J = TM / WM / 16, NB = TN / BLOCK;
@@ -188,8 +190,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   const uint8_t* const a = d.a + (int64_t)m0 * d.a_s;
   const uint8_t* const b = d.b + (int64_t)n0 * d.b_s;
 
-  // blocks on their way through registers at once: as many as there are registers for (512 x 4096 x 4095: 29 us with two, 37 with one)
-  constexpr int SETS = TM == 64 ? 2 : 1;
+  constexpr int SETS = DIRECT ? 1 : 2;   // blocks on their way through registers at once (512 x 4096 x 4095 with four waves: 29 us with two, 37 with one)
   i32x4 staged[SETS][DIRECT ? 1 : CA + CB];
   const Flight<TM, THREADS> fa(a, d.a_s, rows_a, d.K, tid, lds);
   const Flight<TN, THREADS> fb(b, d.b_s, rows_b, d.K, tid, lds + TM * 128);
@@ -250,8 +251,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
   auto arrive_but_one = [&]() GR_INLINE { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(UNDER_WAY) : "memory"); };
 
   // Steps that operands of b are read ahead: a read from LDS takes longer than one step's products (8192^3: 465 us with one, 445 with two).  (With factors of their own for b's rows the
-  // registers hold one, of tiles of 256 x 256.)
-  constexpr int AHEAD = I == 8 && !BLOCKS ? 1 : 2, RING = 2 * AHEAD;
+  // registers hold one, of tiles of 256 x 256; waves with two steps a block read one ahead.)
+  constexpr int AHEAD = (I == 8 && !BLOCKS) || I == 2 ? 1 : 2, RING = 2 * AHEAD;
   constexpr int EARLY = AHEAD + I / 8;   // steps over which a tile is sent for
   constexpr bool PROPER = sizeof(OUT) == 4;
   f32x4 acc[I][J];
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gr_dot_scaled_kernel(const Do
 #pragma unroll
     for (int j = 0; j < J; ++j) read_a(j, even);
     constexpr std::integral_constant<int, 1> odd;
-    if constexpr (SETS > 1 && !DIRECT) {
+    if constexpr (SETS > 1) {
       // (one way out of the loop: with two, the compiler waits for the later set of loads, too)
       int kb = first;
       for (; kb + 1 < last; kb += 2) {
@@ -573,8 +574,8 @@ static hipError_t dot_of(const Dot& d, int form, hipStream_t stream) {
   if constexpr (sizeof(OUT) == 2) if (form == DOT_LARGE) return launch<256, 256, 4, 2, true, 2, BLOCKS, OUT>(d, stream);
   if (form == DOT_LOW) return launch<64, 128, 2, 2, true, 3, BLOCKS, OUT>(d, stream);
   if (form == DOT_DIRECT) return launch<128, 128, 2, 2, true, 2, BLOCKS, OUT>(d, stream);
-  if (form == DOT_STAGED_LOW) return launch<64, 128, 2, 2, false, 2, BLOCKS, OUT>(d, stream);
-  if constexpr (sizeof(OUT) == 2) if (form == DOT_STAGED) return launch<128, 128, 2, 2, false, 2, BLOCKS, OUT>(d, stream);
+  if (form == DOT_STAGED_LOW) return launch<64, 128, 2, 4, false, 2, BLOCKS, OUT>(d, stream);
+  if (form == DOT_STAGED) return launch<128, 128, 4, 2, false, 2, BLOCKS, OUT>(d, stream);
   return hipErrorInvalidValue;
 }
 
