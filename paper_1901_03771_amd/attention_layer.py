@@ -22,7 +22,8 @@ from . import lazy as gr
 
 class AttentionLayer:
     """y = attention(rotary(x Wq), rotary(x Wk), x Wv) Wo; x (B, N, width), `heads` heads of `values` values on `shared` heads of k and v.
-    norm: x / sqrt(mean(x ** 2)) * gain in its place.  eight: products of 8-bit tensors with scales, forward and backward."""
+    norm: x / sqrt(mean(x ** 2)) * gain in its place.  eight: products of 8-bit tensors with scales, forward and backward.
+    Every call takes the tensors in `weights` as they are then, whoever has written into them."""
 
     def __init__(self, ctx: gr.Context, width: int, heads: int, shared: int, values: int, cap: float = 0.0, seed: int = 0, norm: bool = False, eight: bool = False):
         self.ctx, self.width, self.heads, self.shared, self.values, self.cap = ctx, width, heads, shared, values, cap
@@ -35,20 +36,24 @@ class AttentionLayer:
             self.weights["gain"] = torch.ones(width, device=device)
         self._w = {name: ctx.array(t) for name, t in self.weights.items()}
         self.frequencies = gr.rotary_frequencies(values)
-        self._eight = {}   # of each weight, as the products of the forward pass and of the gradients take it
 
     def _weight8(self, name: str, transposed: bool):
-        """The weight in 8 bits, in blocks: (columns, rows) for products with it, or as it lies for those with its transpose.  Laid out once until it is changed."""
-        if (name, transposed) not in self._eight:
-            self._eight[name, transposed] = gr.quantize(self._w[name], blocks=True, transposed=transposed)
-        return self._eight[name, transposed]
+        """The weight in 8 bits, in blocks: (columns, rows) for products with it, or as it lies for those with its transpose."""
+        return gr.quantize(self._w[name], blocks=True, transposed=transposed)
 
-    def _product(self, x, name: str):
+    def laid_out(self):
+        """The weights in 8 bits as `forward` and `step` take them, for a program that makes many calls of weights that stay; None without eight.  They are those of now:
+        the layer keeps none, and after a change of the weights the program lays them out again."""
+        return {name: self._weight8(name, True) for name in "qkvo"} if self.eight else None
+
+    def _product(self, x, name: str, laid=None):
         """x W; with eight, x may come as (values, scales) already."""
+        if laid is not None and not self.eight:
+            raise ValueError("weights in 8 bits for a layer in float32")
         if not self.eight:
             return gr.dot(x, self._w[name])
         q, s = x if isinstance(x, tuple) else gr.quantize(x)
-        return gr.dot_scaled(q, s, *self._weight8(name, True), dtype=gr.GR_F32)
+        return gr.dot_scaled(q, s, *(laid[name] if laid else self._weight8(name, True)), dtype=gr.GR_F32)
 
     def _product_back(self, dy, name: str):
         """dy W'."""
@@ -69,20 +74,20 @@ class AttentionLayer:
         h, _, scales = gr.rms_norm(lx, self._w["gain"], eight=self.eight)
         return (h, scales) if self.eight else h
 
-    def _projected(self, x, name: str, shape):
-        return gr.reshape(self._product(x, name), shape)
+    def _projected(self, x, name: str, shape, laid):
+        return gr.reshape(self._product(x, name, laid), shape)
 
-    def forward(self, x, positions, documents):
-        """Returns y (B * N, width), unevaluated, and what the gradient needs."""
+    def forward(self, x, positions, documents, laid=None):
+        """Returns y (B * N, width), unevaluated, and what the gradient needs.  laid: the weights as `laid_out` gave them, in place of those of now."""
         B, N, _ = x.shape
         lx = self.ctx.array(x.view(B * N, self.width))
         h = self._normed(lx)
-        q = gr.rotary(self._projected(h, "q", (B, N, self.heads, self.values)), self.frequencies, positions)
-        k = gr.rotary(self._projected(h, "k", (B, N, self.shared, self.values)), self.frequencies, positions)
-        v = self._projected(h, "v", (B, N, self.shared, self.values)).materialize()
+        q = gr.rotary(self._projected(h, "q", (B, N, self.heads, self.values), laid), self.frequencies, positions)
+        k = gr.rotary(self._projected(h, "k", (B, N, self.shared, self.values), laid), self.frequencies, positions)
+        v = self._projected(h, "v", (B, N, self.shared, self.values), laid).materialize()
         scores = self.ctx.scores(cap=self.cap, causal=True, documents=documents)
         out, lse = gr.attention(q, k, v, scores)
-        y = self._product(gr.reshape(out, (B * N, self.heads * self.values)), "o")
+        y = self._product(gr.reshape(out, (B * N, self.heads * self.values)), "o", laid)
         return y, (lx, h, positions, scores, q, k, v, out, lse)
 
     def gradients(self, dy, kept):
@@ -116,25 +121,24 @@ class AttentionLayer:
         for name, g in grads.items():
             w = self._w[name]
             w[tuple([slice(None)] * w.ndim)] = w - g * rate
-        self._eight.clear()
         return float(loss.numpy()) / (rows * self.width)
 
-    def step(self, x, cache_k, cache_v, lengths):
+    def step(self, x, cache_k, cache_v, lengths, laid=None):
         """The next token x (B, width) of each sequence: its k and v go into row lengths[b] of the caches (B, M, shared, values), lengths (i32)
-        grows by one, and y (B, width) comes back as a tensor."""
+        grows by one, and y (B, width) comes back as a tensor.  laid: as for `forward`."""
         B = x.shape[0]
         h = self._normed(self.ctx.array(x))
         positions = self.ctx.array(lengths.view(B, 1))
-        q = gr.rotary(self._projected(h, "q", (B, 1, self.heads, self.values)), self.frequencies, positions)
-        k = gr.rotary(self._projected(h, "k", (B, 1, self.shared, self.values)), self.frequencies, positions)
-        v = self._projected(h, "v", (B, 1, self.shared, self.values))
+        q = gr.rotary(self._projected(h, "q", (B, 1, self.heads, self.values), laid), self.frequencies, positions)
+        k = gr.rotary(self._projected(h, "k", (B, 1, self.shared, self.values), laid), self.frequencies, positions)
+        v = self._projected(h, "v", (B, 1, self.shared, self.values), laid)
         each, at = torch.arange(B, device=x.device), lengths.long()
         cache_k[each, at] = k.torch(copy=False)[:, 0]
         cache_v[each, at] = v.torch(copy=False)[:, 0]
         lengths += 1
         out = gr.attention_step(self.ctx.array(q.torch(copy=False)[:, 0]), self.ctx.array(cache_k), self.ctx.array(cache_v),
                                 self.ctx.scores(cap=self.cap, lengths=self.ctx.array(lengths)))
-        return self._product(gr.reshape(out, (B, self.heads * self.values)), "o").torch()
+        return self._product(gr.reshape(out, (B, self.heads * self.values)), "o", laid).torch()
 
 
 def packed_documents(batch: int, rows: int, device, seed: int = 0):
@@ -159,11 +163,12 @@ def main(arguments=()):
     for i in range(8):
         print(f"step {i}: mean square {layer.train_step(x, target, positions, documents, rate=20.0):.4f}", flush=True)
     one = x[:, :32].contiguous()
-    whole, _ = layer.forward(one, 0, None)
+    laid = layer.laid_out()   # generation leaves the weights as they are
+    whole, _ = layer.forward(one, 0, None, laid)
     whole = whole.torch().view(2, 32, 64)
     cache = [torch.full((2, 40, 2, 32), float("nan"), device=device) for _ in range(2)]   # rows that hold nothing yet have no say
     lengths = torch.zeros(2, dtype=torch.int32, device=device)
-    rows = torch.stack([layer.step(one[:, i].contiguous(), *cache, lengths) for i in range(32)], 1)
+    rows = torch.stack([layer.step(one[:, i].contiguous(), *cache, lengths, laid) for i in range(32)], 1)
     print(f"generated rows differ from the forward pass by {float((rows - whole).abs().max()):.2e} at most")
     ctx.close()
 

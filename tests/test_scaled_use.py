@@ -1,0 +1,69 @@
+"""Norms, 8-bit tensors and their products as programs use them: a layer whose weights change, calls that fail after their launch, errors that other calls have
+left."""
+import pytest
+import torch
+
+from paper_1901_03771_amd import lazy as gr
+
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+
+def wide_layer(c, norm, eight=True):
+    from paper_1901_03771_amd import attention_layer as al
+    return al.AttentionLayer(c, width=144, heads=4, shared=2, values=24, cap=8.0, seed=4, norm=norm, eight=eight)
+
+
+def results_of(layer, **laid):
+    """What the layer answers for the same rows: of a forward pass, its gradients and two tokens of generation."""
+    g = torch.Generator().manual_seed(7)
+    x, dy = torch.randn(2, 70, 144, generator=g).cuda(), torch.randn(140, 144, generator=g).cuda()
+    y, kept = layer.forward(x, 0, None, **laid)
+    got = {"y": y.torch(), **{n: t.torch() for n, t in layer.gradients(layer.ctx.array(dy), kept).items()}}
+    cache = [torch.zeros(2, 4, 2, 24, device="cuda") for _ in range(2)]
+    lengths = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for i in range(2):
+        got[f"token {i}"] = layer.step(x[:, i].contiguous(), *cache, lengths, **laid)
+    return got
+
+
+def same(a, b):
+    return {n for n in a if torch.equal(a[n], b[n])}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("norm", [False, True], ids=["plain", "norm"])
+def test_layer_in_eight_bits_takes_its_weights_as_they_are(norm):
+    """Weights that a caller's own optimizer, a checkpoint or an assignment through the lazy arrays has changed, between calls that have used them."""
+    c = gr.Context()
+    layer, other = wide_layer(c, norm), wide_layer(c, norm)
+    first = results_of(layer)
+    g = torch.Generator().manual_seed(8)
+    new = {n: t.cpu() + 0.1 * torch.randn(t.shape, generator=g) for n, t in layer.weights.items()}
+    changes = [lambda t, v: t.copy_(v), lambda t, v: t.data.copy_(v), lambda t, v: c.array(t).__setitem__((slice(None),) * t.dim(), c.array(v) * 1.0)]
+    for i, (name, t) in enumerate(layer.weights.items()):
+        v = new[name].cuda()
+        changes[i % 3](t, v)
+        assert torch.equal(t, v)
+        other.weights[name].copy_(v)
+    torch.cuda.synchronize()
+    now, want = results_of(layer), results_of(other)      # (the other layer's first calls)
+    assert same(now, want) == set(want) and not same(now, first)
+    c.close()
+
+
+@pytest.mark.gpu
+def test_layer_with_weights_that_a_program_has_laid_out():
+    """They give what the weights gave that they were made of, until the program makes them anew; the gradients are always of the weights themselves."""
+    c = gr.Context()
+    layer = wide_layer(c, True)
+    first, laid = results_of(layer), layer.laid_out()
+    assert same(results_of(layer, laid=laid), first) == set(first)
+    for t in layer.weights.values():
+        t.mul_(1.25)
+    now, old = results_of(layer), results_of(layer, laid=laid)
+    assert not same(now, first) and not same(now, old)
+    assert same(results_of(layer, laid=layer.laid_out()), now) == set(first)
+    assert wide_layer(c, True, eight=False).laid_out() is None
+    with pytest.raises(ValueError):
+        results_of(wide_layer(c, True, eight=False), laid=laid)
+    c.close()
