@@ -53,6 +53,7 @@ static __typeof__(&gr_release) p_release;
 static __typeof__(&gr_reduce) p_reduce;
 static __typeof__(&gr_ndim) p_ndim;
 static __typeof__(&gr_shape) p_shape;
+static __typeof__(&gr_dtype_of) p_dtype_of;
 static __typeof__(&gr_rms_norm) p_rms_norm;
 static __typeof__(&gr_rms_norm_grad) p_rms_norm_grad;
 static __typeof__(&gr_quantize) p_quantize;
@@ -599,8 +600,10 @@ static PyObject* mod_rms_norm(PyObject* m, PyObject* const* args, Py_ssize_t nar
   gr_ctx* ctx;
   gr_array h[6];
   double v[2];
+  gr_dtype dt;
   if (nargs != 8) { PyErr_SetString(PyExc_TypeError, "rms_norm(x, residual, weight, total, out, scales, eps, offset)"); return NULL; }
   if (!handles(args, 6, 0x2e, &ctx, h) || !numbers(args + 6, 2, v)) Py_RETURN_NONE;
+  if (!h[5] && p_dtype_of(ctx, h[4], &dt) == GR_OK && dt == GR_E4M3) Py_RETURN_NONE;   /* its scales are to be new */
   return PyLong_FromLong(p_rms_norm(ctx, h[0], h[1], h[2], v[0], v[1], h[3], h[4], h[5]));
 }
 
@@ -649,7 +652,7 @@ static PyObject* mod_bind(PyObject* m, PyObject* d) {
       !take_address(d, "gr_materialize_into_static", (void**)&p_materialize_into_static) ||
       !take_address(d, "gr_is_materialized", (void**)&p_is_materialized) ||
       !take_address(d, "gr_program_run", (void**)&p_program_run) ||
-      !take_address(d, "gr_rms_norm", (void**)&p_rms_norm) || !take_address(d, "gr_rms_norm_grad", (void**)&p_rms_norm_grad) ||
+      !take_address(d, "gr_dtype_of", (void**)&p_dtype_of) || !take_address(d, "gr_rms_norm", (void**)&p_rms_norm) || !take_address(d, "gr_rms_norm_grad", (void**)&p_rms_norm_grad) ||
       !take_address(d, "gr_quantize", (void**)&p_quantize) || !take_address(d, "gr_dot_scaled", (void**)&p_dot_scaled))
     return NULL;
   Py_RETURN_NONE;

@@ -577,7 +577,7 @@ def _bind_fast_paths(L):
         return
     names = ["gr_array_from_device", "gr_unary", "gr_binary", "gr_binary_scalar", "gr_slice", "gr_transpose", "gr_dot", "gr_assign",
              "gr_materialize", "gr_release", "gr_reduce", "gr_ndim", "gr_shape", "gr_materialize_into",
-             "gr_materialize_into_static", "gr_is_materialized", "gr_program_run", "gr_rms_norm", "gr_rms_norm_grad", "gr_quantize",
+             "gr_materialize_into_static", "gr_is_materialized", "gr_program_run", "gr_dtype_of", "gr_rms_norm", "gr_rms_norm_grad", "gr_quantize",
              "gr_dot_scaled"]
     _fastbind.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names})
     _fastbind.set_hooks(_binary_slow, slice_, _setitem_slow, _pow_slow, _reduce_slow)
@@ -1000,9 +1000,10 @@ def rms_norm(x: "Array", weight=None, residual=None, eps: float = 1e-6, offset: 
     eight=True, is the result in 8 bits with scales of rows, as ``dot_scaled`` takes it; else scales is None."""
     if _fastbind is not None and out is not None and (scales is not None or not eight) and (residual is None or total is not None):
         st = _fastbind.rms_norm(x, residual, weight, None if total is False else total, out, scales, eps, offset)
-        if st == 0:
+        if st is not None:   # (None is also an 8-bit result whose scales are to be new.  A failure may come after the launch: the call is not made again)
+            if st:
+                _context_of(x).check(st)
             return out, x if residual is None else None if total is False else total, scales
-        # (what is wrong, or an 8-bit result whose scales are to be new: neither has run, the call is a single launch)
     ctx = _context_of(x)
     hx, hr, hw = _tensor(ctx, x), _optional(ctx, residual), _optional(ctx, weight)
     if out is None or (total is None and residual is not None) or scales is None:

@@ -4,10 +4,58 @@ import pytest
 import torch
 
 from paper_1901_03771_amd import lazy as gr
+from test_attention import Specs, dry, refused  # noqa: F401
 
-F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+# ---------------------------------------------------------------- without a GPU --
+class FailsAfterwards:
+    """The binding's C type, whose calls with kernels of their own run and then report a failure."""
+
+    def __init__(self, real):
+        self.real = real
+
+    def __getattr__(self, name):
+        f = getattr(self.real, name)
+        if name not in ("rms_norm", "rms_norm_grad", "quantize", "dot_scaled"):
+            return f
+
+        def call(*a):
+            st = f(*a)
+            return 8 if st == 0 else st   # GR_ERR_HIP
+        return call
 
 
+def test_a_failure_after_a_launch_is_reported_and_the_call_not_repeated(dry, monkeypatch):  # noqa: F811
+    """A norm in place that ran twice would have added its residual to its own result."""
+    s = Specs(dry)
+    x, res, out, w, dw, q, sc = s((6, 200)), s((6, 200)), s((6, 200)), s((200,)), s((200,)), s((6, 200), gr.GR_E4M3), s((6, 2))
+    b, sb, y = s((70, 200), gr.GR_E4M3), s((70, 2)), s((6, 70))
+    monkeypatch.setattr(gr, "_fastbind", FailsAfterwards(gr._fastbind))
+    for call, launches in ((lambda: gr.rms_norm(x, w, res, out=x, total=res), 1), (lambda: gr.rms_norm(x, w, res, out=q, total=res, scales=sc), 1),
+                           (lambda: gr.rms_norm(x, out=q, scales=sc, eight=True), 1), (lambda: gr.rms_norm(x, w, res, out=out, total=False), 1),
+                           (lambda: gr.rms_norm_grad(x, res, w, dx=out, dweight=dw), 2), (lambda: gr.quantize(x, out=q, scales=sc), 1),
+                           (lambda: gr.dot_scaled(q, sc, b, sb, out=y), 1)):
+        n = dry.stats()["kernel_launches"]
+        refused("GR_ERR_HIP", call)
+        assert dry.stats()["kernel_launches"] == n + launches
+
+
+def test_an_8_bit_result_without_scales_goes_the_longer_way_at_once(dry, monkeypatch):  # noqa: F811
+    """No call of the library is refused on the way to the new scales."""
+    s = Specs(dry)
+    x, q = s((6, 200)), s((6, 200), gr.GR_E4M3)
+    answers = []
+
+    class Watched(FailsAfterwards):
+        def __getattr__(self, name):
+            f = getattr(self.real, name)
+            return (lambda *a: answers.append(f(*a)) or answers[-1]) if name == "rms_norm" else f
+    monkeypatch.setattr(gr, "_fastbind", Watched(gr._fastbind))
+    refused("GR_ERR_NODEVICE", gr.rms_norm, x, out=q)                     # (a dry context has no memory for new scales)
+    assert answers == [None]
+
+
+# ------------------------------------------------------------------- on the GPU --
 def wide_layer(c, norm, eight=True):
     from paper_1901_03771_amd import attention_layer as al
     return al.AttentionLayer(c, width=144, heads=4, shared=2, values=24, cap=8.0, seed=4, norm=norm, eight=eight)
