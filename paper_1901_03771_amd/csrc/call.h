@@ -189,6 +189,7 @@ struct Call {
       }
       CALL_HIP(ctx, hipEventRecord(e0, ctx->stream));
     }
+    (void)hipGetLastError();   // (an error that an earlier call of the thread has left would be taken for the launch's)
     CALL_HIP(ctx, f());
     if (profile) {
       CALL_HIP(ctx, hipEventRecord(e1, ctx->stream));

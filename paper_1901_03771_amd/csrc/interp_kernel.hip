@@ -422,7 +422,9 @@ __global__ __launch_bounds__(256) void gr_interp_gemm_kernel(GrInterpGenArgs A) 
   *(GM unsigned*)(a.out + 4ull * (unsigned long long)o) = my[A.slot * 256];
 }
 
+// (Before each launch: an error that an earlier call of the thread has left would be taken for the launch's.)
 extern "C" int gr_launch_interp_gen(void* stream, const GrInterpGenArgs* args, unsigned grid) {
+  (void)hipGetLastError();
   switch (args->kind) {
     case GI_KIND_REDUCE: hipLaunchKernelGGL(gr_interp_reduce_kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, *args); break;
     case GI_KIND_SCAN: hipLaunchKernelGGL(gr_interp_scan_kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, *args); break;
@@ -434,11 +436,13 @@ extern "C" int gr_launch_interp_gen(void* stream, const GrInterpGenArgs* args, u
 }
 
 extern "C" int gr_launch_interp_rowred(void* stream, const GrInterpRowArgs* args, unsigned grid) {
+  (void)hipGetLastError();
   hipLaunchKernelGGL(gr_interp_rowred_kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, *args);
   return (int)hipGetLastError();
 }
 
 extern "C" int gr_launch_interp_map(void* stream, const GrInterpArgs* args, unsigned grid) {
+  (void)hipGetLastError();
   hipLaunchKernelGGL(gr_interp_map_kernel, dim3(grid), dim3(256), 0, (hipStream_t)stream, *args);
   return (int)hipGetLastError();
 }

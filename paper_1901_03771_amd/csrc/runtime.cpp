@@ -1758,6 +1758,7 @@ gr_status gr_stream_copy(gr_ctx* ctx, void* dst, const void* src, size_t bytes) 
   uintptr_t d = (uintptr_t)dst, s = (uintptr_t)src;
   if (d < s + bytes && s < d + bytes) return fail(ctx, GR_ERR_ALIAS, "stream_copy: buffers overlap");
   if (bytes == 0) return GR_OK;
+  (void)hipGetLastError();   // (an earlier call's)
   gr_launch_stream_copy(ctx->stream, dst, src, bytes / 16);
   GR_HIP(ctx, hipGetLastError());
   return GR_OK;
@@ -1768,6 +1769,7 @@ gr_status gr_stream_read(gr_ctx* ctx, const void* src, size_t bytes, void* sink)
   if (ctx->device < 0) return fail(ctx, GR_ERR_NODEVICE, "context has no device");
   if (bytes % 16 || ((uintptr_t)src % 16) || ((uintptr_t)sink % 4)) return fail(ctx, GR_ERR_ARG, "stream_read: size and pointer must be multiples of 16");
   if (bytes == 0) return GR_OK;
+  (void)hipGetLastError();   // (an earlier call's)
   gr_launch_stream_read(ctx->stream, src, bytes / 16, sink);
   GR_HIP(ctx, hipGetLastError());
   return GR_OK;

@@ -1,5 +1,7 @@
 """Norms, 8-bit tensors and their products as programs use them: a layer whose weights change, calls that fail after their launch, errors that other calls have
 left."""
+import ctypes
+
 import pytest
 import torch
 
@@ -114,4 +116,56 @@ def test_layer_with_weights_that_a_program_has_laid_out():
     assert wide_layer(c, True, eight=False).laid_out() is None
     with pytest.raises(ValueError):
         results_of(wide_layer(c, True, eight=False), laid=laid)
+    c.close()
+
+
+@pytest.mark.gpu
+def test_an_error_that_an_earlier_call_left_is_not_taken_for_the_launchs():
+    """HIP keeps a thread's last error until somebody asks for it: a launch that goes through is not failed by it."""
+    hip = gr.lib()                                                           # (its dependencies' names are found through it)
+    hip.hipSetDevice.argtypes, hip.hipSetDevice.restype = [ctypes.c_int], ctypes.c_int
+    c = gr.Context()
+    A = c.array
+    leave = lambda: hip.hipSetDevice(1 << 20)  # noqa: E731  (refused by the runtime)
+    x, w, one = torch.randn(40, 256, device="cuda"), torch.randn(256, device="cuda"), torch.ones(40, 256, device="cuda")
+    heads = torch.randn(1, 40, 2, 64, device="cuda")
+    torch.cuda.synchronize()
+    b, sb = gr.quantize(A(w[None].expand(30, 256).contiguous()))
+
+    def calls():
+        total, normed, copy = x.clone(), one.clone(), torch.empty(40, 256, device="cuda")
+        torch.cuda.synchronize()
+
+        def run(f):
+            assert leave() != 0
+            return f()
+        run(lambda: gr.rms_norm(A(normed), A(w), A(total), out=A(normed), total=A(total)))     # once: the residual is added to the stream in place
+        q, s = run(lambda: gr.quantize(A(x)))
+        y = run(lambda: gr.dot_scaled(q, s, b, sb))
+        dx, dw = run(lambda: gr.rms_norm_grad(A(one), A(x), A(w)))
+        out, _ = run(lambda: gr.attention(A(heads), A(heads), A(heads), c.scores()))
+        turned = run(lambda: gr.rotary(A(heads), gr.rotary_frequencies(64), 3))
+        run(lambda: c.stream_copy(copy, x))
+        got = [total, normed, *(t.torch().float() for t in (q, s, y, dx, dw, out, turned)), copy]
+        c.sync()
+        return got
+
+    got = calls()
+    leave = lambda: 1  # noqa: E731
+    assert all(torch.equal(a, b) for a, b in zip(got, calls()))
+    assert torch.equal(got[0], x + 1) and torch.equal(got[-1], x)
+    c.close()
+
+
+@pytest.mark.gpu
+def test_an_error_that_an_earlier_call_left_is_not_taken_for_the_interpreters():
+    hip = gr.lib()
+    hip.hipSetDevice.argtypes, hip.hipSetDevice.restype = [ctypes.c_int], ctypes.c_int
+    c = gr.Context()
+    c.set_option("interp", 2)
+    x = torch.rand(300, 200, device="cuda")
+    a = c.array(x)
+    for f, want in ((lambda: gr.exp(a * 0.5) + 0.25, torch.exp(x * 0.5) + 0.25), (lambda: (a * 3.0).sum(axis=1), (x * 3.0).sum(1)), (lambda: a.cumsum(0), x.cumsum(0))):
+        assert hip.hipSetDevice(1 << 20) != 0
+        assert torch.allclose(f().torch(), want, rtol=1e-4)   # (of up to 300 positive values: 300 2^-24 each)
     c.close()
