@@ -282,13 +282,14 @@ static int choose(Dot* d, int out, bool blocks) {
   const Form middle = straight ? Form{DOT_DIRECT, 128, 128, 512, 5.0, proper ? 1.13 : blocks ? 0.65 : 0.72, proper ? 0.72 : blocks ? 0.54 : 0.57}
                                : Form{DOT_STAGED, 128, 128, 256, 5.0, proper ? 1.00 : 0.70, proper ? 0.30 : 0.19};
   const Form large = {DOT_LARGE, 256, 256, 256, 6.0, blocks ? 0.60 : 1.20, blocks ? 1.15 : 1.20};
+  // A launch holds GROUPS workgroups of any form; where tiles of 64 rows are more, those of 128 rows are no more than that.
   const Form* best = nullptr;
   double least = 0.0;
   for (const Form* f : {&low, &middle, &large}) {
     if (f == &middle && M <= 64) continue;
     if (f == &large && (M <= 128 || !straight || proper)) continue;
     const int64_t tiles = tiles_of(f->high, f->wide);
-    for (int64_t s = 1; s == 1 || (f != &large && s <= 16 && s <= KB / 4); ++s) {
+    for (int64_t s = 1; tiles * s <= GROUPS && (s == 1 || (f != &large && s <= 16 && s <= KB / 4)); ++s) {
       const int64_t groups = tiles * s, over = groups % f->slots;
       double beside = std::min(1.0, (double)groups / f->slots), rounds = 1.0;
       if (f->slots == 512) beside = groups > 256 ? 1.2 * beside - 0.2 : 0.0;

@@ -169,3 +169,20 @@ def test_an_error_that_an_earlier_call_left_is_not_taken_for_the_interpreters():
         assert hip.hipSetDevice(1 << 20) != 0
         assert torch.allclose(f().torch(), want, rtol=1e-4)   # (of up to 300 positive values: 300 2^-24 each)
     c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n", [(1 << 18, 1 << 18), (449, (1 << 27) - 127)])
+def test_a_product_over_nothing_of_as_many_tiles_as_a_launch_holds(m, n):
+    """2^22 tiles of 128 x 128: with twice as many of 64 x 128 the launch would pass 2^32 threads.  All results are zero, and written."""
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("128 GiB of results")
+    c = gr.Context()
+    none = lambda *shape, dtype=torch.uint8: torch.empty(*shape, device="cuda", dtype=dtype)  # noqa: E731
+    out = torch.empty(m * n, dtype=torch.bfloat16, device="cuda").fill_(3.0).view(m, n)
+    gr.dot_scaled(*(c.array(t) for t in
+                     (none(m, 0).view(torch.float8_e4m3fn), none(m, 0, dtype=torch.float32), none(n, 0).view(torch.float8_e4m3fn), none((n + 127) // 128, 0, dtype=torch.float32))), out=c.array(out))
+    assert not any(bool(part.any()) for part in out.view(torch.int16).flatten().split(1 << 33))
+    del out
+    torch.cuda.empty_cache()
+    c.close()
