@@ -17,6 +17,7 @@
  *     nearest e4m3, ties to even.  Where one of the values of a scale is infinite or NaN, the scale and all its values are NaN.
  *   - The values of a row (the last axis) of every tensor are neighbours, or GR_ERR_UNSUPPORTED; rows may lie anywhere.  The elements of a result do
  *     not overlap (GR_ERR_UNSUPPORTED), nor do two results or a result and an operand (GR_ERR_ALIAS), except where a call says so.
+ *   - A call that answers GR_ERR_HIP may have been launched: what its results hold is not known, and over operands it is not to be made again.
  *   - Temporary memory and captured graphs: as in grumpy_hip_attention.h, with whose calls these share it.
  *   - Results do not depend on timing: every sum is taken in an order fixed by the shapes.
  */

@@ -1,7 +1,9 @@
 // Root-mean-square norms: r = 1 / sqrt(mean(t^2) + eps), y = t r (offset + weight) of t = x or of the rounded sum x + residual; and the gradient
 //   g = dout (offset + weight),  dx = r g - t r^3 mean(g t) + dtotal,  dweight = sum over rows of dout t r.
 // What is read and written of the tensors bounds them.  A row is shared by 16 to 1024 threads and stays in their registers between the sum and its
-// use, so that every tensor passes once; a workgroup goes through rows with the weights, and the sums for dweight, in registers too.
+// use, so that every tensor passes once; a workgroup goes through rows with the weights, and the sums for dweight, in registers too.  1024 threads of 128 registers hold that up to 16384 values (a
+// gradient's in f32: 8192); of longer rows part of it lies in scratch memory, which every row reads, and gradients over 16384 values write too (1000 rows of 16384 and 32768 values: gradients in bf16 31 and
+// 168 us, in f32 62 and 246; bf16 to 8 bits 17.0 and 36.7).
 // 16384 rows of 8192 bf16 values with a residual, to 8 bits: 165 us, 5.7 TB/s; the gradient of 8192 rows of 4096: 52 us, 5.2 TB/s.
 #include "scaled_kernels.h"
 
@@ -15,7 +17,8 @@ static __device__ __forceinline__ T* row_at(const Rows& r, const Norm& a, int64_
   return (T*)r.p + h * r.s0 + j * r.s1 + k * r.s2;
 }
 
-// The weights of the thread's values, to which the offset is added where they are used: so the first row's loads need not wait for them.  1 where there are none.
+// The weights of the thread's values, to which the offset is added where they are used: so the first row's loads need not wait for them.  1 where there are none.  Only f32 ones side by side come as vectors (8
+// rows of 4096 bf16 values to 8 bits: 3.6 us, with bf16 weights 5.2).
 template <int TPR, int V, int N>
 static __device__ __forceinline__ void weights(const Norm& a, int t, float (&w)[V][N]) {
 #pragma unroll
